@@ -67,6 +67,7 @@
 #ifndef DD_H
 #define DD_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -322,6 +323,155 @@ dd_status dd_simulate_policy(const dd_graph *g, const dd_variants *var, int32_t 
                              const uint8_t *pp, const int32_t *prio,
                              int64_t *d_finish, int64_t *d_start, int64_t *d_makespan,
                              void *stream);
+
+/* ---------------------------------------------------------------------------
+ * The operators that three of the what-if models predict, to run them and
+ * hold the prediction against the measurement (the paper's own check, Sec. 6):
+ * a fused weight update (What_If_Fused_Adam), low-precision weights with f32
+ * masters (What_If_AMP), and the element-wise kernels around a block's
+ * normalization fused into one (What_If_Restructuring_Batchnorm).
+ *
+ *   - All tensors are device memory of the caller, on the current device, and
+ *     are aligned to their elements; nothing is copied.
+ *   - Every call but dd_tensors_load is asynchronous on `stream`, and its
+ *     results are the same bits on every run.
+ *   - Values are computed in 32 bits or more and rounded once, to nearest
+ *     even, where they are stored.
+ */
+#define DD_F32 0
+#define DD_BF16 1
+#define DD_F16 2
+#define DD_E4M3 3     /* 8 bits, largest value 448, no infinities (OCP) */
+#define DD_I8 4
+
+typedef struct dd_tensors dd_tensors;
+
+/*
+ * One tensor of a model: n elements in a row.  grad is required when n > 0.
+ * For dd_adam_step, param (the weights the model reads), m and v are required
+ * for all tensors of a list or for none, and master for a param of 16 bits
+ * (NULL for one of 32).
+ */
+typedef struct {
+    void *grad;           /* grad_type [n] */
+    void *param;          /* param_type [n] */
+    float *master;        /* [n] f32 weights that a 16-bit param is the rounding of */
+    float *m, *v;         /* [n] moments */
+    int64_t n;
+    int32_t grad_type, param_type;   /* DD_F32, DD_BF16 or DD_F16 */
+    int32_t no_decay;     /* 1: weight decay does not apply to this tensor */
+    int32_t reserved;     /* 0 */
+} dd_tensor;
+
+/*
+ * dd_tensors_load -- a list of tensors that is worked on in one launch.
+ *   t   host array of `count` tensors (copied).
+ * The tensors stay where they are for the life of the handle.  The handle
+ * keeps 64 bytes of device memory per chunk (2,048 to 32,768 elements of a
+ * tensor), and the partial sums of dd_grad_norm: calls that use one handle on
+ * several streams are put in order by the library.  Waits for `stream`.
+ */
+dd_status dd_tensors_load(int32_t count, const dd_tensor *t, void *stream, dd_tensors **out);
+void dd_tensors_free(dd_tensors *t);
+
+/*
+ * dd_grad_norm -- the norm of all gradients of a list taken as one vector.
+ *   d_inv_scale  device float [1] or NULL: 1 / loss scale, u below (NULL: 1).
+ *   d_stats      device float [3], written:
+ *                [0] norm    u * sqrt(sum of grad^2), summed in 64 bits;
+ *                [1] factor  u * min(1, max_norm / norm), what to multiply
+ *                            the gradients with; u if max_norm <= 0; 0 if [2];
+ *                [2] skip    1 if some gradient is infinite or not a number
+ *                            (or the norm is, in 64 bits), else 0.
+ */
+dd_status dd_grad_norm(const dd_tensors *t, float max_norm, const float *d_inv_scale, float *d_stats,
+                       void *stream);
+
+/*
+ * dd_grad_clip -- gradients times d_stats[1], rounded to dst's types, into the
+ * gradients of dst (which may be src): unscaled and clipped, or zeros where
+ * the factor is 0.  Both lists have the same number of tensors and sizes
+ * (DD_EMISMATCH); their types and everything but the gradients may differ.
+ * Unless dst is src, the memory of the two must not overlap.
+ */
+dd_status dd_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float *d_stats, void *stream);
+
+/*
+ * dd_adam_step -- one step of Adam on every tensor of a list, in place.
+ *   d_step       device int64 [1]: steps taken before; one more after the call.
+ *   d_stats      as dd_grad_norm wrote it, or NULL: the gradients are
+ *                multiplied with [1] as they are read, and nothing changes
+ *                (d_step neither) if [2] is not 0.
+ *   decoupled    1: weight decay shrinks the weight by lr * weight_decay;
+ *                0: it is added to the gradient.
+ * With t = d_step + 1, g = grad * factor (+ weight_decay * w if not decoupled):
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   w = (1 - lr weight_decay) w (if decoupled)
+ *   w = w - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * where w is master if there is one (param becomes its rounding), else param.
+ * DD_EINVAL unless lr >= 0, 0 <= beta < 1, eps >= 0 and weight_decay >= 0, all
+ * finite, or when the list has no params.
+ */
+dd_status dd_adam_step(const dd_tensors *t, int64_t *d_step, const float *d_stats, double lr, double beta1,
+                       double beta2, double eps, double weight_decay, int32_t decoupled, void *stream);
+
+/*
+ * dd_rms_norm -- for every row, with s = x + residual (x alone if residual is
+ * NULL), in 32 bits:
+ *   rstd = 1 / sqrt(mean of s^2 over the row + eps),   y = s * rstd * weight
+ *   out  = y in `type`, or in 8 bits (out_type DD_E4M3 or DD_I8): for the row,
+ *          or each group of columns (the last may be shorter),
+ *          scale = max(largest |y|, 2^-100) / 448 (/ 127 for DD_I8) and
+ *          out = y / scale.  A NaN in a group makes its scale a NaN.
+ *   h    = s in `type` (optional).
+ * A row is `cols` consecutive elements; rows start `*_stride` elements apart
+ * (of an input any stride, 0 included: the same row for all; of an output at
+ * least cols).  out (of 16 or 32 bits) and h may each be x or residual
+ * themselves, element for element; outputs must not overlap otherwise.
+ */
+typedef struct {
+    int64_t rows, cols;
+    int64_t x_stride, residual_stride, h_stride, out_stride;
+    const void *x, *residual;    /* type; residual may be NULL */
+    const void *weight;          /* weight_type [cols]; NULL: ones */
+    void *h, *out;               /* h: type, may be NULL; out: out_type */
+    float *scales;               /* [rows][groups] for an output of 8 bits, else NULL */
+    float *rstd;                 /* [rows] or NULL */
+    int32_t type;                /* DD_F32, DD_BF16 or DD_F16 */
+    int32_t weight_type;         /* DD_F32, or type */
+    int32_t out_type;            /* type, DD_E4M3 or DD_I8 */
+    int32_t group;               /* columns per scale: 0 (a row), 32, 64 or 128 */
+    float eps;
+    int32_t reserved;            /* 0 */
+} dd_rms_norm_args;
+dd_status dd_rms_norm(const dd_rms_norm_args *a, void *stream);
+
+/*
+ * dd_rms_norm_grad -- from the gradient dy of y: with xh = h * rstd,
+ *   dx = (weight dy - xh mean over the row of (weight dy xh)) * rstd + dh
+ *   dw = sum over rows of dy xh, rounded to weight_type
+ * h and rstd as dd_rms_norm gave them (h is x without a residual), dh the
+ * gradient that reaches h on its other ways (NULL: none).  dx is the gradient
+ * of x and of residual alike.  An output of 8 bits counts as y.
+ * dx may be dy, dh or h themselves (the same stride); otherwise outputs must
+ * not overlap inputs.
+ *   work   device memory of dd_rms_norm_grad_work(rows, cols) bytes, aligned to
+ *          16, which the call overwrites (for calls under graph capture, say),
+ *          or NULL: the library takes it from its cache.
+ */
+typedef struct {
+    int64_t rows, cols;
+    int64_t dy_stride, h_stride, dh_stride, dx_stride;
+    const void *dy, *h, *dh;     /* type; dh may be NULL */
+    const void *weight;          /* weight_type [cols]; NULL: ones */
+    const float *rstd;           /* [rows] */
+    void *dx;                    /* type */
+    void *dw;                    /* weight_type [cols], or NULL */
+    void *work;
+    int32_t type, weight_type;   /* as above */
+} dd_rms_norm_grad_args;
+dd_status dd_rms_norm_grad(const dd_rms_norm_grad_args *a, void *stream);
+size_t dd_rms_norm_grad_work(int64_t rows, int64_t cols);
 
 /*
  * dd_release_cache -- wait for all work on the current device, then return

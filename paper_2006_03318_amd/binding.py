@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 from typing import Optional, Tuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -21,6 +22,7 @@ DD_OK, DD_EINVAL, DD_ECYCLE, DD_ECHAIN, DD_ERANGE, DD_ENOMEM, DD_EHIP, DD_EMISMA
 DD_LEVELS, DD_PHASES = 0, 1
 DD_LOAD_SHARED_THREADS = 1
 DD_POLICY_EARLIEST, DD_POLICY_PRIORITY = 0, 1
+DD_F32, DD_BF16, DD_F16, DD_E4M3, DD_I8 = range(5)
 STATUS_NAMES = ["DD_OK", "DD_EINVAL", "DD_ECYCLE", "DD_ECHAIN", "DD_ERANGE", "DD_ENOMEM",
                 "DD_EHIP", "DD_EMISMATCH", "DD_ELIMIT"]
 
@@ -75,6 +77,14 @@ def lib():
         "dd_sched_task_steps": (_i32, [_vp, _vp, _vp]),
         "dd_sched_info": (_i32, [_vp, ctypes.POINTER(_i64), ctypes.POINTER(_i64),
                                  ctypes.POINTER(_i64), ctypes.POINTER(_i64)]),
+        "dd_tensors_load": (_i32, [_i32, _vp, _vp, ctypes.POINTER(_vp)]),
+        "dd_tensors_free": (None, [_vp]),
+        "dd_grad_norm": (_i32, [_vp, ctypes.c_float, _vp, _vp, _vp]),
+        "dd_grad_clip": (_i32, [_vp, _vp, _vp, _vp]),
+        "dd_adam_step": (_i32, [_vp, _vp, _vp] + [ctypes.c_double] * 5 + [_i32, _vp]),
+        "dd_rms_norm": (_i32, [ctypes.c_char_p, _vp]),
+        "dd_rms_norm_grad": (_i32, [ctypes.c_char_p, _vp]),
+        "dd_rms_norm_grad_work": (ctypes.c_size_t, [_i64, _i64]),
         "dd_graph_free": (None, [_vp]),
         "dd_sched_free": (None, [_vp]),
         "dd_variants_free": (None, [_vp]),
@@ -253,3 +263,186 @@ def dd_sched_free(s):
 def dd_variants_free(v):
     if v:
         lib().dd_variants_free(v)
+
+
+# ---------------------------------------------------------------------------
+# The weight update and the root-mean-square norm.  All arguments are torch
+# tensors on the GPU; the checks are kept short, as these calls take a few
+# microseconds themselves.
+_DT = {}
+
+
+def _types():
+    if not _DT:
+        import torch
+        _DT.update({torch.float32: DD_F32, torch.bfloat16: DD_BF16, torch.float16: DD_F16,
+                    torch.float8_e4m3fn: DD_E4M3, torch.int8: DD_I8})
+    return _DT
+
+
+def _gpu(name, t, count, *types):
+    """Address of a contiguous tensor on the GPU (None stays None)."""
+    if t is None:
+        return 0
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    if (_DT or _types()).get(t.dtype, -1) not in types:
+        raise TypeError("%s: unexpected type %s" % (name, t.dtype))
+    if t.numel() != count:
+        raise ValueError("%s: expected %d elements, got %d" % (name, count, t.numel()))
+    return t.data_ptr()
+
+
+def _state(name, t, count, dtype):
+    if not t.is_cuda or str(t.dtype) != dtype or t.numel() < count or not t.is_contiguous():
+        raise ValueError("%s must be %s [%d] on the GPU" % (name, dtype, count))
+    return t.data_ptr()
+
+
+_TENSOR = struct.Struct("@5Pq4i")
+
+
+def dd_tensors_load(tensors, stream=None):
+    """A handle for a list of tensors: each a dict with `grad` and, for
+    dd_adam_step, `param`, `m`, `v`, `master` (16-bit params) and `decay`
+    (default True).  They must live, where they are, as long as the handle."""
+    rows = []
+    for i, t in enumerate(tensors):
+        unknown = set(t) - {"grad", "param", "master", "m", "v", "decay"}
+        if unknown:
+            raise ValueError("tensor %d: unknown %s" % (i, ", ".join(sorted(unknown))))
+        g, p = t["grad"], t.get("param")
+        n = g.numel()
+        a = [_gpu("tensor %d: grad" % i, g, n, DD_F32, DD_BF16, DD_F16),
+             _gpu("tensor %d: param" % i, p, n, DD_F32, DD_BF16, DD_F16)]
+        a += [_gpu("tensor %d: %s" % (i, k), t.get(k), n, DD_F32) for k in ("master", "m", "v")]
+        rows.append(_TENSOR.pack(*a, n, _DT[g.dtype], DD_F32 if p is None else _DT[p.dtype],
+                                 0 if t.get("decay", True) else 1, 0))
+    out = _vp()
+    buf = ctypes.create_string_buffer(b"".join(rows), len(rows) * _TENSOR.size + 1)
+    _check(lib().dd_tensors_load(len(rows), buf, _stream(stream), ctypes.byref(out)))
+    return out
+
+
+def dd_tensors_free(t):
+    if t:
+        lib().dd_tensors_free(t)
+
+
+def dd_grad_norm(t, d_stats, max_norm=0.0, d_inv_scale=None, stream=None):
+    """d_stats (float32 [3] on the GPU) receives the norm of all gradients, the
+    factor that unscales and clips them, and 1 if one is not finite."""
+    u = None if d_inv_scale is None else _state("d_inv_scale", d_inv_scale, 1, "torch.float32")
+    rc = (_lib or lib()).dd_grad_norm(t, max_norm, u, _state("d_stats", d_stats, 3, "torch.float32"),
+                                      None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_grad_clip(src, dst, d_stats, stream=None):
+    rc = (_lib or lib()).dd_grad_clip(src, dst, _state("d_stats", d_stats, 3, "torch.float32"),
+                                      None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_adam_step(t, d_step, d_stats=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
+                 weight_decay=0.0, decoupled=True, stream=None):
+    """One step of Adam; d_step: int64 [1] on the GPU, the steps taken."""
+    st = None if d_stats is None else _state("d_stats", d_stats, 3, "torch.float32")
+    rc = (_lib or lib()).dd_adam_step(t, _state("d_step", d_step, 1, "torch.int64"), st, lr, beta1,
+                                      beta2, eps, weight_decay, 1 if decoupled else 0,
+                                      None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _rows(name, t, shape, dtype):
+    """(address, row stride) of rows: the last dimension is one row."""
+    if t is None:
+        return 0, 0
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.dtype != dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if t.dim() != 2 or (shape[-1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s: elements of a row must be consecutive, and more than two dimensions "
+                         "contiguous" % name)
+    return t.data_ptr(), t.stride(0)
+
+
+_RMS = struct.Struct("@6q7P4if i")
+_RMS_GRAD = struct.Struct("@6q8P2i")
+
+
+def _row_types(x, weight):
+    types = _DT or _types()
+    kind = types.get(x.dtype, -1)
+    if not 0 <= kind <= DD_F16 or x.dim() < 1 or x.shape[-1] < 1:
+        raise TypeError("rows must be float32, bfloat16 or float16 and not empty")
+    if weight is None:
+        return kind, DD_F32
+    wk = types.get(weight.dtype, -1)
+    if wk != DD_F32 and wk != kind:
+        raise TypeError("weight must be float32 or the rows' type")
+    return kind, wk
+
+
+def dd_rms_norm(x, residual, weight, eps, out, h=None, rstd=None, scales=None, group=0, stream=None):
+    """out = (x + residual) normalized over its last dimension, times weight:
+    in x's type, or in 8 bits (out float8_e4m3fn or int8, with scales float32
+    [rows, groups]).  residual, weight, h (receives x + residual) and rstd may
+    be None."""
+    kind, wk = _row_types(x, weight)
+    shape = x.shape
+    cols = shape[-1]
+    n = x.numel()
+    rows = n // cols
+    px, sx = _rows("x", x, shape, x.dtype)
+    pr, sr = _rows("residual", residual, shape, x.dtype)
+    ph, sh = _rows("h", h, shape, x.dtype)
+    ok = _DT.get(out.dtype, -1)
+    po, so = _rows("out", out, shape, out.dtype)
+    if rstd is not None:
+        _gpu("rstd", rstd, rows, DD_F32)
+    if scales is not None:
+        _gpu("scales", scales, rows * (-(-cols // group) if group > 0 else 1), DD_F32)
+    args = _RMS.pack(rows, cols, sx, sr, sh, so, px, pr, _gpu("weight", weight, cols, wk), ph, po,
+                     0 if scales is None else scales.data_ptr(), 0 if rstd is None else rstd.data_ptr(),
+                     kind, wk, ok, group, eps, 0)
+    rc = (_lib or lib()).dd_rms_norm(args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_rms_norm_grad(dy, h, weight, rstd, dx, dw=None, dh=None, work=None, stream=None):
+    """dx and dw from the gradient dy of the norm's output; dh: what reaches h
+    on its other ways.  work: uint8 of dd_rms_norm_grad_work(rows, cols), or
+    None (from the library's cache)."""
+    kind, wk = _row_types(h, weight if weight is not None else dw)
+    shape = h.shape
+    cols = shape[-1]
+    rows = h.numel() // cols
+    pd, sd = _rows("dy", dy, shape, h.dtype)
+    ph, sh = _rows("h", h, shape, h.dtype)
+    pe, se = _rows("dh", dh, shape, h.dtype)
+    px, sx = _rows("dx", dx, shape, h.dtype)
+    if work is not None and (not work.is_cuda or not work.is_contiguous()
+                             or work.numel() * work.element_size() < dd_rms_norm_grad_work(rows, cols)):
+        raise ValueError("work must hold dd_rms_norm_grad_work(rows, cols) bytes on the GPU")
+    args = _RMS_GRAD.pack(rows, cols, sd, sh, se, sx, pd, ph, pe, _gpu("weight", weight, cols, wk),
+                          _gpu("rstd", rstd, rows, DD_F32), px, _gpu("dw", dw, cols, wk),
+                          0 if work is None else work.data_ptr(), kind, wk)
+    rc = (_lib or lib()).dd_rms_norm_grad(args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_rms_norm_grad_work(rows: int, cols: int) -> int:
+    return lib().dd_rms_norm_grad_work(int(rows), int(cols))

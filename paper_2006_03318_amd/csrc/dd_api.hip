@@ -14,9 +14,11 @@
 #include "dd_internal.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
 std::atomic<uint64_t> g_next_id{1};
+}  // namespace
+
+namespace dd {
 
 dd_status fail(dd_status s, const char *fmt, ...) {
     va_list ap;
@@ -30,6 +32,15 @@ dd_status hip_fail(hipError_t e, const char *what) {
     return fail(e == hipErrorOutOfMemory ? DD_ENOMEM : DD_EHIP, "%s: %s", what,
                 hipGetErrorString(e));
 }
+
+void no_error() { g_err[0] = 0; }
+
+}  // namespace dd
+
+namespace {
+
+using dd::fail;
+using dd::hip_fail;
 
 dd_status map_err_bits(uint32_t e) {
     using namespace dd;
