@@ -21,64 +21,86 @@ __device__ __forceinline__ gptr<T> global(T *p) {
     return (gptr<T>)(p);
 }
 
-// N consecutive elements of E as floats.  The address is aligned to E and no
-// more (tensors start anywhere in a buffer, rows have any stride): CDNA4 loads
-// 16 bytes from any address.
+// N consecutive elements of E.  The address is aligned to E and no more
+// (tensors start anywhere in a buffer, rows have any stride): CDNA4 loads 16
+// bytes from any address.  Loading and converting are separate steps, so that
+// a kernel has all its loads under way before it waits for the first.
 template <class E, int N>
 struct Pack {
     typedef E vec __attribute__((ext_vector_type(N)));
     typedef float fvec __attribute__((ext_vector_type(N)));
+    typedef vec __attribute__((aligned(alignof(E)))) any;
+    vec v;
+    __device__ __forceinline__ void load(const E *p) { v = *(gptr<const any>)(p); }
+    __device__ __forceinline__ void store(E *p) const { *(gptr<any>)(p) = v; }
+    // the first `have` of them, any number; the others read as zero, and are not written
+    __device__ __forceinline__ void load(const E *p, int have) {
+        if (have >= N) {
+            load(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++) v[i] = i < have ? global(p)[i] : (E)0.0f;
+        }
+    }
+    __device__ __forceinline__ void store(E *p, int have) const {
+        if (have >= N) {
+            store(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                if (i < have) global(p)[i] = v[i];
+        }
+    }
+    __device__ __forceinline__ void to(float (&x)[N]) const {
+#pragma unroll
+        for (int i = 0; i < N; i++) x[i] = (float)v[i];
+    }
+    // (rounds to nearest even)
+    __device__ __forceinline__ void from(const float (&x)[N]) {
+        fvec f;
+#pragma unroll
+        for (int i = 0; i < N; i++) f[i] = x[i];
+        v = __builtin_convertvector(f, vec);
+    }
 };
-template <class E, int N>
-__device__ __forceinline__ void load_n(const E *p, float (&x)[N]) {
-    typedef typename Pack<E, N>::vec V;
-    typedef V __attribute__((aligned(alignof(E)))) U;
-    const V v = *(gptr<const U>)(p);
-#pragma unroll
-    for (int i = 0; i < N; i++) x[i] = (float)v[i];
-}
-// (round to nearest even)
-template <class E, int N>
-__device__ __forceinline__ void store_n(E *p, const float (&x)[N]) {
-    typedef typename Pack<E, N>::vec V;
-    typedef V __attribute__((aligned(alignof(E)))) U;
-    typename Pack<E, N>::fvec f;
-#pragma unroll
-    for (int i = 0; i < N; i++) f[i] = x[i];
-    *(gptr<U>)(p) = __builtin_convertvector(f, V);
-}
-// the first `have` (0 to N) of them; the rest reads as zero and is not written
-template <class E, int N>
-__device__ __forceinline__ void load_some(const E *p, float (&x)[N], int have) {
-#pragma unroll
-    for (int i = 0; i < N; i++) x[i] = i < have ? (float)global(p)[i] : 0.0f;
-}
-template <class E, int N>
-__device__ __forceinline__ void store_some(E *p, const float (&x)[N], int have) {
-#pragma unroll
-    for (int i = 0; i < N; i++)
-        if (i < have) global(p)[i] = (E)x[i];
-}
 
-template <class T>
-__device__ __forceinline__ T lane_xor(T x, int d) {
-    return __shfl_xor(x, d, 64);
+// Sums and maxima over aligned groups of W lanes (4, 8, 16 or 64); every lane
+// has the result, the same bits in each.  Steps inside 16 lanes are DPP moves
+// (once the four lanes of a quad agree, mirroring eight lanes pairs the quads;
+// so on for sixteen), the four sixteens are read as scalars: no trips to LDS.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true);
 }
-// over aligned groups of W lanes (a power of two); every lane has the result,
-// the same bits in each (the order of the sums does not depend on the lane)
-template <int W, class T>
-__device__ __forceinline__ T lanes_sum(T x) {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) x += lane_xor(x, o);
+constexpr int kDppXor1 = 0xb1, kDppXor2 = 0x4e, kDppHalfMirror = 0x141, kDppMirror = 0x140;
+
+template <int W, class T, class F>
+__device__ __forceinline__ T lanes_fold(T x, const F &f) {
+    static_assert(sizeof(T) == 4 && (W == 4 || W == 8 || W == 16 || W == 64), "lanes");
+    auto from = [](uint32_t b) { T y; __builtin_memcpy(&y, &b, 4); return y; };
+    auto bits = [](T y) { uint32_t b; __builtin_memcpy(&b, &y, 4); return b; };
+    x = f(x, from(dpp<kDppXor1>(bits(x))));
+    x = f(x, from(dpp<kDppXor2>(bits(x))));
+    if (W >= 8) x = f(x, from(dpp<kDppHalfMirror>(bits(x))));
+    if (W >= 16) x = f(x, from(dpp<kDppMirror>(bits(x))));
+    if (W == 64) {
+        const T a = from(__builtin_amdgcn_readlane((int)bits(x), 0)), b = from(__builtin_amdgcn_readlane((int)bits(x), 16));
+        const T c = from(__builtin_amdgcn_readlane((int)bits(x), 32)), d = from(__builtin_amdgcn_readlane((int)bits(x), 48));
+        x = f(f(a, b), f(c, d));
+    }
     return x;
 }
 template <int W>
+__device__ __forceinline__ float lanes_sum(float x) {
+    return lanes_fold<W>(x, [](float a, float b) { return a + b; });
+}
+template <int W>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t x) {
+    return lanes_fold<W>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ double wave_sum(double x) {
 #pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) {
-        const uint32_t y = lane_xor(x, o);
-        x = y > x ? y : x;
-    }
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
     return x;
 }
 

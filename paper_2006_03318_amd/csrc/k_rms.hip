@@ -62,6 +62,194 @@ __device__ __forceinline__ uint8_t to_8_bits(float x, int32_t out_type) {
     return (uint8_t)(int8_t)(r < -127.0f ? -127 : r > 127.0f ? 127 : r != r ? 0 : (int)r);
 }
 
+// --- rows held in registers -------------------------------------------------
+// A row is taken by LANES lanes, each with NV packs of 8 consecutive columns
+// (lane l has packs l, l + LANES, ...), so x and residual are read once and
+// a group of 32, 64 or 128 columns is 4, 8 or 16 neighbouring lanes.  Up to 64
+// lanes need no barrier; several waves exchange one number through LDS.
+template <int LANES>
+struct RowSum {
+    static constexpr int kWaves = LANES / 64 > 1 ? LANES / 64 : 1;
+    // slot: another one for each exchange of a row, by turns between rows
+    static __device__ __forceinline__ float sum(float x, float *slot) {
+        x = lanes_sum<(LANES < 64 ? LANES : 64)>(x);
+        if (LANES <= 64) return x;
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
+        __syncthreads();
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) t += slot[w];
+        return t;
+    }
+    static __device__ __forceinline__ uint32_t max(uint32_t x, float *slot) {
+        x = lanes_max<(LANES < 64 ? LANES : 64)>(x);
+        if (LANES <= 64) return x;
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = __uint_as_float(x);
+        __syncthreads();
+        uint32_t t = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) {
+            const uint32_t y = __float_as_uint(slot[w]);
+            t = y > t ? y : t;
+        }
+        return t;
+    }
+};
+
+__device__ __forceinline__ void store_pack_8(uint8_t *p, const float (&x)[8], int have, int32_t out_type) {
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    typedef u2 __attribute__((aligned(1))) U;
+    u2 b;
+    if (out_type == DD_E4M3) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i], x[4 * i + 1], 0, false);
+            b[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2], x[4 * i + 3], w, true);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; i++)
+            b[i] = (uint32_t)to_8_bits(x[4 * i], DD_I8) | (uint32_t)to_8_bits(x[4 * i + 1], DD_I8) << 8 |
+                   (uint32_t)to_8_bits(x[4 * i + 2], DD_I8) << 16 | (uint32_t)to_8_bits(x[4 * i + 3], DD_I8) << 24;
+    }
+    if (have >= 8) {
+        *(gptr<U>)(p) = b;
+    } else {
+        for (int i = 0; i < have; i++) global(p)[i] = (uint8_t)(b[i >> 2] >> (8 * (i & 3)));
+    }
+}
+// eight weights, held as they were loaded
+template <class T>
+struct Weights {
+    Pack<float, 8> f;
+    Pack<T, 8> t;
+    __device__ __forceinline__ void load(const void *w, int32_t type, int64_t c, int have) {
+        if (!w) return;
+        if (type == DD_F32) f.load(static_cast<const float *>(w) + c, have);
+        else t.load(static_cast<const T *>(w) + c, have);
+    }
+    __device__ __forceinline__ void to(const void *w, int32_t type, float (&x)[8]) const {
+        if (!w) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = 1.0f;
+        } else if (type == DD_F32) {
+            f.to(x);
+        } else {
+            t.to(x);
+        }
+    }
+};
+
+// (rows that share a workgroup do not share a wave, and need no barrier)
+constexpr int row_threads(int lanes) { return lanes <= 64 ? 256 : lanes; }
+
+template <class T, int LANES, int NV>
+__global__ void __launch_bounds__(row_threads(LANES)) k_rms_row(RmsArgs a) {
+    constexpr int kThreads = row_threads(LANES), kRows = kThreads / LANES;
+    __shared__ float slots[4][16];
+    const int lane = threadIdx.x % LANES;
+    const int cols = (int)a.cols;
+    const bool narrow = a.out_type == DD_E4M3 || a.out_type == DD_I8;
+    const float most = most_of(a.out_type);
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.rows;
+         row += (int64_t)gridDim.x * kRows, turn ^= 1) {
+        const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+        const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
+        float v[NV][8];
+        {
+            Pack<T, 8> px[NV], pr[NV];
+#pragma unroll
+            for (int k = 0; k < NV; k++) px[k].load(x + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+            if (a.residual) {
+#pragma unroll
+                for (int k = 0; k < NV; k++) pr[k].load(r + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+            }
+#pragma unroll
+            for (int k = 0; k < NV; k++) px[k].to(v[k]);
+            if (a.residual) {
+#pragma unroll
+                for (int k = 0; k < NV; k++) {
+                    float y[8];
+                    pr[k].to(y);
+#pragma unroll
+                    for (int i = 0; i < 8; i++) v[k][i] += y[i];
+                }
+            }
+        }
+        float q = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; k++)
+#pragma unroll
+            for (int i = 0; i < 8; i++) q = fmaf(v[k][i], v[k][i], q);
+        const float rstd = 1.0f / sqrtf(RowSum<LANES>::sum(q, slots[turn]) / (float)cols + a.eps);
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        if (a.h) {
+            T *h = static_cast<T *>(a.h) + row * a.h_stride;
+#pragma unroll
+            for (int k = 0; k < NV; k++) {
+                Pack<T, 8> p;
+                p.from(v[k]);
+                p.store(h + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const int c = 8 * (lane + k * LANES);
+            Weights<T> p;
+            float w[8];
+            p.load(a.weight, a.weight_type, c, cols - c);
+            p.to(a.weight, a.weight_type, w);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[k][i] = v[k][i] * rstd * w[i];
+        }
+        if (!narrow) {
+            T *out = static_cast<T *>(a.out) + row * a.out_stride;
+#pragma unroll
+            for (int k = 0; k < NV; k++) {
+                Pack<T, 8> p;
+                p.from(v[k]);
+                p.store(out + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+            }
+            continue;
+        }
+        uint32_t m[NV];
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            m[k] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t b = __float_as_uint(v[k][i]) & 0x7fffffffu;
+                m[k] = b > m[k] ? b : m[k];
+            }
+        }
+        if (a.group == 0) {
+#pragma unroll
+            for (int k = 1; k < NV; k++) m[0] = m[k] > m[0] ? m[k] : m[0];
+            const uint32_t t = RowSum<LANES>::max(m[0], slots[2 + turn]);
+#pragma unroll
+            for (int k = 0; k < NV; k++) m[k] = t;
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; k++)
+                m[k] = a.group == 128 ? lanes_max<16>(m[k]) : a.group == 64 ? lanes_max<8>(m[k]) : lanes_max<4>(m[k]);
+        }
+        const int group = a.group ? a.group : cols, groups = (cols + group - 1) / group;
+        uint8_t *out = static_cast<uint8_t *>(a.out) + row * a.out_stride;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            const int c = 8 * (lane + k * LANES);
+            const float scale = scale_of(m[k], most);
+            const float inv = 1.0f / scale;
+            if (a.group ? c < cols && c % group == 0 : c == 0) a.scales[row * groups + c / group] = scale;
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = v[k][i] * inv;
+            store_pack_8(out + c, y, cols - c, a.out_type);
+        }
+    }
+}
+
 // One workgroup per row, any width: the row is read once for each of its sums.
 template <class T>
 __global__ void __launch_bounds__(kBlock) k_rms_loop(RmsArgs a) {
@@ -175,15 +363,59 @@ int dw_runs(int64_t rows) {
     return r < 1 ? 1 : r > kRmsParts ? kRmsParts : (int)r;
 }
 
+// Lanes per row and packs per lane.  Two packs of each input are enough loads
+// under way, and more cost registers, so the fewest lanes that hold the row
+// with two packs (four at the widest), a whole wave or more past 256 columns
+// so that no lanes idle.  Measured on bf16 with a residual, TB/s: 8,192 x
+// 4,096 to 8 bits 4.8 with 256 lanes x 2 (128 x 4: 4.2, 64 x 8: 3.6, 1,024 x
+// 1: 2.7); 16,384 x 1,024 5.0 with 64 x 2 (256 x 1: 4.3); 65,536 x 2,048
+// 5.8 with 256 x 1 (64 x 4: 5.7); 65,536 x 128 to 8 bits 3.6 with 16 x 1
+// (64 x 1: 1.5).  Few rows take the same: 4 to 512 rows of 4,096 are as fast
+// with any of these shapes, the launch bounds them.
+struct Shape {
+    int lanes, packs;      // 0: k_rms_loop
+};
+Shape row_shape(int64_t cols) {
+    const int64_t n = (cols + 7) / 8;
+    if (n <= 32) return {16, n <= 16 ? 1 : 2};
+    if (n <= 128) return {64, n <= 64 ? 1 : 2};
+    if (n <= 512) return {256, n <= 256 ? 1 : 2};
+    if (n <= 1024) return {512, 2};
+    if (n <= 4096) return {1024, n <= 2048 ? 2 : 4};
+    return {0, 0};
+}
+
+constexpr int kRowBlocks = 1 << 20;    // workgroups of a launch at most; rows beyond go round
+
+template <class T, int LANES, int NV>
+void run_rows(const RmsArgs &a, hipStream_t s) {
+    constexpr int kThreads = row_threads(LANES), kRows = kThreads / LANES;
+    const int64_t need = (a.rows + kRows - 1) / kRows;
+    k_rms_row<T, LANES, NV><<<(unsigned)(need < kRowBlocks ? need : kRowBlocks), kThreads, 0, s>>>(a);
+}
+template <class T>
+void rms_norm(const RmsArgs &a, hipStream_t s) {
+    const Shape p = row_shape(a.cols);
+    if (p.lanes == 16 && p.packs == 1) return run_rows<T, 16, 1>(a, s);
+    if (p.lanes == 16 && p.packs == 2) return run_rows<T, 16, 2>(a, s);
+    if (p.lanes == 64 && p.packs == 1) return run_rows<T, 64, 1>(a, s);
+    if (p.lanes == 64 && p.packs == 2) return run_rows<T, 64, 2>(a, s);
+    if (p.lanes == 256 && p.packs == 1) return run_rows<T, 256, 1>(a, s);
+    if (p.lanes == 256 && p.packs == 2) return run_rows<T, 256, 2>(a, s);
+    if (p.lanes == 512 && p.packs == 2) return run_rows<T, 512, 2>(a, s);
+    if (p.lanes == 1024 && p.packs == 2) return run_rows<T, 1024, 2>(a, s);
+    if (p.lanes == 1024 && p.packs == 4) return run_rows<T, 1024, 4>(a, s);
+    k_rms_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
+}
+
 }  // namespace
 
 size_t rms_grad_work(int64_t rows, int64_t cols) { return (size_t)dw_runs(rows) * (size_t)cols * sizeof(float); }
 
 hipError_t launch_rms_norm(const RmsArgs &a, hipStream_t s) {
-    const dim3 g = grid_of_rows(a.rows);
-    if (a.type == DD_F32) k_rms_loop<float><<<g, kBlock, 0, s>>>(a);
-    else if (a.type == DD_BF16) k_rms_loop<bf16_t><<<g, kBlock, 0, s>>>(a);
-    else k_rms_loop<f16_t><<<g, kBlock, 0, s>>>(a);
+    if (a.type == DD_F32) rms_norm<float>(a, s);
+    else if (a.type == DD_BF16) rms_norm<bf16_t>(a, s);
+    else rms_norm<f16_t>(a, s);
     return hipGetLastError();
 }
 

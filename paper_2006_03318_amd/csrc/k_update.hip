@@ -29,7 +29,7 @@ __device__ double chunk_squares(const G *g, int n) {
 
 __device__ double block_sum(double x) {
     __shared__ double part[kBlock / 64];
-    x = lanes_sum<64>(x);
+    x = wave_sum(x);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     double t = 0.0;
