@@ -143,6 +143,13 @@ struct Weights {
 // (rows that share a workgroup do not share a wave, and need no barrier)
 constexpr int row_threads(int lanes) { return lanes <= 64 ? 256 : lanes; }
 
+// (the same for a whole wave, and said so, where a row has one)
+template <int LANES>
+__device__ __forceinline__ int row_of_thread() {
+    const int r = threadIdx.x / LANES;
+    return LANES >= 64 ? __builtin_amdgcn_readfirstlane(r) : r;
+}
+
 template <class T, int LANES, int NV>
 __global__ void __launch_bounds__(row_threads(LANES)) k_rms_row(RmsArgs a) {
     constexpr int kThreads = row_threads(LANES), kRows = kThreads / LANES;
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(row_threads(LANES)) k_rms_row(RmsArgs a) {
     const bool narrow = a.out_type == DD_E4M3 || a.out_type == DD_I8;
     const float most = most_of(a.out_type);
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.rows;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + row_of_thread<LANES>(); row < a.rows;
          row += (int64_t)gridDim.x * kRows, turn ^= 1) {
         const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
         const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
@@ -296,6 +303,95 @@ __global__ void __launch_bounds__(kBlock) k_rms_loop(RmsArgs a) {
     }
 }
 
+// The gradient of rows held in registers, as k_rms_row holds them.  A workgroup
+// goes over rows (b, b + grid, ...) and keeps its sums of dy * xh per column in
+// registers; at the end rows of one workgroup are joined through LDS, and the
+// workgroup writes one partial sum per column, which k_rms_dw_join adds up in
+// order.
+constexpr int grad_threads(int lanes) { return lanes <= 64 ? 1024 : lanes; }
+
+template <class T, int LANES, int NV>
+__global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArgs a, float *part) {
+    constexpr int kThreads = grad_threads(LANES), kRows = kThreads / LANES;
+    __shared__ float slots[2][16];
+    const int lane = threadIdx.x % LANES;
+    const int cols = (int)a.cols;
+    float sum[NV][8] = {};
+    Weights<T> w[NV];
+#pragma unroll
+    for (int k = 0; k < NV; k++) w[k].load(a.weight, a.weight_type, 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+    int turn = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + row_of_thread<LANES>(); row < a.rows;
+         row += (int64_t)gridDim.x * kRows, turn ^= 1) {
+        const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
+        const T *h = static_cast<const T *>(a.h) + row * a.h_stride;
+        const T *dh = static_cast<const T *>(a.dh) + row * a.dh_stride;
+        T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
+        Pack<T, 8> pd[NV], ph[NV], pe[NV];
+#pragma unroll
+        for (int k = 0; k < NV; k++) pd[k].load(dy + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+#pragma unroll
+        for (int k = 0; k < NV; k++) ph[k].load(h + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+        if (a.dh) {
+#pragma unroll
+            for (int k = 0; k < NV; k++) pe[k].load(dh + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+        }
+        const float rstd = a.rstd[row];
+        float g[NV][8], xh[NV][8], q = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            float y[8];
+            pd[k].to(g[k]);
+            ph[k].to(xh[k]);
+            w[k].to(a.weight, a.weight_type, y);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                xh[k][i] *= rstd;
+                sum[k][i] = fmaf(g[k][i], xh[k][i], sum[k][i]);
+                g[k][i] *= y[i];
+                q = fmaf(g[k][i], xh[k][i], q);
+            }
+        }
+        const float c = RowSum<LANES>::sum(q, slots[turn]) / (float)cols;
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = 0.0f;
+            if (a.dh) pe[k].to(y);
+            Pack<T, 8> p;
+#pragma unroll
+            for (int i = 0; i < 8; i++) y[i] = fmaf(g[k][i] - xh[k][i] * c, rstd, y[i]);
+            p.from(y);
+            p.store(dx + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+        }
+    }
+    if (!a.dw) return;
+    part += (int64_t)blockIdx.x * cols;
+    if (kRows == 1) {
+#pragma unroll
+        for (int k = 0; k < NV; k++) {
+            Pack<float, 8> p;
+            p.from(sum[k]);
+            p.store(part + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+        }
+        return;
+    }
+    __shared__ float all[kRows * LANES * 8];
+#pragma unroll
+    for (int k = 0; k < NV; k++) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; i++) all[threadIdx.x * 8 + i] = sum[k][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < LANES * 8 && k * LANES * 8 + c < cols; c += kThreads) {
+            float t = 0.0f;
+            for (int r = 0; r < kRows; r++) t += all[r * LANES * 8 + c];
+            part[k * LANES * 8 + c] = t;
+        }
+    }
+}
+
 __device__ __forceinline__ float weight_at(const RmsGradArgs &a, int64_t c) {
     if (!a.weight) return 1.0f;
     if (a.weight_type == DD_F32) return global(static_cast<const float *>(a.weight))[c];
@@ -343,11 +439,20 @@ __global__ void __launch_bounds__(kBlock) k_rms_dw_loop(RmsGradArgs a, float *pa
     }
 }
 
-__global__ void __launch_bounds__(kBlock) k_rms_dw_join(RmsGradArgs a, const float *part, int n) {
-    const int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (c >= a.cols) return;
+// A workgroup has 32 columns; 32 threads share a column.
+__global__ void __launch_bounds__(1024) k_rms_dw_join(RmsGradArgs a, const float *part, int n) {
+    __shared__ float lds[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * 32 + x;
     float s = 0.0f;
-    for (int i = 0; i < n; i++) s += part[i * a.cols + c];
+    if (c < a.cols)
+        for (int i = y; i < n; i += 32) s += part[i * a.cols + c];
+    lds[y][x] = s;
+    __syncthreads();
+    if (y || c >= a.cols) return;
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; i++) s += lds[i][x];
     if (a.weight_type == DD_F32) static_cast<float *>(a.dw)[c] = s;
     else if (a.weight_type == DD_BF16) static_cast<bf16_t *>(a.dw)[c] = (bf16_t)s;
     else static_cast<f16_t *>(a.dw)[c] = (f16_t)s;
@@ -408,25 +513,53 @@ void rms_norm(const RmsArgs &a, hipStream_t s) {
     k_rms_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
 }
 
+// Workgroups of the gradient: as many as run at once, each with rows to go over.
+int grad_parts(int64_t rows, int64_t cols) {
+    const Shape p = row_shape(cols);
+    if (!p.lanes) return dw_runs(rows);
+    const int per = grad_threads(p.lanes) / p.lanes;
+    const int64_t need = (rows + per - 1) / per, most = p.lanes <= 64 || p.lanes == 1024 ? 256 : 512;
+    return (int)(need < 1 ? 1 : need < most ? need : most);
+}
+
+template <class T, int LANES, int NV>
+void run_grad(const RmsGradArgs &a, float *work, int parts, hipStream_t s) {
+    k_rms_grad_row<T, LANES, NV><<<parts, grad_threads(LANES), 0, s>>>(a, work);
+}
+template <class T>
+void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
+    const Shape p = row_shape(a.cols);
+    const int n = grad_parts(a.rows, a.cols);
+    auto join = [&] { k_rms_dw_join<<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a, work, n); };
+    if (!p.lanes) {
+        if (a.dw) {       // first: dx may overwrite what it reads
+            k_rms_dw_loop<T><<<dim3((unsigned)((a.cols + 63) / 64), n), kBlock, 0, s>>>(a, work);
+            join();
+        }
+        if (a.rows > 0) k_rms_dx_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
+        return;
+    }
+    if (p.lanes == 16 && p.packs == 1) run_grad<T, 16, 1>(a, work, n, s);
+    else if (p.lanes == 16) run_grad<T, 16, 2>(a, work, n, s);
+    else if (p.lanes == 64 && p.packs == 1) run_grad<T, 64, 1>(a, work, n, s);
+    else if (p.lanes == 64) run_grad<T, 64, 2>(a, work, n, s);
+    else if (p.lanes == 256 && p.packs == 1) run_grad<T, 256, 1>(a, work, n, s);
+    else if (p.lanes == 256) run_grad<T, 256, 2>(a, work, n, s);
+    else if (p.lanes == 512) run_grad<T, 512, 2>(a, work, n, s);
+    else if (p.packs == 2) run_grad<T, 1024, 2>(a, work, n, s);
+    else run_grad<T, 1024, 4>(a, work, n, s);
+    if (a.dw) join();
+}
+
 }  // namespace
 
-size_t rms_grad_work(int64_t rows, int64_t cols) { return (size_t)dw_runs(rows) * (size_t)cols * sizeof(float); }
+size_t rms_grad_work(int64_t rows, int64_t cols) { return (size_t)grad_parts(rows, cols) * (size_t)cols * sizeof(float); }
 
 hipError_t launch_rms_norm(const RmsArgs &a, hipStream_t s) {
     if (a.type == DD_F32) rms_norm<float>(a, s);
     else if (a.type == DD_BF16) rms_norm<bf16_t>(a, s);
     else rms_norm<f16_t>(a, s);
     return hipGetLastError();
-}
-
-template <class T>
-static void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
-    if (a.dw) {       // first: dx may overwrite what it reads
-        const int n = dw_runs(a.rows);
-        k_rms_dw_loop<T><<<dim3((unsigned)((a.cols + 63) / 64), n), kBlock, 0, s>>>(a, work);
-        k_rms_dw_join<<<(unsigned)((a.cols + kBlock - 1) / kBlock), kBlock, 0, s>>>(a, work, n);
-    }
-    if (a.rows > 0) k_rms_dx_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
 }
 
 hipError_t launch_rms_norm_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
