@@ -367,9 +367,9 @@ typedef struct {
  * dd_tensors_load -- a list of tensors that is worked on in one launch.
  *   t   host array of `count` tensors (copied).
  * The tensors stay where they are for the life of the handle.  The handle
- * keeps 64 bytes of device memory per chunk (2,048 to 32,768 elements of a
- * tensor), and the partial sums of dd_grad_norm: calls that use one handle on
- * several streams are put in order by the library.  Waits for `stream`.
+ * keeps 64 bytes of device memory for every 8,192 elements of a tensor (or
+ * fewer), and working memory of 8 KiB for dd_grad_norm and dd_adam_step: their
+ * calls on several streams are put in order by the library.  Waits for `stream`.
  */
 dd_status dd_tensors_load(int32_t count, const dd_tensor *t, void *stream, dd_tensors **out);
 void dd_tensors_free(dd_tensors *t);

@@ -270,11 +270,13 @@ def dd_variants_free(v):
 # tensors on the GPU; the checks are kept short, as these calls take a few
 # microseconds themselves.
 _DT = {}
+_NAMED = {}
 
 
 def _types():
     if not _DT:
         import torch
+        _NAMED.update(float32=torch.float32, int64=torch.int64)
         _DT.update({torch.float32: DD_F32, torch.bfloat16: DD_BF16, torch.float16: DD_F16,
                     torch.float8_e4m3fn: DD_E4M3, torch.int8: DD_I8})
     return _DT
@@ -295,8 +297,10 @@ def _gpu(name, t, count, *types):
     return t.data_ptr()
 
 
-def _state(name, t, count, dtype):
-    if not t.is_cuda or str(t.dtype) != dtype or t.numel() < count or not t.is_contiguous():
+def _small(name, t, count, dtype):
+    """Address of a few numbers of one type on the GPU."""
+    if (not t.is_cuda or t.dtype is not (_NAMED or _types() and _NAMED)[dtype]
+            or t.numel() < count or not t.is_contiguous()):
         raise ValueError("%s must be %s [%d] on the GPU" % (name, dtype, count))
     return t.data_ptr()
 
@@ -334,15 +338,15 @@ def dd_tensors_free(t):
 def dd_grad_norm(t, d_stats, max_norm=0.0, d_inv_scale=None, stream=None):
     """d_stats (float32 [3] on the GPU) receives the norm of all gradients, the
     factor that unscales and clips them, and 1 if one is not finite."""
-    u = None if d_inv_scale is None else _state("d_inv_scale", d_inv_scale, 1, "torch.float32")
-    rc = (_lib or lib()).dd_grad_norm(t, max_norm, u, _state("d_stats", d_stats, 3, "torch.float32"),
+    u = None if d_inv_scale is None else _small("d_inv_scale", d_inv_scale, 1, "float32")
+    rc = (_lib or lib()).dd_grad_norm(t, max_norm, u, _small("d_stats", d_stats, 3, "float32"),
                                       None if stream is None else _stream(stream))
     if rc:
         _check(rc)
 
 
 def dd_grad_clip(src, dst, d_stats, stream=None):
-    rc = (_lib or lib()).dd_grad_clip(src, dst, _state("d_stats", d_stats, 3, "torch.float32"),
+    rc = (_lib or lib()).dd_grad_clip(src, dst, _small("d_stats", d_stats, 3, "float32"),
                                       None if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -351,8 +355,8 @@ def dd_grad_clip(src, dst, d_stats, stream=None):
 def dd_adam_step(t, d_step, d_stats=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
                  weight_decay=0.0, decoupled=True, stream=None):
     """One step of Adam; d_step: int64 [1] on the GPU, the steps taken."""
-    st = None if d_stats is None else _state("d_stats", d_stats, 3, "torch.float32")
-    rc = (_lib or lib()).dd_adam_step(t, _state("d_step", d_step, 1, "torch.int64"), st, lr, beta1,
+    st = None if d_stats is None else _small("d_stats", d_stats, 3, "float32")
+    rc = (_lib or lib()).dd_adam_step(t, _small("d_step", d_step, 1, "int64"), st, lr, beta1,
                                       beta2, eps, weight_decay, 1 if decoupled else 0,
                                       None if stream is None else _stream(stream))
     if rc:

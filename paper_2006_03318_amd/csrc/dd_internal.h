@@ -206,7 +206,22 @@ struct alignas(64) TensorChunk {
     uint64_t pad2[2];
 };
 static_assert(sizeof(TensorChunk) == 64, "record size");
-constexpr int kNormParts = 2048;  // partial sums of the norm, and workgroups of a pass, at most
+constexpr int64_t kChunkLen = 8192;
+constexpr int kNormParts = 1024;  // workgroups of the norm, at most
+struct AdamFactors {
+    float f;                      // factor of the gradients
+    float b1, c1, b2, c2;         // beta1, 1 - beta1, beta2, 1 - beta2
+    float l2, keep;               // weight decay: added weight * l2, kept share of the weight
+    float lr, rv, eps;            // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    int32_t skip;                 // nothing is applied
+};
+// Working memory of a list, zero when no call is under way but for what a
+// call writes before it reads it.
+struct TensorWork {
+    uint32_t ticket;              // workgroups that are done
+    AdamFactors factors;
+    alignas(64) double part[kNormParts];
+};
 }  // namespace dd
 
 struct dd_tensors {
@@ -216,10 +231,9 @@ struct dd_tensors {
     int device = 0;
     hipStream_t stream = nullptr;
     std::vector<int64_t> sizes;
-    void *mem = nullptr;          // one block: the partial sums, then the chunks
-    double *part = nullptr;       // [kNormParts]
+    dd::TensorWork *work = nullptr;   // one block of memory, the chunks behind it
     dd::TensorChunk *chunks = nullptr;
-    mutable std::mutex mu;        // held while a call that uses part is queued
+    mutable std::mutex mu;        // held while a call that uses work is queued
     mutable dd::ForeignUses uses;
 };
 
@@ -448,12 +462,6 @@ struct AdamParams {
     double lr, beta1, beta2, eps, weight_decay;
     int32_t decoupled;
 };
-// elements per chunk: about kNormParts chunks in all, so that each workgroup
-// has one, but whole turns of a workgroup (2,048 elements) and at most 32,768
-inline int64_t tensor_chunk_len(int64_t total) {
-    const int64_t l = ((total + kNormParts - 1) / kNormParts + 2047) / 2048 * 2048;
-    return l < 2048 ? 2048 : l > 32768 ? 32768 : l;
-}
 hipError_t launch_grad_norm(const dd_tensors *t, double max_norm, const float *inv_scale, float *stats, hipStream_t s);
 hipError_t launch_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float *stats, hipStream_t s);
 hipError_t launch_adam(const dd_tensors *t, int64_t *step, const float *stats, const AdamParams &p, hipStream_t s);

@@ -68,7 +68,7 @@ dd_status check_tensor(int32_t i, const dd_tensor &t) {
 
 void free_tensors(dd_tensors *x) {
     dd::join_uses(x->uses, x->stream);
-    dd::dfree(x->mem, x->stream);
+    dd::dfree(x->work, x->stream);
     delete x;
 }
 
@@ -85,13 +85,12 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
         x->sizes.push_back(t[i].n);
     }
     if (with && without) return fail(DD_EINVAL, "some tensors have params and some have none");
-    const int64_t len = dd::tensor_chunk_len(total);
+    const int64_t len = dd::kChunkLen;
     for (int32_t i = 0; i < count; i++) chunks += (t[i].n + len - 1) / len;
-    if (chunks >= (int64_t(1) << 31) - dd::kNormParts) return fail(DD_EINVAL, "too many elements for one list");
+    if (chunks >= (int64_t(1) << 31)) return fail(DD_EINVAL, "too many elements for one list");
     x->count = count;
     x->n_chunks = (int32_t)chunks;
     x->params = without == 0;
-    const size_t part_bytes = sizeof(double) * dd::kNormParts;
     std::vector<dd::TensorChunk> h;
     h.reserve((size_t)chunks);
     for (int32_t i = 0; i < count; i++) {
@@ -114,11 +113,14 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
         }
     }
     hipError_t e = hipGetDevice(&x->device);
-    if (e == hipSuccess) e = dd::dalloc(&x->mem, part_bytes + sizeof(dd::TensorChunk) * h.size(), s);
+    void *mem = nullptr;
+    if (e == hipSuccess) e = dd::dalloc(&mem, sizeof(dd::TensorWork) + sizeof(dd::TensorChunk) * h.size(), s);
     if (e != hipSuccess) return hip_fail(e, "alloc tensor list");
-    x->part = static_cast<double *>(x->mem);
-    x->chunks = reinterpret_cast<dd::TensorChunk *>(static_cast<char *>(x->mem) + part_bytes);
-    if (!h.empty())
+    x->work = static_cast<dd::TensorWork *>(mem);
+    x->chunks = reinterpret_cast<dd::TensorChunk *>(x->work + 1);
+    const uint32_t none = 0;
+    e = hipMemcpyAsync(&x->work->ticket, &none, sizeof(none), hipMemcpyHostToDevice, s);
+    if (e == hipSuccess && !h.empty())
         e = hipMemcpyAsync(x->chunks, h.data(), sizeof(dd::TensorChunk) * h.size(), hipMemcpyHostToDevice, s);
     if (e == hipSuccess) e = hipStreamSynchronize(s);
     return e == hipSuccess ? DD_OK : hip_fail(e, "copy tensor list");

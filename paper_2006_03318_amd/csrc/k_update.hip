@@ -1,10 +1,19 @@
 // The weight update over many tensors: global gradient norm, clipping, Adam.
 //
-// A handle cuts its tensors into chunks of one length (the last of a tensor
-// shorter) and holds one record per chunk with the chunk's own addresses, so
-// one launch takes any number of tensors and a workgroup finds its work with
-// one read.  All three passes move each element once and compute little:
-// they are bound by memory, small lists by the launch.
+// A handle cuts its tensors into chunks of kChunkLen elements (the last of a
+// tensor shorter) and holds one record per chunk with the chunk's own
+// addresses, so one launch takes any number of tensors and a workgroup finds
+// its work with one read.  All three passes move each element once and compute
+// little: they are bound by memory, small lists by the launch.
+//
+// The norm only reads: 1,024 workgroups go over all chunks, four loads of 16
+// bytes or more under way in every lane (302 M bf16 gradients 5.7 TB/s; a
+// workgroup per chunk 4.2).  Clipping and Adam write as much as they read, and
+// go fastest with a workgroup for each kPartLen elements that does nothing else
+// (Adam on the same list 5.3 TB/s, 5.1 with 8,192 elements to a workgroup, 5.0
+// with 2,048 workgroups that go round).
+#include <type_traits>
+
 #include "dd_elem.h"
 #include "dd_internal.h"
 
@@ -15,16 +24,42 @@ namespace {
 constexpr int kBlock = 256;
 
 
+// Elements per thread and load.
+constexpr int kWide = 8, kTurn = kBlock * kWide, kAhead = kChunkLen / kTurn;
+static_assert(kChunkLen == kAhead * kTurn, "a chunk is whole turns of a workgroup");
+constexpr int kPartLen = 2048, kPartsOf = kChunkLen / kPartLen;
+static_assert(kPartLen == kTurn, "clipping: a pack for each thread");
+
 // Squares in 64 bits: one of an f32 (or bf16) gradient leaves the 32-bit range
 // above 1.8e19 and below 1e-19, and a sum over 10^9 elements keeps its digits.
-template <class G>
-__device__ double chunk_squares(const G *g, int n) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kBlock) {
-        const double x = (double)(float)global(g)[i];
-        s = fma(x, x, s);
-    }
+__device__ __forceinline__ double squares(const float (&x)[kWide], double s) {
+#pragma unroll
+    for (int i = 0; i < kWide; i++) s = fma((double)x[i], (double)x[i], s);
     return s;
+}
+template <class G>
+__device__ __forceinline__ double chunk_squares(const G *g, int n) {
+    double s[2] = {0.0, 0.0};
+    float x[kWide];
+    int i = threadIdx.x * kWide;
+    if (n == kChunkLen) {
+        Pack<G, kWide> p[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) p[u].load(g + i + u * kTurn);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            p[u].to(x);
+            s[u & 1] = squares(x, s[u & 1]);
+        }
+        return s[0] + s[1];
+    }
+    for (; i < n; i += kTurn) {
+        Pack<G, kWide> p;
+        p.load(g + i, n - i);
+        p.to(x);
+        s[0] = squares(x, s[0]);
+    }
+    return s[0];
 }
 
 __device__ double block_sum(double x) {
@@ -39,21 +74,6 @@ __device__ double block_sum(double x) {
     return t;
 }
 
-// Each workgroup sums its chunks (a fixed set: chunk b, b + grid, ...) into
-// its own partial; a second launch joins them in order.  No atomics: the
-// result is the same on every call.
-__global__ void __launch_bounds__(kBlock) k_grad_squares(const TensorChunk *ck, int n_chunks, double *part) {
-    double s = 0.0;
-    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const TensorChunk k = ck[c];
-        if (k.grad_type == DD_F32) s += chunk_squares(static_cast<const float *>(k.grad), k.n);
-        else if (k.grad_type == DD_BF16) s += chunk_squares(static_cast<const bf16_t *>(k.grad), k.n);
-        else s += chunk_squares(static_cast<const f16_t *>(k.grad), k.n);
-    }
-    s = block_sum(s);
-    if (threadIdx.x == 0) part[blockIdx.x] = s;
-}
-
 __device__ void write_stats(double s, double max_norm, const float *inv_scale, float *stats) {
     const double u = inv_scale ? (double)*inv_scale : 1.0;
     const double norm = sqrt(s) * u;
@@ -65,38 +85,79 @@ __device__ void write_stats(double s, double max_norm, const float *inv_scale, f
     stats[2] = finite ? 0.0f : 1.0f;
 }
 
-__global__ void __launch_bounds__(kBlock) k_grad_join(const double *part, int n, double max_norm, const float *inv_scale,
-                                                      float *stats) {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += kBlock) s += part[i];
-    s = block_sum(s);
-    if (threadIdx.x == 0) write_stats(s, max_norm, inv_scale, stats);
+// How the workgroups of a launch find out which of them is the last: each takes
+// a ticket when it is done.  What they hand to the last one are atomic stores
+// and loads of the device's scope, which pass the caches of the eight XCDs, so
+// all that is needed is that a store has arrived before its ticket is taken:
+// the wait.  (An acquire-release ticket writes back and invalidates an L2 each
+// time: 20 ns a workgroup one after the other, 1,024 of them 25 us.)
+__device__ __forceinline__ bool last_ticket(uint32_t *ticket) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    return __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
 }
 
-template <class G, class D>
-__device__ void chunk_clip(const G *g, D *d, int n, float f) {
-    for (int i = threadIdx.x; i < n; i += kBlock) {
-        const float x = (float)global(g)[i];
-        global(d)[i] = (D)(f == 0.0f ? 0.0f : x * f);
+// Each workgroup sums its chunks (a fixed set: chunk b, b + grid, ...) into its
+// own partial; the one that finishes last adds the partials in their order, so
+// the result is the same bits on every call.
+__global__ void __launch_bounds__(kBlock) k_grad_norm(const TensorChunk *ck, int n_chunks, double *part, uint32_t *ticket,
+                                                      double max_norm, const float *inv_scale, float *stats) {
+    double s = 0.0;
+    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
+        const TensorChunk k = ck[c];
+        if (k.grad_type == DD_F32) s += chunk_squares(static_cast<const float *>(k.grad), k.n);
+        else if (k.grad_type == DD_BF16) s += chunk_squares(static_cast<const bf16_t *>(k.grad), k.n);
+        else s += chunk_squares(static_cast<const f16_t *>(k.grad), k.n);
+    }
+    s = block_sum(s);
+    __shared__ bool last;
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(&part[blockIdx.x], s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = last_ticket(ticket);
+    }
+    __syncthreads();
+    if (!last) return;
+    s = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kBlock)
+        s += __hip_atomic_load(&part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s = block_sum(s);
+    if (threadIdx.x == 0) {
+        write_stats(s, max_norm, inv_scale, stats);
+        *ticket = 0;
     }
 }
 
-template <class G>
-__device__ void chunk_clip_to(const G *g, const TensorChunk &d, int n, float f) {
-    if (d.grad_type == DD_F32) chunk_clip(g, static_cast<float *>(d.grad), n, f);
-    else if (d.grad_type == DD_BF16) chunk_clip(g, static_cast<bf16_t *>(d.grad), n, f);
-    else chunk_clip(g, static_cast<f16_t *>(d.grad), n, f);
+template <class G, class D>
+__device__ __forceinline__ void part_clip(const G *g, D *d, int n, float f) {
+    const int i = threadIdx.x * kWide;
+    if (i >= n) return;
+    Pack<G, kWide> p;
+    Pack<D, kWide> q;
+    float x[kWide];
+    p.load(g + i, n - i);
+    p.to(x);
+#pragma unroll
+    for (int j = 0; j < kWide; j++) x[j] = f == 0.0f ? 0.0f : x[j] * f;   // (an infinity too)
+    q.from(x);
+    q.store(d + i, n - i);
 }
 
-// Chunks of both lists are alike (equal sizes, one rule for the chunk length).
-__global__ void __launch_bounds__(kBlock) k_grad_clip(const TensorChunk *src, const TensorChunk *dst, int n_chunks,
+template <class G>
+__device__ __forceinline__ void part_clip_to(const G *g, const TensorChunk &d, int o, int n, float f) {
+    if (d.grad_type == DD_F32) part_clip(g + o, static_cast<float *>(d.grad) + o, n, f);
+    else if (d.grad_type == DD_BF16) part_clip(g + o, static_cast<bf16_t *>(d.grad) + o, n, f);
+    else part_clip(g + o, static_cast<f16_t *>(d.grad) + o, n, f);
+}
+
+// Chunks of both lists are alike (equal sizes).
+__global__ void __launch_bounds__(kBlock) k_grad_clip(const TensorChunk *src, const TensorChunk *dst, int64_t n_parts,
                                                       const float *stats) {
     const float f = stats[1];
-    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const TensorChunk a = src[c], b = dst[c];
-        if (a.grad_type == DD_F32) chunk_clip_to(static_cast<const float *>(a.grad), b, a.n, f);
-        else if (a.grad_type == DD_BF16) chunk_clip_to(static_cast<const bf16_t *>(a.grad), b, a.n, f);
-        else chunk_clip_to(static_cast<const f16_t *>(a.grad), b, a.n, f);
+    for (int64_t b = blockIdx.x; b < n_parts; b += gridDim.x) {
+        const TensorChunk a = src[b / kPartsOf], d = dst[b / kPartsOf];
+        const int o = (int)(b % kPartsOf) * kPartLen, n = a.n - o < kPartLen ? a.n - o : kPartLen;
+        if (a.grad_type == DD_F32) part_clip_to(static_cast<const float *>(a.grad), d, o, n, f);
+        else if (a.grad_type == DD_BF16) part_clip_to(static_cast<const bf16_t *>(a.grad), d, o, n, f);
+        else part_clip_to(static_cast<const f16_t *>(a.grad), d, o, n, f);
     }
 }
 
@@ -109,43 +170,8 @@ __device__ double power(double b, int64_t t) {
     return r;
 }
 
-struct AdamFactors {      // of one call, rounded once from 64 bits
-    float f;              // factor of the gradients
-    float b1, c1, b2, c2; // beta1, 1 - beta1, beta2, 1 - beta2
-    float l2, keep;       // added weight * l2, or kept share of the weight
-    float lr, rv, eps;    // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-};
-
-__device__ __forceinline__ void adam_one(const AdamFactors &a, bool decay, float g, float &w, float &m, float &v) {
-    g *= a.f;
-    if (decay) g = fmaf(a.l2, w, g);
-    m = fmaf(a.b1, m, a.c1 * g);
-    v = fmaf(a.b2, v, a.c2 * (g * g));
-    if (decay) w *= a.keep;
-    w -= a.lr * (m / fmaf(sqrtf(v), a.rv, a.eps));
-}
-
-template <class G>
-__device__ void chunk_adam(const TensorChunk &k, const AdamFactors &a) {
-    const G *g = static_cast<const G *>(k.grad);
-    const bool low = k.param_type != DD_F32;
-    for (int i = threadIdx.x; i < k.n; i += kBlock) {
-        float w = global(k.w)[i], m = global(k.m)[i], v = global(k.v)[i];
-        adam_one(a, k.decay, (float)global(g)[i], w, m, v);
-        global(k.w)[i] = w;
-        global(k.m)[i] = m;
-        global(k.v)[i] = v;
-        if (low) {
-            if (k.param_type == DD_BF16) global(static_cast<bf16_t *>(k.param))[i] = (bf16_t)w;
-            else global(static_cast<f16_t *>(k.param))[i] = (f16_t)w;
-        }
-    }
-}
-
-__global__ void __launch_bounds__(kBlock) k_adam(const TensorChunk *ck, int n_chunks, const int64_t *step, const float *stats,
-                                                 AdamParams p) {
-    if (stats && stats[2] != 0.0f) return;
-    const int64_t t = *step + 1;
+// What one call multiplies with, each rounded once from 64 bits.
+__device__ AdamFactors adam_factors(const AdamParams &p, int64_t t, const float *stats) {
     AdamFactors a;
     a.f = stats ? stats[1] : 1.0f;
     a.b1 = (float)p.beta1;
@@ -157,38 +183,159 @@ __global__ void __launch_bounds__(kBlock) k_adam(const TensorChunk *ck, int n_ch
     a.lr = (float)(p.lr / (1.0 - power(p.beta1, t)));
     a.rv = (float)(1.0 / sqrt(1.0 - power(p.beta2, t)));
     a.eps = (float)p.eps;
-    for (int c = blockIdx.x; c < n_chunks; c += gridDim.x) {
-        const TensorChunk k = ck[c];
-        if (k.grad_type == DD_F32) chunk_adam<float>(k, a);
-        else if (k.grad_type == DD_BF16) chunk_adam<bf16_t>(k, a);
-        else chunk_adam<f16_t>(k, a);
+    a.skip = 0;
+    return a;
+}
+
+__device__ __forceinline__ void adam_one(const AdamFactors &a, bool decay, float g, float &w, float &m, float &v) {
+    g *= a.f;
+    if (decay) g = fmaf(a.l2, w, g);
+    m = fmaf(a.b1, m, a.c1 * g);
+    v = fmaf(a.b2, v, a.c2 * (g * g));
+    if (decay) w *= a.keep;
+    w -= a.lr * (m / fmaf(sqrtf(v), a.rv, a.eps));
+}
+
+// Four elements per thread and load, two loads of each array at a time.
+constexpr int kAdamWide = 4, kAdamTurn = kBlock * kAdamWide, kAdamAhead = kPartLen / kAdamTurn;
+static_assert(kPartLen == kAdamAhead * kAdamTurn, "a part is whole turns of a workgroup");
+
+template <class G, class P>
+struct AdamPack {
+    Pack<G, kAdamWide> g;
+    Pack<float, kAdamWide> w, m, v;
+    template <class... Have>
+    __device__ __forceinline__ void load(const TensorChunk &k, int i, Have... have) {
+        g.load(static_cast<const G *>(k.grad) + i, have...);
+        w.load(k.w + i, have...);
+        m.load(k.m + i, have...);
+        v.load(k.v + i, have...);
+    }
+    template <class... Have>
+    __device__ __forceinline__ void step(const TensorChunk &k, const AdamFactors &a, int i, Have... have) {
+        float xg[kAdamWide], xw[kAdamWide], xm[kAdamWide], xv[kAdamWide];
+        g.to(xg);
+        w.to(xw);
+        m.to(xm);
+        v.to(xv);
+#pragma unroll
+        for (int j = 0; j < kAdamWide; j++) adam_one(a, k.decay, xg[j], xw[j], xm[j], xv[j]);
+        w.from(xw);
+        m.from(xm);
+        v.from(xv);
+        w.store(k.w + i, have...);
+        m.store(k.m + i, have...);
+        v.store(k.v + i, have...);
+        if (!std::is_same<P, float>::value) {
+            Pack<P, kAdamWide> p;
+            p.from(xw);
+            p.store(static_cast<P *>(k.param) + i, have...);
+        }
+    }
+};
+
+template <class G, class P>
+__device__ __forceinline__ void part_adam(const TensorChunk &k, const AdamFactors &a, int o, int n) {
+    int i = o + threadIdx.x * kAdamWide;
+    if (n - o >= kPartLen) {
+        AdamPack<G, P> p[kAdamAhead];
+#pragma unroll
+        for (int u = 0; u < kAdamAhead; u++) p[u].load(k, i + u * kAdamTurn);
+#pragma unroll
+        for (int u = 0; u < kAdamAhead; u++) p[u].step(k, a, i + u * kAdamTurn);
+        return;
+    }
+    for (; i < n; i += kAdamTurn) {
+        AdamPack<G, P> p;
+        p.load(k, i, n - i);
+        p.step(k, a, i, n - i);
+    }
+}
+template <class G>
+__device__ __forceinline__ void part_adam(const TensorChunk &k, const AdamFactors &a, int o, int n) {
+    if (k.param_type == DD_F32) part_adam<G, float>(k, a, o, n);
+    else if (k.param_type == DD_BF16) part_adam<G, bf16_t>(k, a, o, n);
+    else part_adam<G, f16_t>(k, a, o, n);
+}
+
+__device__ __forceinline__ void adam_part(const TensorChunk *ck, int64_t b, const AdamFactors &a) {
+    const TensorChunk k = ck[b / kPartsOf];
+    const int o = (int)(b % kPartsOf) * kPartLen;
+    if (o >= k.n) return;
+    const int n = k.n < o + kPartLen ? k.n : o + kPartLen;
+    if (k.grad_type == DD_F32) part_adam<float>(k, a, o, n);
+    else if (k.grad_type == DD_BF16) part_adam<bf16_t>(k, a, o, n);
+    else part_adam<f16_t>(k, a, o, n);
+}
+
+// The factors of a step, once for all workgroups, and the step's number.
+__global__ void k_adam_begin(int64_t *step, const float *stats, AdamParams p, AdamFactors *out) {
+    AdamFactors a = {};
+    a.skip = stats && stats[2] != 0.0f;
+    if (!a.skip) a = adam_factors(p, *step += 1, stats);
+    *out = a;
+}
+__global__ void __launch_bounds__(kBlock) k_adam(const TensorChunk *ck, int64_t n_parts, const AdamFactors *factors) {
+    const AdamFactors a = *factors;
+    if (a.skip) return;
+    for (int64_t b = blockIdx.x; b < n_parts; b += gridDim.x) adam_part(ck, b, a);
+}
+
+// Small lists: one launch, in which every workgroup finds the factors itself,
+// and the one that finishes last counts the step.  By then all others have
+// read its number: each takes its ticket after it has used the number, and
+// only the last ticket is followed by the write.
+__global__ void __launch_bounds__(kBlock) k_adam_small(const TensorChunk *ck, int64_t n_parts, int64_t *step, const float *stats,
+                                                       AdamParams p, uint32_t *ticket) {
+    if (stats && stats[2] != 0.0f) return;
+    const int64_t t = __hip_atomic_load(step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+    const AdamFactors a = adam_factors(p, t, stats);
+    if (blockIdx.x < n_parts) adam_part(ck, blockIdx.x, a);
+    __syncthreads();
+    if (threadIdx.x == 0 && last_ticket(ticket)) {
+        *step = t;
+        *ticket = 0;
     }
 }
 
-__global__ void k_adam_step(int64_t *step, const float *stats) {
-    if (!(stats && stats[2] != 0.0f)) *step += 1;
-}
+constexpr int64_t kMaxGrid = 1 << 22;     // workgroups of a launch; parts beyond go round
 
-int grid_of(int n_chunks) { return n_chunks < kNormParts ? (n_chunks < 1 ? 1 : n_chunks) : kNormParts; }
+// Workgroups of the norm: four chunks each, at least 256 (one per compute
+// unit), at most kNormParts: each ticket is 12 ns, one after the other (1,000
+// tensors of 300 elements or fewer: 7.5 us with 256, 15.6 with 1,024).
+int norm_grid(int n_chunks) {
+    const int g = n_chunks / 4 < 256 ? 256 : n_chunks / 4 < kNormParts ? n_chunks / 4 : kNormParts;
+    return n_chunks < 1 ? 1 : n_chunks < g ? n_chunks : g;
+}
+// Up to here the tickets of k_adam_small (12 ns each) cost less than a launch
+// more: 1 part 4.6 us against 7.2, 320 parts 6.7 against 7.1, 480 parts 8.5
+// against 7.3.
+constexpr int64_t kSmallParts = 320;
+
+unsigned grid_of(int64_t parts) { return (unsigned)(parts < kMaxGrid ? parts : kMaxGrid); }
 
 }  // namespace
 
 hipError_t launch_grad_norm(const dd_tensors *t, double max_norm, const float *inv_scale, float *stats, hipStream_t s) {
-    const int g = grid_of(t->n_chunks);
-    k_grad_squares<<<g, kBlock, 0, s>>>(t->chunks, t->n_chunks, t->part);
-    k_grad_join<<<1, kBlock, 0, s>>>(t->part, g, max_norm, inv_scale, stats);
+    k_grad_norm<<<norm_grid(t->n_chunks), kBlock, 0, s>>>(t->chunks, t->n_chunks, t->work->part, &t->work->ticket, max_norm, inv_scale, stats);
     return hipGetLastError();
 }
 
 hipError_t launch_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float *stats, hipStream_t s) {
-    if (src->n_chunks == 0) return hipSuccess;
-    k_grad_clip<<<grid_of(src->n_chunks), kBlock, 0, s>>>(src->chunks, dst->chunks, src->n_chunks, stats);
+    const int64_t parts = (int64_t)src->n_chunks * kPartsOf;
+    if (parts == 0) return hipSuccess;
+    k_grad_clip<<<grid_of(parts), kBlock, 0, s>>>(src->chunks, dst->chunks, parts, stats);
     return hipGetLastError();
 }
 
 hipError_t launch_adam(const dd_tensors *t, int64_t *step, const float *stats, const AdamParams &p, hipStream_t s) {
-    if (t->n_chunks) k_adam<<<grid_of(t->n_chunks), kBlock, 0, s>>>(t->chunks, t->n_chunks, step, stats, p);
-    k_adam_step<<<1, 1, 0, s>>>(step, stats);
+    const int64_t parts = (int64_t)t->n_chunks * kPartsOf;
+    if (parts <= kSmallParts) {
+        k_adam_small<<<parts < 1 ? 1 : (unsigned)parts, kBlock, 0, s>>>(t->chunks, parts, step, stats, p, &t->work->ticket);
+    } else {
+        k_adam_begin<<<1, 1, 0, s>>>(step, stats, p, &t->work->factors);
+        k_adam<<<grid_of(parts), kBlock, 0, s>>>(t->chunks, parts, &t->work->factors);
+    }
     return hipGetLastError();
 }
 
