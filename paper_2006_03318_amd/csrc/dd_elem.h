@@ -55,6 +55,19 @@ struct Pack {
 #pragma unroll
         for (int i = 0; i < N; i++) x[i] = (float)v[i];
     }
+    // What was computed from the pack before is not kept beyond this point: it
+    // is cheaper to convert again than to hold twice the registers.
+    __device__ __forceinline__ void forget() {
+        typedef uint32_t words __attribute__((ext_vector_type(N * sizeof(E) / 4)));
+        words w = __builtin_bit_cast(words, v);
+#pragma unroll
+        for (unsigned i = 0; i < N * sizeof(E) / 4; i++) {
+            uint32_t x = w[i];
+            asm volatile("" : "+v"(x));
+            w[i] = x;
+        }
+        v = __builtin_bit_cast(vec, w);
+    }
     // (rounds to nearest even)
     __device__ __forceinline__ void from(const float (&x)[N]) {
         fvec f;

@@ -317,9 +317,13 @@ __global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArg
     const int lane = threadIdx.x % LANES;
     const int cols = (int)a.cols;
     float sum[NV][8] = {};
-    Weights<T> w[NV];
+    float w[NV][8];
 #pragma unroll
-    for (int k = 0; k < NV; k++) w[k].load(a.weight, a.weight_type, 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+    for (int k = 0; k < NV; k++) {
+        Weights<T> p;
+        p.load(a.weight, a.weight_type, 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
+        p.to(a.weight, a.weight_type, w[k]);
+    }
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * kRows + row_of_thread<LANES>(); row < a.rows;
          row += (int64_t)gridDim.x * kRows, turn ^= 1) {
@@ -337,46 +341,63 @@ __global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArg
             for (int k = 0; k < NV; k++) pe[k].load(dh + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
         }
         const float rstd = a.rstd[row];
-        float g[NV][8], xh[NV][8], q = 0.0f;
+        float q = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            float y[8];
-            pd[k].to(g[k]);
-            ph[k].to(xh[k]);
-            w[k].to(a.weight, a.weight_type, y);
+            float d[8], x[8];
+            pd[k].to(d);
+            ph[k].to(x);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                xh[k][i] *= rstd;
-                sum[k][i] = fmaf(g[k][i], xh[k][i], sum[k][i]);
-                g[k][i] *= y[i];
-                q = fmaf(g[k][i], xh[k][i], q);
+                const float t = d[i] * (x[i] * rstd);
+                sum[k][i] += t;
+                q = fmaf(w[k][i], t, q);
             }
         }
         const float c = RowSum<LANES>::sum(q, slots[turn]) / (float)cols;
 #pragma unroll
         for (int k = 0; k < NV; k++) {
-            float y[8];
+            float d[8], x[8], y[8];
+            if (LANES == 16 || LANES == 1024) {     // (their registers would spill)
+                pd[k].forget();
+                ph[k].forget();
+            }
+            pd[k].to(d);
+            ph[k].to(x);
 #pragma unroll
             for (int i = 0; i < 8; i++) y[i] = 0.0f;
             if (a.dh) pe[k].to(y);
             Pack<T, 8> p;
 #pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = fmaf(g[k][i] - xh[k][i] * c, rstd, y[i]);
+            for (int i = 0; i < 8; i++) y[i] = fmaf(d[i] * w[k][i] - x[i] * rstd * c, rstd, y[i]);
             p.from(y);
             p.store(dx + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
         }
     }
     if (!a.dw) return;
-    part += (int64_t)blockIdx.x * cols;
+    // one workgroup has all rows: its sums are the result
+    if (gridDim.x > 1) part += (int64_t)blockIdx.x * cols;
+    auto put = [&](int c, const float (&x)[8]) {
+        if (gridDim.x > 1) {
+            Pack<float, 8> p;
+            p.from(x);
+            p.store(part + c, cols - c);
+        } else if (a.weight_type == DD_F32) {
+            Pack<float, 8> p;
+            p.from(x);
+            p.store(static_cast<float *>(a.dw) + c, cols - c);
+        } else {
+            Pack<T, 8> p;
+            p.from(x);
+            p.store(static_cast<T *>(a.dw) + c, cols - c);
+        }
+    };
     if (kRows == 1) {
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            Pack<float, 8> p;
-            p.from(sum[k]);
-            p.store(part + 8 * (lane + k * LANES), cols - 8 * (lane + k * LANES));
-        }
+        for (int k = 0; k < NV; k++) put(8 * (lane + k * LANES), sum[k]);
         return;
     }
+    // rows that share the workgroup, joined in order, LANES packs at a time
     __shared__ float all[kRows * LANES * 8];
 #pragma unroll
     for (int k = 0; k < NV; k++) {
@@ -384,10 +405,12 @@ __global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArg
 #pragma unroll
         for (int i = 0; i < 8; i++) all[threadIdx.x * 8 + i] = sum[k][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < LANES * 8 && k * LANES * 8 + c < cols; c += kThreads) {
-            float t = 0.0f;
-            for (int r = 0; r < kRows; r++) t += all[r * LANES * 8 + c];
-            part[k * LANES * 8 + c] = t;
+        if (threadIdx.x < LANES) {
+            float t[8] = {};
+            for (int r = 0; r < kRows; r++)
+#pragma unroll
+                for (int i = 0; i < 8; i++) t[i] += all[(r * LANES + threadIdx.x) * 8 + i];
+            put(8 * (threadIdx.x + k * LANES), t);
         }
     }
 }
@@ -439,14 +462,20 @@ __global__ void __launch_bounds__(kBlock) k_rms_dw_loop(RmsGradArgs a, float *pa
     }
 }
 
-// A workgroup has 32 columns; 32 threads share a column.
+// A workgroup has 32 columns; 32 threads share a column, each with up to 16
+// loads under way (512 partial sums, all of them).
 __global__ void __launch_bounds__(1024) k_rms_dw_join(RmsGradArgs a, const float *part, int n) {
     __shared__ float lds[32][33];
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + x;
     float s = 0.0f;
-    if (c < a.cols)
-        for (int i = y; i < n; i += 32) s += part[i * a.cols + c];
+    if (c < a.cols) {
+        float t[kRmsParts / 32];
+#pragma unroll
+        for (int i = 0; i < kRmsParts / 32; i++) t[i] = y + 32 * i < n ? part[(y + 32 * i) * a.cols + c] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kRmsParts / 32; i++) s += t[i];
+    }
     lds[y][x] = s;
     __syncthreads();
     if (y || c >= a.cols) return;
@@ -513,12 +542,21 @@ void rms_norm(const RmsArgs &a, hipStream_t s) {
     k_rms_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
 }
 
-// Workgroups of the gradient: as many as run at once, each with rows to go over.
-int grad_parts(int64_t rows, int64_t cols) {
+// The gradient holds three times as much per column: four packs do not fit.
+Shape grad_shape(int64_t cols) {
     const Shape p = row_shape(cols);
+    return p.packs > 2 ? Shape{0, 0} : p;
+}
+
+// Workgroups of the gradient: as many as run at once, each with rows to go
+// over: two to a compute unit where they are of four waves and hold less than
+// 16 KiB of a row (65,536 x 2,048 bf16: 196 us, one to each 306; 16,384 x 4,096
+// f32: 204, one to each 188; 32,768 x 8,192 bf16: 404 and 369).
+int grad_parts(int64_t rows, int64_t cols, int elem) {
+    const Shape p = grad_shape(cols);
     if (!p.lanes) return dw_runs(rows);
     const int per = grad_threads(p.lanes) / p.lanes;
-    const int64_t need = (rows + per - 1) / per, most = p.lanes <= 64 || p.lanes == 1024 ? 256 : 512;
+    const int64_t need = (rows + per - 1) / per, most = p.lanes == 256 && p.lanes * p.packs * 8 * elem < 16384 ? 512 : 256;
     return (int)(need < 1 ? 1 : need < most ? need : most);
 }
 
@@ -528,8 +566,8 @@ void run_grad(const RmsGradArgs &a, float *work, int parts, hipStream_t s) {
 }
 template <class T>
 void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
-    const Shape p = row_shape(a.cols);
-    const int n = grad_parts(a.rows, a.cols);
+    const Shape p = grad_shape(a.cols);
+    const int n = grad_parts(a.rows, a.cols, sizeof(T));
     auto join = [&] { k_rms_dw_join<<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a, work, n); };
     if (!p.lanes) {
         if (a.dw) {       // first: dx may overwrite what it reads
@@ -546,14 +584,15 @@ void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
     else if (p.lanes == 256 && p.packs == 1) run_grad<T, 256, 1>(a, work, n, s);
     else if (p.lanes == 256) run_grad<T, 256, 2>(a, work, n, s);
     else if (p.lanes == 512) run_grad<T, 512, 2>(a, work, n, s);
-    else if (p.packs == 2) run_grad<T, 1024, 2>(a, work, n, s);
-    else run_grad<T, 1024, 4>(a, work, n, s);
-    if (a.dw) join();
+    else run_grad<T, 1024, 2>(a, work, n, s);
+    if (a.dw && n > 1) join();
 }
 
 }  // namespace
 
-size_t rms_grad_work(int64_t rows, int64_t cols) { return (size_t)grad_parts(rows, cols) * (size_t)cols * sizeof(float); }
+size_t rms_grad_work(int64_t rows, int64_t cols) {
+    return (size_t)grad_parts(rows, cols, 2) * (size_t)cols * sizeof(float);    // (the most of any type)
+}
 
 hipError_t launch_rms_norm(const RmsArgs &a, hipStream_t s) {
     if (a.type == DD_F32) rms_norm<float>(a, s);
