@@ -286,15 +286,18 @@ def _gpu(name, t, count, *types):
     """Address of a contiguous tensor on the GPU (None stays None)."""
     if t is None:
         return 0
+    if (t.is_cuda and (_DT or _types()).get(t.dtype, -1) in types and t.numel() == count
+            and t.is_contiguous()):
+        return t.data_ptr()
+    if not isinstance(name, str):
+        name = "tensor %d: %s" % name
     if not t.is_cuda:
         raise ValueError("%s must be on the GPU" % name)
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if (_DT or _types()).get(t.dtype, -1) not in types:
-        raise TypeError("%s: unexpected type %s" % (name, t.dtype))
     if t.numel() != count:
         raise ValueError("%s: expected %d elements, got %d" % (name, count, t.numel()))
-    return t.data_ptr()
+    raise TypeError("%s: unexpected type %s" % (name, t.dtype))
 
 
 def _small(name, t, count, dtype):
@@ -312,17 +315,19 @@ def dd_tensors_load(tensors, stream=None):
     """A handle for a list of tensors: each a dict with `grad` and, for
     dd_adam_step, `param`, `m`, `v`, `master` (16-bit params) and `decay`
     (default True).  They must live, where they are, as long as the handle."""
+    known = {"grad", "param", "master", "m", "v", "decay"}
     rows = []
     for i, t in enumerate(tensors):
-        unknown = set(t) - {"grad", "param", "master", "m", "v", "decay"}
-        if unknown:
-            raise ValueError("tensor %d: unknown %s" % (i, ", ".join(sorted(unknown))))
+        if not known.issuperset(t):
+            raise ValueError("tensor %d: unknown %s" % (i, ", ".join(sorted(set(t) - known))))
         g, p = t["grad"], t.get("param")
         n = g.numel()
-        a = [_gpu("tensor %d: grad" % i, g, n, DD_F32, DD_BF16, DD_F16),
-             _gpu("tensor %d: param" % i, p, n, DD_F32, DD_BF16, DD_F16)]
-        a += [_gpu("tensor %d: %s" % (i, k), t.get(k), n, DD_F32) for k in ("master", "m", "v")]
-        rows.append(_TENSOR.pack(*a, n, _DT[g.dtype], DD_F32 if p is None else _DT[p.dtype],
+        rows.append(_TENSOR.pack(_gpu((i, "grad"), g, n, DD_F32, DD_BF16, DD_F16),
+                                 _gpu((i, "param"), p, n, DD_F32, DD_BF16, DD_F16),
+                                 _gpu((i, "master"), t.get("master"), n, DD_F32),
+                                 _gpu((i, "m"), t.get("m"), n, DD_F32),
+                                 _gpu((i, "v"), t.get("v"), n, DD_F32), n, _DT[g.dtype],
+                                 DD_F32 if p is None else _DT[p.dtype],
                                  0 if t.get("decay", True) else 1, 0))
     out = _vp()
     buf = ctypes.create_string_buffer(b"".join(rows), len(rows) * _TENSOR.size + 1)
@@ -363,22 +368,24 @@ def dd_adam_step(t, d_step, d_stats=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1
         _check(rc)
 
 
-def _rows(name, t, shape, dtype):
-    """(address, row stride) of rows: the last dimension is one row."""
+def _rows(name, t, n, cols, dtype):
+    """(address, row stride) of n elements in rows of cols: the last dimension
+    is one row."""
     if t is None:
         return 0, 0
+    if t.is_cuda and t.dtype is dtype and t.numel() == n and t.size(-1) == cols:
+        if t.is_contiguous():
+            return t.data_ptr(), cols
+        if t.dim() == 2 and (cols == 1 or t.stride(1) == 1):
+            return t.data_ptr(), t.stride(0)
     if not t.is_cuda:
         raise ValueError("%s must be on the GPU" % name)
-    if t.shape != shape:
-        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if t.is_contiguous():
-        return t.data_ptr(), shape[-1]
-    if t.dim() != 2 or (shape[-1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s: elements of a row must be consecutive, and more than two dimensions "
-                         "contiguous" % name)
-    return t.data_ptr(), t.stride(0)
+    if t.numel() != n or t.size(-1) != cols:
+        raise ValueError("%s: expected %d rows of %d, got %s" % (name, n // cols, cols, tuple(t.shape)))
+    raise ValueError("%s: elements of a row must be consecutive, and more than two dimensions "
+                     "contiguous" % name)
 
 
 _RMS = struct.Struct("@6q7P4if i")
@@ -388,7 +395,7 @@ _RMS_GRAD = struct.Struct("@6q8P2i")
 def _row_types(x, weight):
     types = _DT or _types()
     kind = types.get(x.dtype, -1)
-    if not 0 <= kind <= DD_F16 or x.dim() < 1 or x.shape[-1] < 1:
+    if not 0 <= kind <= DD_F16 or x.dim() < 1 or x.size(-1) < 1:
         raise TypeError("rows must be float32, bfloat16 or float16 and not empty")
     if weight is None:
         return kind, DD_F32
@@ -404,22 +411,15 @@ def dd_rms_norm(x, residual, weight, eps, out, h=None, rstd=None, scales=None, g
     [rows, groups]).  residual, weight, h (receives x + residual) and rstd may
     be None."""
     kind, wk = _row_types(x, weight)
-    shape = x.shape
-    cols = shape[-1]
-    n = x.numel()
+    cols, n, dt = x.size(-1), x.numel(), x.dtype
     rows = n // cols
-    px, sx = _rows("x", x, shape, x.dtype)
-    pr, sr = _rows("residual", residual, shape, x.dtype)
-    ph, sh = _rows("h", h, shape, x.dtype)
-    ok = _DT.get(out.dtype, -1)
-    po, so = _rows("out", out, shape, out.dtype)
-    if rstd is not None:
-        _gpu("rstd", rstd, rows, DD_F32)
-    if scales is not None:
-        _gpu("scales", scales, rows * (-(-cols // group) if group > 0 else 1), DD_F32)
+    px, sx = _rows("x", x, n, cols, dt)
+    pr, sr = _rows("residual", residual, n, cols, dt)
+    ph, sh = _rows("h", h, n, cols, dt)
+    po, so = _rows("out", out, n, cols, out.dtype)
     args = _RMS.pack(rows, cols, sx, sr, sh, so, px, pr, _gpu("weight", weight, cols, wk), ph, po,
-                     0 if scales is None else scales.data_ptr(), 0 if rstd is None else rstd.data_ptr(),
-                     kind, wk, ok, group, eps, 0)
+                     _gpu("scales", scales, rows * (-(-cols // group) if group > 0 else 1), DD_F32),
+                     _gpu("rstd", rstd, rows, DD_F32), kind, wk, _DT.get(out.dtype, -1), group, eps, 0)
     rc = (_lib or lib()).dd_rms_norm(args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -430,13 +430,12 @@ def dd_rms_norm_grad(dy, h, weight, rstd, dx, dw=None, dh=None, work=None, strea
     on its other ways.  work: uint8 of dd_rms_norm_grad_work(rows, cols), or
     None (from the library's cache)."""
     kind, wk = _row_types(h, weight if weight is not None else dw)
-    shape = h.shape
-    cols = shape[-1]
-    rows = h.numel() // cols
-    pd, sd = _rows("dy", dy, shape, h.dtype)
-    ph, sh = _rows("h", h, shape, h.dtype)
-    pe, se = _rows("dh", dh, shape, h.dtype)
-    px, sx = _rows("dx", dx, shape, h.dtype)
+    cols, n, dt = h.size(-1), h.numel(), h.dtype
+    rows = n // cols
+    pd, sd = _rows("dy", dy, n, cols, dt)
+    ph, sh = _rows("h", h, n, cols, dt)
+    pe, se = _rows("dh", dh, n, cols, dt)
+    px, sx = _rows("dx", dx, n, cols, dt)
     if work is not None and (not work.is_cuda or not work.is_contiguous()
                              or work.numel() * work.element_size() < dd_rms_norm_grad_work(rows, cols)):
         raise ValueError("work must hold dd_rms_norm_grad_work(rows, cols) bytes on the GPU")

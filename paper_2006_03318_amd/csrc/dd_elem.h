@@ -117,7 +117,7 @@ __device__ __forceinline__ double wave_sum(double x) {
     return x;
 }
 
-inline int32_t elem_size(int32_t type) {
+__host__ __device__ inline int32_t elem_size(int32_t type) {
     return type == DD_F32 ? 4 : type == DD_BF16 || type == DD_F16 ? 2 : type == DD_E4M3 || type == DD_I8 ? 1 : 0;
 }
 

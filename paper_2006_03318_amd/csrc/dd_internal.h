@@ -207,6 +207,11 @@ struct alignas(64) TensorChunk {
 };
 static_assert(sizeof(TensorChunk) == 64, "record size");
 constexpr int64_t kChunkLen = 8192;
+// A tensor of n elements, whose chunks start at `first`.
+struct TensorPlace {
+    TensorChunk whole;
+    int64_t n, first;
+};
 constexpr int kNormParts = 1024;  // workgroups of the norm, at most
 struct AdamFactors {
     float f;                      // factor of the gradients
@@ -462,6 +467,8 @@ struct AdamParams {
     double lr, beta1, beta2, eps, weight_decay;
     int32_t decoupled;
 };
+// the list's chunks from its tensors (of n > 0), and its working memory
+hipError_t launch_tensor_chunks(const TensorPlace *p, int count, const dd_tensors *t, hipStream_t s);
 hipError_t launch_grad_norm(const dd_tensors *t, double max_norm, const float *inv_scale, float *stats, hipStream_t s);
 hipError_t launch_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float *stats, hipStream_t s);
 hipError_t launch_adam(const dd_tensors *t, int64_t *step, const float *stats, const AdamParams &p, hipStream_t s);

@@ -85,44 +85,48 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
         x->sizes.push_back(t[i].n);
     }
     if (with && without) return fail(DD_EINVAL, "some tensors have params and some have none");
-    const int64_t len = dd::kChunkLen;
-    for (int32_t i = 0; i < count; i++) chunks += (t[i].n + len - 1) / len;
+    for (int32_t i = 0; i < count; i++) chunks += (t[i].n + dd::kChunkLen - 1) / dd::kChunkLen;
     if (chunks >= (int64_t(1) << 31)) return fail(DD_EINVAL, "too many elements for one list");
     x->count = count;
     x->n_chunks = (int32_t)chunks;
     x->params = without == 0;
-    std::vector<dd::TensorChunk> h;
-    h.reserve((size_t)chunks);
+    std::vector<dd::TensorPlace> h;
+    h.reserve((size_t)count);
+    int64_t first = 0;
     for (int32_t i = 0; i < count; i++) {
         const dd_tensor &a = t[i];
-        for (int64_t o = 0; o < a.n; o += len) {
-            dd::TensorChunk c;
-            memset(&c, 0, sizeof(c));
-            c.grad = static_cast<char *>(a.grad) + o * dd::elem_size(a.grad_type);
-            if (a.param) {
-                c.param = static_cast<char *>(a.param) + o * dd::elem_size(a.param_type);
-                c.w = (a.master ? a.master : static_cast<float *>(a.param)) + o;
-                c.m = a.m + o;
-                c.v = a.v + o;
-            }
-            c.n = (int32_t)(a.n - o < len ? a.n - o : len);
-            c.grad_type = (uint8_t)a.grad_type;
-            c.param_type = (uint8_t)a.param_type;
-            c.decay = !a.no_decay;
-            h.push_back(c);
-        }
+        if (a.n == 0) continue;
+        dd::TensorPlace c;
+        memset(&c, 0, sizeof(c));
+        c.whole.grad = a.grad;
+        c.whole.param = a.param;
+        c.whole.w = a.master ? a.master : static_cast<float *>(a.param);
+        c.whole.m = a.m;
+        c.whole.v = a.v;
+        c.whole.grad_type = (uint8_t)a.grad_type;
+        c.whole.param_type = (uint8_t)a.param_type;
+        c.whole.decay = !a.no_decay;
+        c.n = a.n;
+        c.first = first;
+        first += (a.n + dd::kChunkLen - 1) / dd::kChunkLen;
+        h.push_back(c);
     }
     hipError_t e = hipGetDevice(&x->device);
-    void *mem = nullptr;
-    if (e == hipSuccess) e = dd::dalloc(&mem, sizeof(dd::TensorWork) + sizeof(dd::TensorChunk) * h.size(), s);
+    void *mem = nullptr, *places = nullptr;
+    if (e == hipSuccess) e = dd::dalloc(&mem, sizeof(dd::TensorWork) + sizeof(dd::TensorChunk) * (size_t)chunks, s);
     if (e != hipSuccess) return hip_fail(e, "alloc tensor list");
     x->work = static_cast<dd::TensorWork *>(mem);
     x->chunks = reinterpret_cast<dd::TensorChunk *>(x->work + 1);
-    const uint32_t none = 0;
-    e = hipMemcpyAsync(&x->work->ticket, &none, sizeof(none), hipMemcpyHostToDevice, s);
-    if (e == hipSuccess && !h.empty())
-        e = hipMemcpyAsync(x->chunks, h.data(), sizeof(dd::TensorChunk) * h.size(), hipMemcpyHostToDevice, s);
-    if (e == hipSuccess) e = hipStreamSynchronize(s);
+    if (!h.empty()) {
+        e = dd::dalloc(&places, sizeof(dd::TensorPlace) * h.size(), s);
+        if (e == hipSuccess)
+            e = hipMemcpyAsync(places, h.data(), sizeof(dd::TensorPlace) * h.size(), hipMemcpyHostToDevice, s);
+    }
+    if (e == hipSuccess)
+        e = dd::launch_tensor_chunks(static_cast<dd::TensorPlace *>(places), (int)h.size(), x, s);
+    const hipError_t done = hipStreamSynchronize(s);      // (h is read until here)
+    if (e == hipSuccess) e = done;
+    dd::dfree(places, s);
     return e == hipSuccess ? DD_OK : hip_fail(e, "copy tensor list");
 }
 

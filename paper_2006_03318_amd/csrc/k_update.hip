@@ -24,6 +24,31 @@ namespace {
 constexpr int kBlock = 256;
 
 
+// One thread per chunk finds its tensor (the last that starts at or before it).
+__global__ void __launch_bounds__(kBlock) k_tensor_chunks(const TensorPlace *p, int count, TensorChunk *ck, int n_chunks,
+                                                          uint32_t *ticket) {
+    const int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (c == 0) *ticket = 0;
+    if (c >= n_chunks) return;
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (p[mid].first <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    TensorChunk k = p[lo].whole;
+    const int64_t o = (c - p[lo].first) * kChunkLen, left = p[lo].n - o;
+    k.grad = static_cast<char *>(k.grad) + o * elem_size(k.grad_type);
+    if (k.param) {
+        k.param = static_cast<char *>(k.param) + o * elem_size(k.param_type);
+        k.w += o;
+        k.m += o;
+        k.v += o;
+    }
+    k.n = (int)(left < kChunkLen ? left : kChunkLen);
+    ck[c] = k;
+}
+
 // Elements per thread and load.
 constexpr int kWide = 8, kTurn = kBlock * kWide, kAhead = kChunkLen / kTurn;
 static_assert(kChunkLen == kAhead * kTurn, "a chunk is whole turns of a workgroup");
@@ -315,6 +340,12 @@ constexpr int64_t kSmallParts = 320;
 unsigned grid_of(int64_t parts) { return (unsigned)(parts < kMaxGrid ? parts : kMaxGrid); }
 
 }  // namespace
+
+hipError_t launch_tensor_chunks(const TensorPlace *p, int count, const dd_tensors *t, hipStream_t s) {
+    const int64_t grid = ((int64_t)t->n_chunks + kBlock - 1) / kBlock;
+    k_tensor_chunks<<<grid < 1 ? 1 : (unsigned)grid, kBlock, 0, s>>>(p, count, t->chunks, t->n_chunks, &t->work->ticket);
+    return hipGetLastError();
+}
 
 hipError_t launch_grad_norm(const dd_tensors *t, double max_norm, const float *inv_scale, float *stats, hipStream_t s) {
     k_grad_norm<<<norm_grid(t->n_chunks), kBlock, 0, s>>>(t->chunks, t->n_chunks, t->work->part, &t->work->ticket, max_norm, inv_scale, stats);
