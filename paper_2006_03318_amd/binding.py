@@ -336,8 +336,8 @@ def dd_tensors_load(tensors, stream=None):
 
 
 def dd_tensors_free(t):
-    if t:
-        lib().dd_tensors_free(t)
+    if t and _lib is not None:      # (None: the interpreter is shutting down)
+        _lib.dd_tensors_free(t)
 
 
 def dd_grad_norm(t, d_stats, max_norm=0.0, d_inv_scale=None, stream=None):

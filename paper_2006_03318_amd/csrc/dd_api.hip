@@ -11,7 +11,7 @@
 #include <stdlib.h>
 #include <string.h>
 
-#include "dd_internal.h"
+#include "dd_train.h"
 
 namespace {
 thread_local char g_err[512] = "";

@@ -195,59 +195,7 @@ struct dd_variants {
     mutable dd::ForeignUses uses;
 };
 
-// A list of tensors for the weight update (k_update.hip).
 namespace dd {
-// Part of one tensor, with the part's own addresses.
-struct alignas(64) TensorChunk {
-    void *grad, *param;
-    float *w, *m, *v;             // w: the f32 weights (master, or param itself)
-    int32_t n;
-    uint8_t grad_type, param_type, decay, pad;
-    uint64_t pad2[2];
-};
-static_assert(sizeof(TensorChunk) == 64, "record size");
-constexpr int64_t kChunkLen = 8192;
-// A tensor of n elements, whose chunks start at `first`.
-struct TensorPlace {
-    TensorChunk whole;
-    int64_t n, first;
-};
-constexpr int kNormParts = 1024;  // workgroups of the norm, at most
-struct AdamFactors {
-    float f;                      // factor of the gradients
-    float b1, c1, b2, c2;         // beta1, 1 - beta1, beta2, 1 - beta2
-    float l2, keep;               // weight decay: added weight * l2, kept share of the weight
-    float lr, rv, eps;            // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
-    int32_t skip;                 // nothing is applied
-};
-// Working memory of a list, zero when no call is under way but for what a
-// call writes before it reads it.
-struct TensorWork {
-    uint32_t ticket;              // workgroups that are done
-    AdamFactors factors;
-    alignas(64) double part[kNormParts];
-};
-}  // namespace dd
-
-struct dd_tensors {
-    int32_t count = 0;
-    int32_t n_chunks = 0;
-    bool params = false;          // weights and moments are there (dd_adam_step)
-    int device = 0;
-    hipStream_t stream = nullptr;
-    std::vector<int64_t> sizes;
-    dd::TensorWork *work = nullptr;   // one block of memory, the chunks behind it
-    dd::TensorChunk *chunks = nullptr;
-    mutable std::mutex mu;        // held while a call that uses work is queued
-    mutable dd::ForeignUses uses;
-};
-
-namespace dd {
-
-// the message of dd_last_error() for this host thread
-dd_status fail(dd_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-dd_status hip_fail(hipError_t e, const char *what);
-void no_error();
 
 // Read-backs of small results (below 4,000 bytes) through a pinned host buffer.  A copy from the device into
 // pageable memory waits for its stream by itself (about 10 us each); into
@@ -462,26 +410,6 @@ hipError_t launch_sim_event(const dd_graph *g, const EventLists &ev, const dd_va
                             int32_t policy, const uint8_t *pp, const int32_t *prio, int32_t *ref,
                             int64_t *est, uint32_t **keep, int64_t *finish, int64_t *start,
                             int64_t *makespan, uint32_t *err, hipStream_t s);
-// weight update over a list of tensors (k_update.hip)
-struct AdamParams {
-    double lr, beta1, beta2, eps, weight_decay;
-    int32_t decoupled;
-};
-// the list's chunks from its tensors (of n > 0), and its working memory
-hipError_t launch_tensor_chunks(const TensorPlace *p, int count, const dd_tensors *t, hipStream_t s);
-hipError_t launch_grad_norm(const dd_tensors *t, double max_norm, const float *inv_scale, float *stats, hipStream_t s);
-hipError_t launch_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float *stats, hipStream_t s);
-hipError_t launch_adam(const dd_tensors *t, int64_t *step, const float *stats, const AdamParams &p, hipStream_t s);
-
-// root-mean-square norm over rows (k_rms.hip); rows and cols at least 1 (the
-// gradient takes rows == 0: dw is zero then), work of rms_grad_work bytes
-typedef dd_rms_norm_args RmsArgs;
-typedef dd_rms_norm_grad_args RmsGradArgs;
-constexpr int kRmsParts = 512;         // partial sums of a weight's gradient, at most
-size_t rms_grad_work(int64_t rows, int64_t cols);
-hipError_t launch_rms_norm(const RmsArgs &a, hipStream_t s);
-hipError_t launch_rms_norm_grad(const RmsGradArgs &a, float *work, hipStream_t s);
-
 constexpr int kEventQueue = 1024;      // ready tasks one variant may hold
 constexpr int kEventIdBits = 22;       // tasks: n < 2^22
 constexpr int kEventMaxThreads = 4096;

@@ -7,7 +7,7 @@
 #include <new>
 
 #include "dd_elem.h"
-#include "dd_internal.h"
+#include "dd_train.h"
 
 namespace {
 
@@ -87,7 +87,6 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
     if (with && without) return fail(DD_EINVAL, "some tensors have params and some have none");
     for (int32_t i = 0; i < count; i++) chunks += (t[i].n + dd::kChunkLen - 1) / dd::kChunkLen;
     if (chunks >= (int64_t(1) << 31)) return fail(DD_EINVAL, "too many elements for one list");
-    x->count = count;
     x->n_chunks = (int32_t)chunks;
     x->params = without == 0;
     std::vector<dd::TensorPlace> h;
@@ -111,9 +110,8 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
         first += (a.n + dd::kChunkLen - 1) / dd::kChunkLen;
         h.push_back(c);
     }
-    hipError_t e = hipGetDevice(&x->device);
     void *mem = nullptr, *places = nullptr;
-    if (e == hipSuccess) e = dd::dalloc(&mem, sizeof(dd::TensorWork) + sizeof(dd::TensorChunk) * (size_t)chunks, s);
+    hipError_t e = dd::dalloc(&mem, sizeof(dd::TensorWork) + sizeof(dd::TensorChunk) * (size_t)chunks, s);
     if (e != hipSuccess) return hip_fail(e, "alloc tensor list");
     x->work = static_cast<dd::TensorWork *>(mem);
     x->chunks = reinterpret_cast<dd::TensorChunk *>(x->work + 1);

@@ -9,7 +9,7 @@
 //
 // Everything is computed in 32 bits and rounded once, where it is stored.
 #include "dd_elem.h"
-#include "dd_internal.h"
+#include "dd_train.h"
 
 namespace dd {
 

@@ -15,7 +15,7 @@
 #include <type_traits>
 
 #include "dd_elem.h"
-#include "dd_internal.h"
+#include "dd_train.h"
 
 namespace dd {
 
