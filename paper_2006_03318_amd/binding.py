@@ -373,7 +373,7 @@ def _rows(name, t, n, cols, dtype):
     is one row."""
     if t is None:
         return 0, 0
-    if t.is_cuda and t.dtype is dtype and t.numel() == n and t.size(-1) == cols:
+    if t.dtype is dtype and t.numel() == n and t.size(-1) == cols and t.is_cuda:
         if t.is_contiguous():
             return t.data_ptr(), cols
         if t.dim() == 2 and (cols == 1 or t.stride(1) == 1):

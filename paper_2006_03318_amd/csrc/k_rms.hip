@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArg
 #pragma unroll
         for (int k = 0; k < NV; k++) {
             float d[8], x[8], y[8];
-            if (LANES == 16 || LANES == 1024) {     // (their registers would spill)
+            if (LANES <= 16 || LANES == 1024) {     // (their registers would spill)
                 pd[k].forget();
                 ph[k].forget();
             }
@@ -504,13 +504,14 @@ int dw_runs(int64_t rows) {
 // 4,096 to 8 bits 4.8 with 256 lanes x 2 (128 x 4: 4.2, 64 x 8: 3.6, 1,024 x
 // 1: 2.7); 16,384 x 1,024 5.0 with 64 x 2 (256 x 1: 4.3); 65,536 x 2,048
 // 5.8 with 256 x 1 (64 x 4: 5.7); 65,536 x 128 to 8 bits 3.6 with 16 x 1
-// (64 x 1: 1.5).  Few rows take the same: 4 to 512 rows of 4,096 are as fast
+// (64 x 1: 1.5); 65,536 x 64 3.5 with 8 x 1 (16 x 1: 2.7).  Few rows take the same: 4 to 512 rows of 4,096 are as fast
 // with any of these shapes, the launch bounds them.
 struct Shape {
     int lanes, packs;      // 0: k_rms_loop
 };
 Shape row_shape(int64_t cols) {
     const int64_t n = (cols + 7) / 8;
+    if (n <= 8) return {8, 1};
     if (n <= 32) return {16, n <= 16 ? 1 : 2};
     if (n <= 128) return {64, n <= 64 ? 1 : 2};
     if (n <= 512) return {256, n <= 256 ? 1 : 2};
@@ -530,6 +531,7 @@ void run_rows(const RmsArgs &a, hipStream_t s) {
 template <class T>
 void rms_norm(const RmsArgs &a, hipStream_t s) {
     const Shape p = row_shape(a.cols);
+    if (p.lanes == 8) return run_rows<T, 8, 1>(a, s);
     if (p.lanes == 16 && p.packs == 1) return run_rows<T, 16, 1>(a, s);
     if (p.lanes == 16 && p.packs == 2) return run_rows<T, 16, 2>(a, s);
     if (p.lanes == 64 && p.packs == 1) return run_rows<T, 64, 1>(a, s);
@@ -577,7 +579,8 @@ void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
         if (a.rows > 0) k_rms_dx_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
         return;
     }
-    if (p.lanes == 16 && p.packs == 1) run_grad<T, 16, 1>(a, work, n, s);
+    if (p.lanes == 8) run_grad<T, 8, 1>(a, work, n, s);
+    else if (p.lanes == 16 && p.packs == 1) run_grad<T, 16, 1>(a, work, n, s);
     else if (p.lanes == 16) run_grad<T, 16, 2>(a, work, n, s);
     else if (p.lanes == 64 && p.packs == 1) run_grad<T, 64, 1>(a, work, n, s);
     else if (p.lanes == 64) run_grad<T, 64, 2>(a, work, n, s);
@@ -594,7 +597,9 @@ size_t rms_grad_work(int64_t rows, int64_t cols) {
     return (size_t)grad_parts(rows, cols, 2) * (size_t)cols * sizeof(float);    // (the most of any type)
 }
 
-hipError_t launch_rms_norm(const RmsArgs &a, hipStream_t s) {
+hipError_t launch_rms_norm(const RmsArgs &args, hipStream_t s) {
+    RmsArgs a = args;
+    if (a.group >= a.cols) a.group = 0;     // (a row narrower than a group may have fewer lanes than one)
     if (a.type == DD_F32) rms_norm<float>(a, s);
     else if (a.type == DD_BF16) rms_norm<bf16_t>(a, s);
     else rms_norm<f16_t>(a, s);
