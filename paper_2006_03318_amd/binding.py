@@ -368,12 +368,12 @@ def dd_adam_step(t, d_step, d_stats=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1
         _check(rc)
 
 
-def _rows(name, t, n, cols, dtype):
-    """(address, row stride) of n elements in rows of cols: the last dimension
-    is one row."""
+def _rows(name, t, shape, cols, dtype):
+    """(address, row stride) of rows of cols elements: the last dimension is
+    one row."""
     if t is None:
         return 0, 0
-    if t.dtype is dtype and t.numel() == n and t.size(-1) == cols and t.is_cuda:
+    if t.dtype is dtype and t.is_cuda and t.shape == shape:
         if t.is_contiguous():
             return t.data_ptr(), cols
         if t.dim() == 2 and (cols == 1 or t.stride(1) == 1):
@@ -382,8 +382,8 @@ def _rows(name, t, n, cols, dtype):
         raise ValueError("%s must be on the GPU" % name)
     if t.dtype is not dtype:
         raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
-    if t.numel() != n or t.size(-1) != cols:
-        raise ValueError("%s: expected %d rows of %d, got %s" % (name, n // cols, cols, tuple(t.shape)))
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     raise ValueError("%s: elements of a row must be consecutive, and more than two dimensions "
                      "contiguous" % name)
 
@@ -393,16 +393,18 @@ _RMS_GRAD = struct.Struct("@6q8P2i")
 
 
 def _row_types(x, weight):
+    """Types of the rows and the weight, and the rows' shape and length."""
     types = _DT or _types()
     kind = types.get(x.dtype, -1)
-    if not 0 <= kind <= DD_F16 or x.dim() < 1 or x.size(-1) < 1:
-        raise TypeError("rows must be float32, bfloat16 or float16 and not empty")
-    if weight is None:
-        return kind, DD_F32
-    wk = types.get(weight.dtype, -1)
+    if not 0 <= kind <= DD_F16:
+        raise TypeError("rows must be float32, bfloat16 or float16")
+    shape = x.shape
+    if not shape or shape[-1] < 1:
+        raise ValueError("rows must have a dimension and not be empty")
+    wk = DD_F32 if weight is None else types.get(weight.dtype, -1)
     if wk != DD_F32 and wk != kind:
         raise TypeError("weight must be float32 or the rows' type")
-    return kind, wk
+    return kind, wk, shape, shape[-1]
 
 
 def dd_rms_norm(x, residual, weight, eps, out, h=None, rstd=None, scales=None, group=0, stream=None):
@@ -410,16 +412,15 @@ def dd_rms_norm(x, residual, weight, eps, out, h=None, rstd=None, scales=None, g
     in x's type, or in 8 bits (out float8_e4m3fn or int8, with scales float32
     [rows, groups]).  residual, weight, h (receives x + residual) and rstd may
     be None."""
-    kind, wk = _row_types(x, weight)
-    cols, n, dt = x.size(-1), x.numel(), x.dtype
-    rows = n // cols
-    px, sx = _rows("x", x, n, cols, dt)
-    pr, sr = _rows("residual", residual, n, cols, dt)
-    ph, sh = _rows("h", h, n, cols, dt)
-    po, so = _rows("out", out, n, cols, out.dtype)
+    kind, wk, shape, cols = _row_types(x, weight)
+    rows, dt, odt = x.numel() // cols, x.dtype, out.dtype
+    px, sx = _rows("x", x, shape, cols, dt)
+    pr, sr = _rows("residual", residual, shape, cols, dt)
+    ph, sh = _rows("h", h, shape, cols, dt)
+    po, so = _rows("out", out, shape, cols, odt)
     args = _RMS.pack(rows, cols, sx, sr, sh, so, px, pr, _gpu("weight", weight, cols, wk), ph, po,
                      _gpu("scales", scales, rows * (-(-cols // group) if group > 0 else 1), DD_F32),
-                     _gpu("rstd", rstd, rows, DD_F32), kind, wk, _DT.get(out.dtype, -1), group, eps, 0)
+                     _gpu("rstd", rstd, rows, DD_F32), kind, wk, _DT.get(odt, -1), group, eps, 0)
     rc = (_lib or lib()).dd_rms_norm(args, None if stream is None else _stream(stream))
     if rc:
         _check(rc)
@@ -429,13 +430,12 @@ def dd_rms_norm_grad(dy, h, weight, rstd, dx, dw=None, dh=None, work=None, strea
     """dx and dw from the gradient dy of the norm's output; dh: what reaches h
     on its other ways.  work: uint8 of dd_rms_norm_grad_work(rows, cols), or
     None (from the library's cache)."""
-    kind, wk = _row_types(h, weight if weight is not None else dw)
-    cols, n, dt = h.size(-1), h.numel(), h.dtype
-    rows = n // cols
-    pd, sd = _rows("dy", dy, n, cols, dt)
-    ph, sh = _rows("h", h, n, cols, dt)
-    pe, se = _rows("dh", dh, n, cols, dt)
-    px, sx = _rows("dx", dx, n, cols, dt)
+    kind, wk, shape, cols = _row_types(h, weight if weight is not None else dw)
+    rows, dt = h.numel() // cols, h.dtype
+    pd, sd = _rows("dy", dy, shape, cols, dt)
+    ph, sh = _rows("h", h, shape, cols, dt)
+    pe, se = _rows("dh", dh, shape, cols, dt)
+    px, sx = _rows("dx", dx, shape, cols, dt)
     if work is not None and (not work.is_cuda or not work.is_contiguous()
                              or work.numel() * work.element_size() < dd_rms_norm_grad_work(rows, cols)):
         raise ValueError("work must hold dd_rms_norm_grad_work(rows, cols) bytes on the GPU")
