@@ -15,38 +15,6 @@ namespace dd {
 
 namespace {
 
-constexpr int kBlock = 256;
-
-__device__ float block_sum(float x) {
-    __shared__ float part[kBlock / 64];
-    x = lanes_sum<64>(x);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    float t = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kBlock / 64; w++) t += part[w];
-    __syncthreads();
-    return t;
-}
-__device__ uint32_t block_max(uint32_t x) {
-    __shared__ uint32_t part[kBlock / 64];
-    x = lanes_max<64>(x);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-    __syncthreads();
-    uint32_t t = 0;
-#pragma unroll
-    for (int w = 0; w < kBlock / 64; w++) t = part[w] > t ? part[w] : t;
-    __syncthreads();
-    return t;
-}
-
-__device__ __forceinline__ float weight_at(const RmsArgs &a, int64_t c) {
-    if (!a.weight) return 1.0f;
-    if (a.weight_type == DD_F32) return global(static_cast<const float *>(a.weight))[c];
-    if (a.weight_type == DD_BF16) return (float)global(static_cast<const bf16_t *>(a.weight))[c];
-    return (float)global(static_cast<const f16_t *>(a.weight))[c];
-}
-
 __device__ __forceinline__ float most_of(int32_t out_type) { return out_type == DD_E4M3 ? 448.0f : 127.0f; }
 
 // The largest |y| is taken over its bits: those of a NaN are above infinity's,
@@ -67,6 +35,11 @@ __device__ __forceinline__ uint8_t to_8_bits(float x, int32_t out_type) {
 // (lane l has packs l, l + LANES, ...), so x and residual are read once and
 // a group of 32, 64 or 128 columns is 4, 8 or 16 neighbouring lanes.  Up to 64
 // lanes need no barrier; several waves exchange one number through LDS.
+//
+// Bound: HBM, at the rate of a large copy (4.9 TB/s) or above it; a few rows,
+// the launch.  8,192 x 4,096 bf16 with a residual to e4m3 by 128 columns 48 us
+// (4.9 TB/s), 65,536 x 2,048 bf16 184 us (5.8), 4,099 x 1,237 f32 16.5 us
+// (4.9), 4 x 4,096 4.3 us.
 template <int LANES>
 struct RowSum {
     static constexpr int kWaves = LANES / 64 > 1 ? LANES / 64 : 1;
@@ -257,49 +230,116 @@ __global__ void __launch_bounds__(row_threads(LANES)) k_rms_row(RmsArgs a) {
     }
 }
 
-// One workgroup per row, any width: the row is read once for each of its sums.
+// --- rows of any width --------------------------------------------------------
+// A workgroup of 1,024 threads goes over the row in packs, again for each of
+// its sums (a row of x and residual mostly stays in the L2).
+constexpr int kLoopLanes = 1024;
+
+// columns of the pack at c that the row has: 0 to 8
+__device__ __forceinline__ int have_of(int64_t cols, int64_t c) {
+    const int64_t n = cols - c;
+    return n < 0 ? 0 : n < 8 ? (int)n : 8;
+}
+
 template <class T>
-__global__ void __launch_bounds__(kBlock) k_rms_loop(RmsArgs a) {
+struct LoopRow {
+    const T *x, *r;
+    int64_t cols;
+    __device__ __forceinline__ void sum_at(int64_t c, int have, float (&v)[8]) const {
+        Pack<T, 8> px, pr;
+        px.load(x + c, have);
+        if (r) pr.load(r + c, have);
+        px.to(v);
+        if (r) {
+            float y[8];
+            pr.to(y);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] += y[i];
+        }
+    }
+};
+template <class T, class Args>
+__device__ __forceinline__ void weights_at(const Args &a, int64_t c, int have, float (&w)[8]) {
+    Weights<T> p;
+    p.load(a.weight, a.weight_type, c, have);
+    p.to(a.weight, a.weight_type, w);
+}
+__device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+
+// Wider than 32,768 columns: bound by HBM and what the L2 does not keep.
+// 4,000 x 40,000 bf16 with a residual 289 us (4.4 TB/s of what has to move), to
+// 8 bits by 128 columns 267 us (column by column 641 and 1,463).
+template <class T>
+__global__ void __launch_bounds__(kLoopLanes) k_rms_loop(RmsArgs a) {
+    __shared__ float slots[2][16];
     const int64_t row = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (row >= a.rows) return;
-    const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
-    const T *r = a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr;
-    T *h = a.h ? static_cast<T *>(a.h) + row * a.h_stride : nullptr;
-    auto at = [&](int64_t c) { return (float)global(x)[c] + (r ? (float)global(r)[c] : 0.0f); };
+    const LoopRow<T> in{static_cast<const T *>(a.x) + row * a.x_stride,
+                        a.residual ? static_cast<const T *>(a.residual) + row * a.residual_stride : nullptr, a.cols};
+    const bool narrow = a.out_type == DD_E4M3 || a.out_type == DD_I8;
+    const float most = most_of(a.out_type);
     float q = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kBlock) {
-        const float s = at(c);
-        q = fmaf(s, s, q);
+    for (int64_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kLoopLanes) {
+        float v[8];
+        in.sum_at(c, have_of(a.cols, c), v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) q = fmaf(v[i], v[i], q);
     }
-    const float rstd = 1.0f / sqrtf(block_sum(q) / (float)a.cols + a.eps);
+    const float rstd = 1.0f / sqrtf(RowSum<kLoopLanes>::sum(q, slots[0]) / (float)a.cols + a.eps);
     if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
-    if (a.out_type == DD_E4M3 || a.out_type == DD_I8) {
-        uint8_t *out = static_cast<uint8_t *>(a.out) + row * a.out_stride;
-        const int64_t group = a.group ? a.group : a.cols;
-        const int64_t groups = (a.cols + group - 1) / group;
-        for (int64_t k = 0; k < groups; k++) {
-            const int64_t c0 = k * group, c1 = c0 + group < a.cols ? c0 + group : a.cols;
-            uint32_t m = 0;
-            for (int64_t c = c0 + threadIdx.x; c < c1; c += kBlock) {
-                const uint32_t b = __float_as_uint(at(c) * rstd * weight_at(a, c)) & 0x7fffffffu;
-                m = b > m ? b : m;
-            }
-            const float scale = scale_of(block_max(m), most_of(a.out_type));
-            const float inv = 1.0f / scale;
-            if (threadIdx.x == 0) a.scales[row * groups + k] = scale;
-            for (int64_t c = c0 + threadIdx.x; c < c1; c += kBlock) {
-                const float s = at(c);
-                if (h) global(h)[c] = (T)s;
-                out[c] = to_8_bits(s * rstd * weight_at(a, c) * inv, a.out_type);
-            }
+    uint32_t all = 0;
+    if (narrow && a.group == 0) {
+        for (int64_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kLoopLanes) {
+            float v[8], w[8];
+            in.sum_at(c, have_of(a.cols, c), v);
+            weights_at<T>(a, c, have_of(a.cols, c), w);
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = v[i] * rstd * w[i];
+            const uint32_t m = largest(v);
+            all = m > all ? m : all;
         }
-        return;
+        all = RowSum<kLoopLanes>::max(all, slots[1]);
+        if (threadIdx.x == 0) a.scales[row] = scale_of(all, most);
     }
-    T *out = static_cast<T *>(a.out) + row * a.out_stride;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kBlock) {
-        const float s = at(c);
-        if (h) global(h)[c] = (T)s;
-        global(out)[c] = (T)(s * rstd * weight_at(a, c));
+    const int64_t groups = a.group ? (a.cols + a.group - 1) / a.group : 1;
+    // (every lane goes round as often as the first: groups are exchanged)
+    for (int64_t first = 0; first < a.cols; first += 8 * kLoopLanes) {
+        const int64_t c = first + 8 * threadIdx.x;
+        const int have = have_of(a.cols, c);
+        float v[8], w[8];
+        in.sum_at(c, have, v);
+        weights_at<T>(a, c, have, w);
+        if (a.h) {
+            Pack<T, 8> p;
+            p.from(v);
+            p.store(static_cast<T *>(a.h) + row * a.h_stride + c, have);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] = v[i] * rstd * w[i];
+        if (!narrow) {
+            Pack<T, 8> p;
+            p.from(v);
+            p.store(static_cast<T *>(a.out) + row * a.out_stride + c, have);
+            continue;
+        }
+        uint32_t m = all;
+        if (a.group) {
+            m = largest(v);
+            m = a.group == 128 ? lanes_max<16>(m) : a.group == 64 ? lanes_max<8>(m) : lanes_max<4>(m);
+        }
+        const float scale = scale_of(m, most), inv = 1.0f / scale;
+        if (a.group && c < a.cols && c % a.group == 0) a.scales[row * groups + c / a.group] = scale;
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[i] *= inv;
+        store_pack_8(static_cast<uint8_t *>(a.out) + row * a.out_stride + c, v, have, a.out_type);
     }
 }
 
@@ -307,7 +347,10 @@ __global__ void __launch_bounds__(kBlock) k_rms_loop(RmsArgs a) {
 // goes over rows (b, b + grid, ...) and keeps its sums of dy * xh per column in
 // registers; at the end rows of one workgroup are joined through LDS, and the
 // workgroup writes one partial sum per column, which k_rms_dw_join adds up in
-// order.
+// order (no atomics: the same bits on every call).
+//
+// Bound: HBM.  32,768 x 8,192 bf16 with dh 369 us (5.8 TB/s); 16,384 x 1,024
+// 28.6 us (4.7) and 4.2 for the join, of which a launch alone is 2.8.
 constexpr int grad_threads(int lanes) { return lanes <= 64 ? 1024 : lanes; }
 
 template <class T, int LANES, int NV>
@@ -415,15 +458,12 @@ __global__ void __launch_bounds__(grad_threads(LANES)) k_rms_grad_row(RmsGradArg
     }
 }
 
-__device__ __forceinline__ float weight_at(const RmsGradArgs &a, int64_t c) {
-    if (!a.weight) return 1.0f;
-    if (a.weight_type == DD_F32) return global(static_cast<const float *>(a.weight))[c];
-    if (a.weight_type == DD_BF16) return (float)global(static_cast<const bf16_t *>(a.weight))[c];
-    return (float)global(static_cast<const f16_t *>(a.weight))[c];
-}
-
+// Wider than 16,384 columns: dweight first (dx may overwrite what it reads),
+// then dx, in passes over the rows: dy and h are read three times.  4,000 x
+// 40,000 bf16 with dh 410 us (column by column 940).
 template <class T>
-__global__ void __launch_bounds__(kBlock) k_rms_dx_loop(RmsGradArgs a) {
+__global__ void __launch_bounds__(kLoopLanes) k_rms_dx_loop(RmsGradArgs a) {
+    __shared__ float slot[16];
     const int64_t row = blockIdx.x + (int64_t)blockIdx.y * gridDim.x;
     if (row >= a.rows) return;
     const T *dy = static_cast<const T *>(a.dy) + row * a.dy_stride;
@@ -431,35 +471,77 @@ __global__ void __launch_bounds__(kBlock) k_rms_dx_loop(RmsGradArgs a) {
     const T *dh = a.dh ? static_cast<const T *>(a.dh) + row * a.dh_stride : nullptr;
     T *dx = static_cast<T *>(a.dx) + row * a.dx_stride;
     const float rstd = a.rstd[row];
+    // weight * dy, and xh
+    auto terms = [&](int64_t c, int have, float (&g)[8], float (&x)[8]) {
+        Pack<T, 8> pd, ph;
+        float w[8];
+        pd.load(dy + c, have);
+        ph.load(h + c, have);
+        weights_at<T>(a, c, have, w);
+        pd.to(g);
+        ph.to(x);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            g[i] *= w[i];
+            x[i] *= rstd;
+        }
+    };
     float q = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kBlock)
-        q = fmaf((float)global(dy)[c] * weight_at(a, c), (float)global(h)[c] * rstd, q);
-    const float m = block_sum(q) / (float)a.cols;
-    for (int64_t c = threadIdx.x; c < a.cols; c += kBlock) {
-        const float g = (float)global(dy)[c] * weight_at(a, c) - (float)global(h)[c] * rstd * m;
-        global(dx)[c] = (T)(g * rstd + (dh ? (float)global(dh)[c] : 0.0f));
+    for (int64_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kLoopLanes) {
+        float g[8], x[8];
+        terms(c, have_of(a.cols, c), g, x);
+#pragma unroll
+        for (int i = 0; i < 8; i++) q = fmaf(g[i], x[i], q);
+    }
+    const float m = RowSum<kLoopLanes>::sum(q, slot) / (float)a.cols;
+    for (int64_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kLoopLanes) {
+        const int have = have_of(a.cols, c);
+        float g[8], x[8], y[8] = {};
+        Pack<T, 8> p;
+        if (dh) {
+            p.load(dh + c, have);
+            p.to(y);
+        }
+        terms(c, have, g, x);
+#pragma unroll
+        for (int i = 0; i < 8; i++) y[i] = fmaf(g[i] - x[i] * m, rstd, y[i]);
+        p.from(y);
+        p.store(dx + c, have);
     }
 }
 
-// Partial sums of dweight: workgroup (i, j) has 64 columns and the j-th of
-// gridDim.y runs of rows.
+// Partial sums of dweight: workgroup (i, j) has 256 columns and the j-th of
+// gridDim.y runs of rows, eight rows at a time.
+constexpr int kDwCols = 256, kDwRows = 8;
 template <class T>
-__global__ void __launch_bounds__(kBlock) k_rms_dw_loop(RmsGradArgs a, float *part) {
-    __shared__ float lds[kBlock];
-    const int64_t c = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+__global__ void __launch_bounds__(kDwCols) k_rms_dw_loop(RmsGradArgs a, float *part) {
+    __shared__ float lds[kDwRows][kDwCols];
+    const int x = threadIdx.x % (kDwCols / 8), y = threadIdx.x / (kDwCols / 8);
+    const int64_t c = (int64_t)blockIdx.x * kDwCols + 8 * x;
+    const int have = have_of(a.cols, c);
     const int64_t run = (a.rows + gridDim.y - 1) / gridDim.y;
     const int64_t r0 = blockIdx.y * run, r1 = r0 + run < a.rows ? r0 + run : a.rows;
-    float s = 0.0f;
-    if (c < a.cols)
-        for (int64_t r = r0 + (threadIdx.x >> 6); r < r1; r += kBlock / 64)
-            s = fmaf((float)global(static_cast<const T *>(a.dy))[r * a.dy_stride + c],
-                     (float)global(static_cast<const T *>(a.h))[r * a.h_stride + c] * a.rstd[r], s);
-    lds[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 64 && c < a.cols) {
-        for (int w = 1; w < kBlock / 64; w++) s += lds[threadIdx.x + 64 * w];
-        part[blockIdx.y * a.cols + c] = s;
+    float s[8] = {};
+    for (int64_t r = r0 + y; r < r1; r += kDwRows) {
+        Pack<T, 8> pd, ph;
+        float d[8], v[8];
+        pd.load(static_cast<const T *>(a.dy) + r * a.dy_stride + c, have);
+        ph.load(static_cast<const T *>(a.h) + r * a.h_stride + c, have);
+        const float rstd = a.rstd[r];
+        pd.to(d);
+        ph.to(v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) s[i] = fmaf(d[i], v[i] * rstd, s[i]);
     }
+#pragma unroll
+    for (int i = 0; i < 8; i++) lds[y][8 * x + i] = s[i];
+    __syncthreads();
+    const int64_t mine = (int64_t)blockIdx.x * kDwCols + threadIdx.x;
+    if (mine >= a.cols) return;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kDwRows; i++) t += lds[i][threadIdx.x];
+    part[blockIdx.y * a.cols + mine] = t;
 }
 
 // A workgroup has 32 columns; 32 threads share a column, each with up to 16
@@ -487,7 +569,7 @@ __global__ void __launch_bounds__(1024) k_rms_dw_join(RmsGradArgs a, const float
     else static_cast<f16_t *>(a.dw)[c] = (f16_t)s;
 }
 
-dim3 grid_of_rows(int64_t rows) {
+dim3 grid_of_rows(int64_t rows) {       // (a launch takes fewer than 2^32 threads a dimension)
     const int64_t x = rows < (1 << 20) ? rows : (1 << 20);
     return dim3((unsigned)x, (unsigned)((rows + x - 1) / x));
 }
@@ -504,8 +586,9 @@ int dw_runs(int64_t rows) {
 // 4,096 to 8 bits 4.8 with 256 lanes x 2 (128 x 4: 4.2, 64 x 8: 3.6, 1,024 x
 // 1: 2.7); 16,384 x 1,024 5.0 with 64 x 2 (256 x 1: 4.3); 65,536 x 2,048
 // 5.8 with 256 x 1 (64 x 4: 5.7); 65,536 x 128 to 8 bits 3.6 with 16 x 1
-// (64 x 1: 1.5); 65,536 x 64 3.5 with 8 x 1 (16 x 1: 2.7).  Few rows take the same: 4 to 512 rows of 4,096 are as fast
-// with any of these shapes, the launch bounds them.
+// (64 x 1: 1.5); 65,536 x 64 3.5 with 8 x 1 (16 x 1: 2.7).  Few rows take the
+// same: 4 to 512 rows of 4,096 are as fast with any of these shapes, the launch
+// bounds them.
 struct Shape {
     int lanes, packs;      // 0: k_rms_loop
 };
@@ -541,7 +624,7 @@ void rms_norm(const RmsArgs &a, hipStream_t s) {
     if (p.lanes == 512 && p.packs == 2) return run_rows<T, 512, 2>(a, s);
     if (p.lanes == 1024 && p.packs == 2) return run_rows<T, 1024, 2>(a, s);
     if (p.lanes == 1024 && p.packs == 4) return run_rows<T, 1024, 4>(a, s);
-    k_rms_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
+    k_rms_loop<T><<<grid_of_rows(a.rows), kLoopLanes, 0, s>>>(a);
 }
 
 // The gradient holds three times as much per column: four packs do not fit.
@@ -572,11 +655,11 @@ void rms_grad(const RmsGradArgs &a, float *work, hipStream_t s) {
     const int n = grad_parts(a.rows, a.cols, sizeof(T));
     auto join = [&] { k_rms_dw_join<<<(unsigned)((a.cols + 31) / 32), 1024, 0, s>>>(a, work, n); };
     if (!p.lanes) {
-        if (a.dw) {       // first: dx may overwrite what it reads
-            k_rms_dw_loop<T><<<dim3((unsigned)((a.cols + 63) / 64), n), kBlock, 0, s>>>(a, work);
+        if (a.dw) {
+            k_rms_dw_loop<T><<<dim3((unsigned)((a.cols + kDwCols - 1) / kDwCols), n), kDwCols, 0, s>>>(a, work);
             join();
         }
-        if (a.rows > 0) k_rms_dx_loop<T><<<grid_of_rows(a.rows), kBlock, 0, s>>>(a);
+        if (a.rows > 0) k_rms_dx_loop<T><<<grid_of_rows(a.rows), kLoopLanes, 0, s>>>(a);
         return;
     }
     if (p.lanes == 8) run_grad<T, 8, 1>(a, work, n, s);
