@@ -23,7 +23,6 @@ namespace {
 
 constexpr int kBlock = 256;
 
-
 // One thread per chunk finds its tensor (the last that starts at or before it).
 __global__ void __launch_bounds__(kBlock) k_tensor_chunks(const TensorPlace *p, int count, TensorChunk *ck, int n_chunks,
                                                           uint32_t *ticket) {
@@ -177,6 +176,7 @@ __device__ __forceinline__ void part_clip_to(const G *g, const TensorChunk &d, i
 __global__ void __launch_bounds__(kBlock) k_grad_clip(const TensorChunk *src, const TensorChunk *dst, int64_t n_parts,
                                                       const float *stats) {
     const float f = stats[1];
+    if (src == dst && f == 1.0f) return;     // in place, within the bound: nothing changes
     for (int64_t b = blockIdx.x; b < n_parts; b += gridDim.x) {
         const TensorChunk a = src[b / kPartsOf], d = dst[b / kPartsOf];
         const int o = (int)(b % kPartsOf) * kPartLen, n = a.n - o < kPartLen ? a.n - o : kPartLen;

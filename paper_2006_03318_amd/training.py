@@ -41,6 +41,7 @@ class _AddRmsNorm(torch.autograd.Function):
         return out if residual is None else (out, h)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dy, dh=None):
         h, weight, rstd = ctx.saved_tensors
         if dy is None:
@@ -95,7 +96,9 @@ class Adam:
             if low:
                 t["master"] = self.masters[-1]
             tensors.append(t)
-        self._grads = [(p, p.grad) for p in self.params]
+        # the handle works on these addresses: they are kept, and looked at in every step
+        self._tensors = tensors
+        self._places = [(p, p.grad, p.data_ptr()) for p in self.params]
         self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
         self.stats = torch.zeros(3, device=dev)
         self._handle = B.dd_tensors_load(tensors, _stream())
@@ -106,9 +109,10 @@ class Adam:
 
     def step(self, inv_scale: Optional[torch.Tensor] = None):
         """inv_scale: float32 [1] on the GPU, 1 / the scale of the loss."""
-        for p, g in self._grads:
-            if p.grad is not g:
-                raise RuntimeError("a gradient was replaced: zero_grad() of this optimizer keeps them in place")
+        for p, g, at in self._places:
+            if p.grad is not g or p.data_ptr() != at:
+                raise RuntimeError("a parameter or its gradient was replaced: both stay where they were when this "
+                                   "optimizer was made (its zero_grad() keeps gradients in place)")
         s = _stream()
         B.dd_grad_norm(self._handle, self.stats, max_norm=self.max_norm, d_inv_scale=inv_scale, stream=s)
         B.dd_adam_step(self._handle, self.steps, self.stats, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1],

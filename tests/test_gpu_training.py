@@ -68,6 +68,16 @@ def test_add_rms_norm_shapes_and_unused_outputs():
     _check_norm(x, None, None, y2, None, None, "float32")
 
 
+def test_second_derivatives_are_refused():
+    import torch
+    from paper_2006_03318_amd.training import add_rms_norm
+    require_gpu()
+    x = torch.randn(4, 32, device="cuda", requires_grad=True)
+    g, = torch.autograd.grad(add_rms_norm(x).square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 @pytest.mark.parametrize("kind", ["float32", "bfloat16", "float16"])
 def test_adam(kind):
     import torch
@@ -90,7 +100,12 @@ def test_adam(kind):
             a, b, c, ew, em, ev = _adam64(_f64(g), w, m, v, step, f, p.dim() >= 2, 0.02, 0.8, 0.95, 1e-6, 0.1, True)
             assert np.all(np.abs(_f64(w1) - a) <= ew) and np.all(np.abs(_f64(m1) - b) <= em) and np.all(np.abs(_f64(v1) - c) <= ev)
             assert torch.equal(p.detach(), w1.to(t))
+    kept = params[0].grad
     params[0].grad = torch.zeros_like(params[0])
+    with pytest.raises(RuntimeError, match="replaced"):
+        opt.step()
+    params[0].grad = kept
+    params[1].data = params[1].data.clone()
     with pytest.raises(RuntimeError, match="replaced"):
         opt.step()
     opt.close()

@@ -158,6 +158,18 @@ def test_clip(name, src, dst):
             assert torch.equal(g, x[guard:guard + g.numel()])
 
 
+def test_clip_in_place_within_the_bound():
+    """A factor of one leaves every bit, a factor just below one does not."""
+    import torch
+    require_gpu()
+    g = torch.from_numpy(np.random.default_rng(3).standard_normal(5000)).float().cuda()
+    before = g.clone()
+    for max_norm, same in ((1e6, True), (0.0, True), (0.999 * float(g.double().norm()), False)):
+        li, stats = _norm([g], max_norm=max_norm)
+        B.dd_grad_clip(li.h, li.h, stats)
+        assert torch.equal(g, before) == same
+
+
 def test_clip_refuses_other_sizes():
     import torch
     require_gpu()
