@@ -39,6 +39,7 @@ struct TensorWork {
 
 struct dd_tensors {
     int32_t n_chunks = 0;
+    int64_t total = 0;            // elements
     bool params = false;          // weights and moments are there (dd_adam_step)
     hipStream_t stream = nullptr;
     std::vector<int64_t> sizes;

@@ -88,6 +88,7 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
     for (int32_t i = 0; i < count; i++) chunks += (t[i].n + dd::kChunkLen - 1) / dd::kChunkLen;
     if (chunks >= (int64_t(1) << 31)) return fail(DD_EINVAL, "too many elements for one list");
     x->n_chunks = (int32_t)chunks;
+    x->total = total;
     x->params = without == 0;
     std::vector<dd::TensorPlace> h;
     h.reserve((size_t)count);

@@ -54,6 +54,25 @@ static_assert(kChunkLen == kAhead * kTurn, "a chunk is whole turns of a workgrou
 constexpr int kPartLen = 2048, kPartsOf = kChunkLen / kPartLen;
 static_assert(kPartLen == kTurn, "clipping: a pack for each thread");
 
+// Adam: 1, 2 or 4 workgroups share a chunk (`split` is the logarithm), each
+// taking every so many-th part of it: four, a part each, but of many chunks
+// (past kSmallShares) no more than the mean chunk fills, as workgroups that
+// find no part only cost (1,000 tensors of 3,000 elements or fewer: 9.0 us with
+// one to a chunk, 12.6 with four; 30 tensors of 5,000 or fewer 6.3 and 5.3).
+// Clipping always takes four: with a loop over parts it ran 5 % longer on large
+// lists.
+//
+// Up to kSmallShares the tickets of k_adam_small (12 ns each) cost less than a
+// launch more: 50 shares 5.4 us against 7.4, 300 shares 6.5 against 7.4, 480
+// shares 8.5 against 7.3.
+constexpr int64_t kSmallShares = 320;
+int split_of(const dd_tensors *t) {
+    const int64_t mean = t->total / (t->n_chunks ? t->n_chunks : 1);
+    int split = 2;
+    while (split > 0 && (int64_t)t->n_chunks << split > kSmallShares && mean <= kPartLen << (split - 1)) split--;
+    return split;
+}
+
 // Squares in 64 bits: one of an f32 (or bf16) gradient leaves the 32-bit range
 // above 1.8e19 and below 1e-19, and a sum over 10^9 elements keeps its digits.
 __device__ __forceinline__ double squares(const float (&x)[kWide], double s) {
@@ -283,14 +302,14 @@ __device__ __forceinline__ void part_adam(const TensorChunk &k, const AdamFactor
     else part_adam<G, f16_t>(k, a, o, n);
 }
 
-__device__ __forceinline__ void adam_part(const TensorChunk *ck, int64_t b, const AdamFactors &a) {
-    const TensorChunk k = ck[b / kPartsOf];
-    const int o = (int)(b % kPartsOf) * kPartLen;
-    if (o >= k.n) return;
-    const int n = k.n < o + kPartLen ? k.n : o + kPartLen;
-    if (k.grad_type == DD_F32) part_adam<float>(k, a, o, n);
-    else if (k.grad_type == DD_BF16) part_adam<bf16_t>(k, a, o, n);
-    else part_adam<f16_t>(k, a, o, n);
+__device__ __forceinline__ void adam_share(const TensorChunk *ck, int64_t b, int split, const AdamFactors &a) {
+    const TensorChunk k = ck[b >> split];
+    for (int o = (int)(b & ((1 << split) - 1)) * kPartLen; o < k.n; o += kPartLen << split) {
+        const int n = k.n < o + kPartLen ? k.n : o + kPartLen;
+        if (k.grad_type == DD_F32) part_adam<float>(k, a, o, n);
+        else if (k.grad_type == DD_BF16) part_adam<bf16_t>(k, a, o, n);
+        else part_adam<f16_t>(k, a, o, n);
+    }
 }
 
 // The factors of a step, once for all workgroups, and the step's number.
@@ -300,22 +319,23 @@ __global__ void k_adam_begin(int64_t *step, const float *stats, AdamParams p, Ad
     if (!a.skip) a = adam_factors(p, *step += 1, stats);
     *out = a;
 }
-__global__ void __launch_bounds__(kBlock) k_adam(const TensorChunk *ck, int64_t n_parts, const AdamFactors *factors) {
+__global__ void __launch_bounds__(kBlock) k_adam(const TensorChunk *ck, int64_t n_shares, int split,
+                                                 const AdamFactors *factors) {
     const AdamFactors a = *factors;
     if (a.skip) return;
-    for (int64_t b = blockIdx.x; b < n_parts; b += gridDim.x) adam_part(ck, b, a);
+    for (int64_t b = blockIdx.x; b < n_shares; b += gridDim.x) adam_share(ck, b, split, a);
 }
 
 // Small lists: one launch, in which every workgroup finds the factors itself,
 // and the one that finishes last counts the step.  By then all others have
 // read its number: each takes its ticket after it has used the number, and
 // only the last ticket is followed by the write.
-__global__ void __launch_bounds__(kBlock) k_adam_small(const TensorChunk *ck, int64_t n_parts, int64_t *step, const float *stats,
-                                                       AdamParams p, uint32_t *ticket) {
+__global__ void __launch_bounds__(kBlock) k_adam_small(const TensorChunk *ck, int64_t n_shares, int split, int64_t *step,
+                                                       const float *stats, AdamParams p, uint32_t *ticket) {
     if (stats && stats[2] != 0.0f) return;
     const int64_t t = __hip_atomic_load(step, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
     const AdamFactors a = adam_factors(p, t, stats);
-    if (blockIdx.x < n_parts) adam_part(ck, blockIdx.x, a);
+    if (blockIdx.x < n_shares) adam_share(ck, blockIdx.x, split, a);
     __syncthreads();
     if (threadIdx.x == 0 && last_ticket(ticket)) {
         *step = t;
@@ -323,7 +343,7 @@ __global__ void __launch_bounds__(kBlock) k_adam_small(const TensorChunk *ck, in
     }
 }
 
-constexpr int64_t kMaxGrid = 1 << 22;     // workgroups of a launch; parts beyond go round
+constexpr int64_t kMaxGrid = 1 << 22;     // workgroups of a launch; shares beyond go round
 
 // Workgroups of the norm: four chunks each, at least 256 (one per compute
 // unit), at most kNormParts: each ticket is 12 ns, one after the other (1,000
@@ -332,12 +352,7 @@ int norm_grid(int n_chunks) {
     const int g = n_chunks / 4 < 256 ? 256 : n_chunks / 4 < kNormParts ? n_chunks / 4 : kNormParts;
     return n_chunks < 1 ? 1 : n_chunks < g ? n_chunks : g;
 }
-// Up to here the tickets of k_adam_small (12 ns each) cost less than a launch
-// more: 1 part 4.6 us against 7.2, 320 parts 6.7 against 7.1, 480 parts 8.5
-// against 7.3.
-constexpr int64_t kSmallParts = 320;
-
-unsigned grid_of(int64_t parts) { return (unsigned)(parts < kMaxGrid ? parts : kMaxGrid); }
+unsigned grid_of(int64_t shares) { return (unsigned)(shares < kMaxGrid ? shares : kMaxGrid); }
 
 }  // namespace
 
@@ -360,12 +375,13 @@ hipError_t launch_grad_clip(const dd_tensors *src, const dd_tensors *dst, const 
 }
 
 hipError_t launch_adam(const dd_tensors *t, int64_t *step, const float *stats, const AdamParams &p, hipStream_t s) {
-    const int64_t parts = (int64_t)t->n_chunks * kPartsOf;
-    if (parts <= kSmallParts) {
-        k_adam_small<<<parts < 1 ? 1 : (unsigned)parts, kBlock, 0, s>>>(t->chunks, parts, step, stats, p, &t->work->ticket);
+    const int split = split_of(t);
+    const int64_t shares = (int64_t)t->n_chunks << split;
+    if (shares <= kSmallShares) {
+        k_adam_small<<<shares < 1 ? 1 : (unsigned)shares, kBlock, 0, s>>>(t->chunks, shares, split, step, stats, p, &t->work->ticket);
     } else {
         k_adam_begin<<<1, 1, 0, s>>>(step, stats, p, &t->work->factors);
-        k_adam<<<grid_of(parts), kBlock, 0, s>>>(t->chunks, parts, &t->work->factors);
+        k_adam<<<grid_of(shares), kBlock, 0, s>>>(t->chunks, shares, split, &t->work->factors);
     }
     return hipGetLastError();
 }
