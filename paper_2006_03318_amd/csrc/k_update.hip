@@ -120,7 +120,7 @@ __device__ double block_sum(double x) {
 __device__ void write_stats(double s, double max_norm, const float *inv_scale, float *stats) {
     const double u = inv_scale ? (double)*inv_scale : 1.0;
     const double norm = sqrt(s) * u;
-    const bool finite = isfinite(s);
+    const bool finite = isfinite(norm);
     double f = u;
     if (max_norm > 0.0 && norm > max_norm) f = u * (max_norm / norm);
     stats[0] = (float)norm;

@@ -134,6 +134,16 @@ def test_not_finite_is_skipped(kind, bad):
         assert int(step) == 4 and all(torch.equal(a, b) for a, b in zip(before, after))
 
 
+@pytest.mark.parametrize("scale", [math.inf, math.nan])
+def test_a_scale_that_is_not_finite_is_skipped(scale):
+    import torch
+    require_gpu()
+    _, stats = _norm([torch.ones(10, device="cuda")], max_norm=1.0, inv_scale=scale)
+    assert _f64(stats)[1:].tolist() == [0.0, 1.0]
+    _, stats = _norm([torch.ones(10, device="cuda")], max_norm=1.0, inv_scale=0.0)
+    assert _f64(stats).tolist() == [0.0, 0.0, 0.0]
+
+
 @pytest.mark.parametrize("name", ["none", "empty", "holes", "edges", "vectors", "many", "ragged"])
 @pytest.mark.parametrize("src,dst", [("float32", "float32"), ("bfloat16", "float32"), ("float16", "bfloat16"),
                                      ("float32", "float16"), ("bfloat16", "bfloat16")])
