@@ -7,7 +7,7 @@
 // little: they are bound by memory, small lists by the launch.
 //
 // The norm only reads: 1,024 workgroups go over all chunks, four loads of 16
-// bytes or more under way in every lane (302 M bf16 gradients 5.7 TB/s; a
+// bytes or more under way in every lane (302 M bf16 gradients 5.9 TB/s; a
 // workgroup per chunk 4.2).  Clipping and Adam write as much as they read, and
 // go fastest with a workgroup for each kPartLen elements that does nothing else
 // (Adam on the same list 5.3 TB/s, 5.1 with 8,192 elements to a workgroup, 5.0
