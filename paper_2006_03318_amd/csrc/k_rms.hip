@@ -91,6 +91,18 @@ __device__ __forceinline__ void store_pack_8(uint8_t *p, const float (&x)[8], in
         for (int i = 0; i < have; i++) global(p)[i] = (uint8_t)(b[i >> 2] >> (8 * (i & 3)));
     }
 }
+
+// bits of the largest magnitude
+__device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+        m = b > m ? b : m;
+    }
+    return m;
+}
+
 // eight weights, held as they were loaded
 template <class T>
 struct Weights {
@@ -195,14 +207,7 @@ __global__ void __launch_bounds__(row_threads(LANES)) k_rms_row(RmsArgs a) {
         }
         uint32_t m[NV];
 #pragma unroll
-        for (int k = 0; k < NV; k++) {
-            m[k] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t b = __float_as_uint(v[k][i]) & 0x7fffffffu;
-                m[k] = b > m[k] ? b : m[k];
-            }
-        }
+        for (int k = 0; k < NV; k++) m[k] = largest(v[k]);
         if (a.group == 0) {
 #pragma unroll
             for (int k = 1; k < NV; k++) m[0] = m[k] > m[0] ? m[k] : m[0];
@@ -264,16 +269,6 @@ __device__ __forceinline__ void weights_at(const Args &a, int64_t c, int have, f
     p.load(a.weight, a.weight_type, c, have);
     p.to(a.weight, a.weight_type, w);
 }
-__device__ __forceinline__ uint32_t largest(const float (&v)[8]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
-        m = b > m ? b : m;
-    }
-    return m;
-}
-
 // Wider than 32,768 columns: bound by HBM and what the L2 does not keep.
 // 4,000 x 40,000 bf16 with a residual 289 us (4.4 TB/s of what has to move), to
 // 8 bits by 128 columns 267 us (column by column 641 and 1,463).
