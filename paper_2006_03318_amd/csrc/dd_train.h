@@ -25,7 +25,7 @@ constexpr int kNormParts = 1024;  // workgroups of the norm, at most
 struct AdamFactors {
     float f;                      // factor of the gradients
     float b1, c1, b2, c2;         // beta1, 1 - beta1, beta2, 1 - beta2
-    float l2, keep;               // weight decay: added weight * l2, kept share of the weight
+    float l2, shrink;             // weight decay: weight * l2 added to the gradient, weight * shrink taken off
     float lr, rv, eps;            // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
     int32_t skip;                 // nothing is applied
 };

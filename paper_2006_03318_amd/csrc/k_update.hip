@@ -223,7 +223,7 @@ __device__ AdamFactors adam_factors(const AdamParams &p, int64_t t, const float 
     a.b2 = (float)p.beta2;
     a.c2 = (float)(1.0 - p.beta2);
     a.l2 = p.decoupled ? 0.0f : (float)p.weight_decay;
-    a.keep = p.decoupled ? (float)(1.0 - p.lr * p.weight_decay) : 1.0f;
+    a.shrink = p.decoupled ? (float)(p.lr * p.weight_decay) : 0.0f;
     a.lr = (float)(p.lr / (1.0 - power(p.beta1, t)));
     a.rv = (float)(1.0 / sqrt(1.0 - power(p.beta2, t)));
     a.eps = (float)p.eps;
@@ -231,13 +231,18 @@ __device__ AdamFactors adam_factors(const AdamParams &p, int64_t t, const float 
     return a;
 }
 
+// The weight changes by one number, decay and update together, so what is small
+// beside the weight is rounded once and not away on its own; and the decay is
+// held as lr * weight_decay, as 1 - lr * weight_decay has 2^-24 for a grid (at
+// 1e-7 that would be 19 % off, every step).
 __device__ __forceinline__ void adam_one(const AdamFactors &a, bool decay, float g, float &w, float &m, float &v) {
     g *= a.f;
     if (decay) g = fmaf(a.l2, w, g);
     m = fmaf(a.b1, m, a.c1 * g);
     v = fmaf(a.b2, v, a.c2 * (g * g));
-    if (decay) w *= a.keep;
-    w -= a.lr * (m / fmaf(sqrtf(v), a.rv, a.eps));
+    float change = a.lr * (m / fmaf(sqrtf(v), a.rv, a.eps));
+    if (decay) change = fmaf(a.shrink, w, change);
+    w -= change;
 }
 
 // Four elements per thread and load, two loads of each array at a time.
