@@ -239,7 +239,7 @@ __device__ __forceinline__ void adam_one(const AdamFactors &a, bool decay, float
     g *= a.f;
     if (decay) g = fmaf(a.l2, w, g);
     m = fmaf(a.b1, m, a.c1 * g);
-    v = fmaf(a.b2, v, a.c2 * (g * g));
+    v = fmaf(a.b2, v, (a.c2 * g) * g);      // (g * g alone leaves the range from 1.8e19 on)
     float change = a.lr * (m / fmaf(sqrtf(v), a.rv, a.eps));
     if (decay) change = fmaf(a.shrink, w, change);
     w -= change;

@@ -38,3 +38,19 @@ def test_small_weight_decay(n, kind, decay):
         drift += float(np.mean(_f64(w) - w1))
         want += decay * float(np.mean(old[0]))
     assert abs(drift) <= 4 * 6 * 2.0 ** -23 / np.sqrt(12 * n) + 2.0 ** -22 * want
+
+
+@pytest.mark.parametrize("n", [1000, 1 << 20])
+@pytest.mark.parametrize("value,beta2", [(1e20, 0.999), (-5e20, 0.999), (1e20, 0.99), (3e18, 0.5)])
+def test_second_moment_of_large_gradients(n, value, beta2):
+    """(1 - beta2) g^2 within the range of 32 bits, though g^2 is not."""
+    import torch
+    require_gpu()
+    g = torch.full((n,), value, device="cuda")
+    w, m, v = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    li = List([dict(grad=g, param=w, m=m, v=v)])
+    B.dd_adam_step(li.h, torch.zeros(1, dtype=torch.int64, device="cuda"), lr=0.25, beta2=beta2)
+    one = np.ones(1)
+    w1, m1, v1, ew, em, ev = _adam64(_f64(g)[:1], one, 0 * one, 0 * one, 1, 1.0, True, 0.25, 0.9, beta2, 1e-8, 0.0, True)
+    assert np.all(np.abs(_f64(v) - v1) <= ev) and np.all(np.abs(_f64(m) - m1) <= em)
+    assert np.all(np.abs(_f64(w) - w1) <= ew)
