@@ -227,6 +227,7 @@ __device__ AdamFactors adam_factors(const AdamParams &p, int64_t t, const float 
     a.lr = (float)(p.lr / (1.0 - power(p.beta1, t)));
     a.rv = (float)(1.0 / sqrt(1.0 - power(p.beta2, t)));
     a.eps = (float)p.eps;
+    if (p.eps > 0.0 && a.eps == 0.0f) a.eps = 0x1p-149f;      // (0 / 0 where both moments are 0)
     a.skip = 0;
     return a;
 }

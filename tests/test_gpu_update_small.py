@@ -54,3 +54,16 @@ def test_second_moment_of_large_gradients(n, value, beta2):
     w1, m1, v1, ew, em, ev = _adam64(_f64(g)[:1], one, 0 * one, 0 * one, 1, 1.0, True, 0.25, 0.9, beta2, 1e-8, 0.0, True)
     assert np.all(np.abs(_f64(v) - v1) <= ev) and np.all(np.abs(_f64(m) - m1) <= em)
     assert np.all(np.abs(_f64(w) - w1) <= ew)
+
+
+@pytest.mark.parametrize("n", [1000, 1 << 20])
+@pytest.mark.parametrize("eps", [1e-42, 1e-60, 1e-300])
+def test_eps_below_the_range_of_32_bits(n, eps):
+    """Weights without a gradient stay where they are for any eps above 0."""
+    import torch
+    require_gpu()
+    w = torch.linspace(-2, 2, n, device="cuda")
+    g, m, v, before = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), w.clone()
+    li = List([dict(grad=g, param=w, m=m, v=v)])
+    B.dd_adam_step(li.h, torch.zeros(1, dtype=torch.int64, device="cuda"), lr=0.1, eps=eps)
+    assert torch.equal(w, before)
