@@ -48,8 +48,12 @@ class _AddRmsNorm(torch.autograd.Function):
             return dh, dh if ctx.needs_input_grad[1] else None, None, None
         dy = _rows(dy)
         dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
-        dw = torch.empty_like(weight) if weight is not None and ctx.needs_input_grad[2] else None
-        B.dd_rms_norm_grad(dy, h, weight, rstd, dx, dw, dh=None if dh is None else _rows(dh), stream=_stream())
+        dw = work = None
+        if weight is not None and ctx.needs_input_grad[2]:
+            dw = torch.empty_like(weight)
+            # (torch's memory: in a captured graph it stays the graph's)
+            work = torch.empty(B.dd_rms_norm_grad_work(rstd.numel(), h.shape[-1]), dtype=torch.uint8, device=h.device)
+        B.dd_rms_norm_grad(dy, h, weight, rstd, dx, dw, dh=None if dh is None else _rows(dh), work=work, stream=_stream())
         return dx, dx if ctx.needs_input_grad[1] else None, dw, None
 
 
