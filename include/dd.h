@@ -458,8 +458,9 @@ dd_status dd_rms_norm(const dd_rms_norm_args *a, void *stream);
  * dx may be dy, dh or h themselves (the same stride); otherwise outputs must
  * not overlap inputs.
  *   work   device memory of dd_rms_norm_grad_work(rows, cols) bytes, aligned to
- *          16, which the call overwrites (for calls under graph capture, say),
- *          or NULL: the library takes it from its cache.
+ *          16, which the call overwrites, or NULL: the library takes it from its
+ *          cache for the time of the call.  A call with dw that is captured into
+ *          a graph needs it (DD_EINVAL): the replays write there too.
  */
 typedef struct {
     int64_t rows, cols;

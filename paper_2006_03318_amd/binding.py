@@ -429,7 +429,7 @@ def dd_rms_norm(x, residual, weight, eps, out, h=None, rstd=None, scales=None, g
 def dd_rms_norm_grad(dy, h, weight, rstd, dx, dw=None, dh=None, work=None, stream=None):
     """dx and dw from the gradient dy of the norm's output; dh: what reaches h
     on its other ways.  work: uint8 of dd_rms_norm_grad_work(rows, cols), or
-    None (from the library's cache)."""
+    None (from the library's cache; not under graph capture)."""
     kind, wk, shape, cols = _row_types(h, weight if weight is not None else dw)
     rows, dt = h.numel() // cols, h.dtype
     pd, sd = _rows("dy", dy, shape, cols, dt)

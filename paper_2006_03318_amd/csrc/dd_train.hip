@@ -281,6 +281,11 @@ dd_status dd_rms_norm_grad(const dd_rms_norm_grad_args *a, void *stream) {
         void *work = a->work, *taken = nullptr;
         hipError_t e = hipSuccess;
         if (a->dw && !work) {
+            // (the block goes back to the cache, a graph would keep writing to it)
+            hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+            e = hipStreamIsCapturing(s, &capture);
+            if (e != hipSuccess) return hip_fail(e, "alloc partial sums");
+            if (capture != hipStreamCaptureStatusNone) return fail(DD_EINVAL, "a captured gradient needs work from the caller");
             e = dd::dalloc(&taken, dd::rms_grad_work(a->rows, a->cols), s);
             if (e != hipSuccess) return hip_fail(e, "alloc partial sums");
             work = taken;

@@ -47,3 +47,28 @@ def test_norm_and_gradient(rows, cols):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
         B.dd_release_cache()
+
+
+def test_gradient_without_working_memory_is_not_captured():
+    import torch
+    require_gpu()
+    rows, cols = 5000, 64
+    dy, h, dx = (torch.ones(rows, cols, device="cuda") for _ in range(3))
+    rstd, dw = torch.ones(rows, device="cuda"), torch.empty(cols, device="cuda")
+    work = torch.empty(B.dd_rms_norm_grad_work(rows, cols), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    B.dd_rms_norm_grad(dy, h, None, rstd, dx, dw, stream=side)       # the cache has a block for the stream
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(B.DDError) as e:
+            B.dd_rms_norm_grad(dy, h, None, rstd, dx, dw, stream=side)
+        assert e.value.code == B.DD_EINVAL and "work" in str(e.value)
+        B.dd_rms_norm_grad(dy, h, None, rstd, dx, stream=side)       # without dw there is nothing to keep
+        B.dd_rms_norm_grad(dy, h, None, rstd, dx, dw, work=work, stream=side)
+    dw.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert bool((dw == float(rows)).all())
