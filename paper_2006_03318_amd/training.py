@@ -71,7 +71,10 @@ class Adam:
 
     Gradients live in one buffer per type that stays where it is; parameters of
     16 bits get f32 masters.  Weight decay spares parameters of fewer than two
-    dimensions.  `stats` holds the last step's gradient norm, factor and
+    dimensions.  What else writes a parameter in place (a checkpoint that is
+    loaded, a broadcast) is seen at the next step and goes on from there; after
+    writes that torch does not count (through `.data`, by other libraries) call
+    `read_weights()`.  `stats` holds the last step's gradient norm, factor and
     whether it was skipped, `steps` the steps taken, both on the GPU."""
 
     def __init__(self, params: Iterable[torch.nn.Parameter], lr=1e-3, betas=(0.9, 0.999), eps=1e-8,
@@ -103,6 +106,7 @@ class Adam:
         # the handle works on these addresses: they are kept, and looked at in every step
         self._tensors = tensors
         self._places = [(p, p.grad, p.data_ptr()) for p in self.params]
+        self._versions = [p._version for p in self.params]
         self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
         self.stats = torch.zeros(3, device=dev)
         self._handle = B.dd_tensors_load(tensors, _stream())
@@ -111,12 +115,25 @@ class Adam:
         for b in self.buffers.values():
             b.zero_()
 
+    @torch.no_grad()
+    def read_weights(self, which: Optional[Iterable[int]] = None):
+        """Takes the parameters as they are (all, or those of these numbers): a
+        master whose rounding is no longer its weight becomes the weight."""
+        for i in range(len(self.params)) if which is None else which:
+            p, w = self.params[i], self.masters[i]
+            if p.dtype != w.dtype:
+                w.copy_(torch.where(w.to(p.dtype) == p, w, p.to(w.dtype)))
+            self._versions[i] = p._version
+
     def step(self, inv_scale: Optional[torch.Tensor] = None):
         """inv_scale: float32 [1] on the GPU, 1 / the scale of the loss."""
         for p, g, at in self._places:
             if p.grad is not g or p.data_ptr() != at:
                 raise RuntimeError("a parameter or its gradient was replaced: both stay where they were when this "
                                    "optimizer was made (its zero_grad() keeps gradients in place)")
+        written = [i for i, (p, seen) in enumerate(zip(self.params, self._versions)) if p._version != seen]
+        if written:
+            self.read_weights(written)
         s = _stream()
         B.dd_grad_norm(self._handle, self.stats, max_norm=self.max_norm, d_inv_scale=inv_scale, stream=s)
         B.dd_adam_step(self._handle, self.steps, self.stats, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1],
