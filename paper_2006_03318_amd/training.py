@@ -138,6 +138,8 @@ class Adam:
         B.dd_grad_norm(self._handle, self.stats, max_norm=self.max_norm, d_inv_scale=inv_scale, stream=s)
         B.dd_adam_step(self._handle, self.steps, self.stats, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1],
                        eps=self.eps, weight_decay=self.weight_decay, decoupled=self.decoupled, stream=s)
+        torch.autograd.graph.increment_version(self.params)     # (graphs that kept the old weights are refused)
+        self._versions = [p._version for p in self.params]
 
     def close(self):
         h, self._handle = self._handle, None

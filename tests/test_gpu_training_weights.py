@@ -38,3 +38,18 @@ def test_a_loaded_checkpoint_stays(kind):
     opt.step()
     assert all(bool((p == 100.0).all()) for p in model.parameters())
     opt.close()
+
+
+def test_a_graph_from_before_the_step_is_refused():
+    import torch
+    from paper_2006_03318_amd.training import Adam, add_rms_norm
+    require_gpu()
+    w = torch.nn.Parameter(torch.ones(64, dtype=torch.bfloat16, device="cuda"))
+    x = torch.randn(10, 64, device="cuda").to(torch.bfloat16).requires_grad_()
+    opt = Adam([w], lr=0.1)
+    loss = add_rms_norm(x, None, w).float().square().sum()
+    loss.backward(retain_graph=True)
+    opt.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    opt.close()

@@ -77,3 +77,22 @@ def test_weights_written_between_steps_reach_the_masters(calls, kind):
     model.b.data.copy_(torch.full((30,), 5.0))  # behind torch's back: said, not seen
     opt.read_weights()
     assert torch.equal(opt.masters[1], torch.full((30,), 5.0)) and torch.equal(opt.masters[2], model.c.float())
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+def test_a_step_counts_as_a_write(calls, kind):
+    """A backward pass through a graph kept from before the step is refused, as
+    with any other optimizer: its weights are gone."""
+    p, = _params(kind, 40)
+    opt = training.Adam([p])
+    x = torch.ones(40, dtype=kind, requires_grad=True)
+    loss = (p * x).sum()
+    loss.backward(retain_graph=True)
+    loss.backward(retain_graph=True)
+    opt.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    fine = opt.masters[0].clone()
+    (p * x).sum().backward()
+    opt.step()                                  # its own writes are no one else's
+    assert torch.equal(opt.masters[0], fine)
