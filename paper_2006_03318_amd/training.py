@@ -82,6 +82,8 @@ class Adam:
         self.params = [p for p in params if p.requires_grad]
         if not self.params:
             raise ValueError("no parameters to train")
+        if len({id(p) for p in self.params}) != len(self.params):
+            raise ValueError("a parameter is given twice")
         self.lr, self.betas, self.eps = lr, betas, eps
         self.weight_decay, self.decoupled, self.max_norm = weight_decay, decoupled, max_norm
         dev = self.params[0].device

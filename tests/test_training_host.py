@@ -96,3 +96,13 @@ def test_a_step_counts_as_a_write(calls, kind):
     (p * x).sum().backward()
     opt.step()                                  # its own writes are no one else's
     assert torch.equal(opt.masters[0], fine)
+
+
+def test_a_parameter_given_twice_is_refused(calls):
+    """Two tensors of the list would update it, one from a gradient that no one
+    writes."""
+    a, b = _params(torch.float32, 40, 30)
+    with pytest.raises(ValueError, match="twice"):
+        training.Adam([a, b, a])
+    assert a.grad is None and b.grad is None
+    training.Adam([a, b])
