@@ -96,7 +96,10 @@ class Adam:
         for p in self.params:
             o = used[p.dtype]
             used[p.dtype] += -(-p.numel() // 64) * 64
-            p.grad = self.buffers[p.dtype][o:o + p.numel()].view_as(p)
+            grad = self.buffers[p.dtype][o:o + p.numel()].view_as(p)
+            if p.grad is not None:
+                grad.copy_(p.grad)
+            p.grad = grad
             low = p.dtype != torch.float32
             self.masters.append(p.detach().float() if low else p.detach())
             self.m.append(torch.zeros_like(self.masters[-1]))

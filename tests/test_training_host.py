@@ -106,3 +106,16 @@ def test_a_parameter_given_twice_is_refused(calls):
         training.Adam([a, b, a])
     assert a.grad is None and b.grad is None
     training.Adam([a, b])
+
+
+def test_gradients_that_are_there_stay(calls):
+    """The optimizer's buffers take over gradients from before it was made."""
+    a, b, c = _params(torch.bfloat16, 40, 30, 20)
+    ((a * 3).sum() + (b[:4] * 2).sum()).backward()
+    want = [a.grad.clone(), b.grad.clone()]
+    opt = training.Adam([a, b, c])
+    assert torch.equal(a.grad, want[0]) and torch.equal(b.grad, want[1]) and not bool(c.grad.any())
+    (a * 1).sum().backward()                            # and add to them
+    assert torch.equal(a.grad, want[0] + 1)
+    opt.zero_grad()
+    assert not any(bool(p.grad.any()) for p in opt.params)
