@@ -9,6 +9,7 @@ precision).
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Iterable, Optional
 
 import torch
@@ -18,6 +19,14 @@ from . import binding as B
 
 def _stream():
     return torch.cuda.current_stream().cuda_stream
+
+
+def _on(first, *others):
+    """The device of all these tensors as the current one, where the library works."""
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("tensors on %s and %s: one device is needed" % (first.device, t.device))
+    return torch.cuda.device(first.device) if first.is_cuda else contextlib.nullcontext()
 
 
 def _rows(t):
@@ -36,7 +45,8 @@ class _AddRmsNorm(torch.autograd.Function):
         else:
             residual = _rows(residual)
             h = torch.empty_like(out)
-        B.dd_rms_norm(x, residual, weight, eps, out, h=None if residual is None else h, rstd=rstd, stream=_stream())
+        with _on(x, residual, weight):
+            B.dd_rms_norm(x, residual, weight, eps, out, h=None if residual is None else h, rstd=rstd, stream=_stream())
         ctx.save_for_backward(h, weight, rstd)
         return out if residual is None else (out, h)
 
@@ -53,7 +63,9 @@ class _AddRmsNorm(torch.autograd.Function):
             dw = torch.empty_like(weight)
             # (torch's memory: in a captured graph it stays the graph's)
             work = torch.empty(B.dd_rms_norm_grad_work(rstd.numel(), h.shape[-1]), dtype=torch.uint8, device=h.device)
-        B.dd_rms_norm_grad(dy, h, weight, rstd, dx, dw, dh=None if dh is None else _rows(dh), work=work, stream=_stream())
+        dh = None if dh is None else _rows(dh)
+        with _on(h, dy, dh, weight):
+            B.dd_rms_norm_grad(dy, h, weight, rstd, dx, dw, dh=dh, work=work, stream=_stream())
         return dx, dx if ctx.needs_input_grad[1] else None, dw, None
 
 
@@ -86,6 +98,7 @@ class Adam:
             raise ValueError("a parameter is given twice")
         self.lr, self.betas, self.eps = lr, betas, eps
         self.weight_decay, self.decoupled, self.max_norm = weight_decay, decoupled, max_norm
+        on = _on(*self.params)
         dev = self.params[0].device
         self.buffers = {}
         for dt in {p.dtype for p in self.params}:
@@ -114,7 +127,8 @@ class Adam:
         self._versions = [p._version for p in self.params]
         self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
         self.stats = torch.zeros(3, device=dev)
-        self._handle = B.dd_tensors_load(tensors, _stream())
+        with on:
+            self._handle = B.dd_tensors_load(tensors, _stream())
 
     def zero_grad(self):
         for b in self.buffers.values():
@@ -139,10 +153,11 @@ class Adam:
         written = [i for i, (p, seen) in enumerate(zip(self.params, self._versions)) if p._version != seen]
         if written:
             self.read_weights(written)
-        s = _stream()
-        B.dd_grad_norm(self._handle, self.stats, max_norm=self.max_norm, d_inv_scale=inv_scale, stream=s)
-        B.dd_adam_step(self._handle, self.steps, self.stats, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1],
-                       eps=self.eps, weight_decay=self.weight_decay, decoupled=self.decoupled, stream=s)
+        with _on(self.params[0], inv_scale):
+            s = _stream()
+            B.dd_grad_norm(self._handle, self.stats, max_norm=self.max_norm, d_inv_scale=inv_scale, stream=s)
+            B.dd_adam_step(self._handle, self.steps, self.stats, lr=self.lr, beta1=self.betas[0], beta2=self.betas[1],
+                           eps=self.eps, weight_decay=self.weight_decay, decoupled=self.decoupled, stream=s)
         torch.autograd.graph.increment_version(self.params)     # (graphs that kept the old weights are refused)
         self._versions = [p._version for p in self.params]
 

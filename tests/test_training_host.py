@@ -119,3 +119,44 @@ def test_gradients_that_are_there_stay(calls):
     assert torch.equal(a.grad, want[0] + 1)
     opt.zero_grad()
     assert not any(bool(p.grad.any()) for p in opt.params)
+
+
+def test_calls_are_made_on_the_tensors_device(calls, monkeypatch):
+    """The library works on the current device: it is the tensors' own while a
+    call is made, whatever it is outside."""
+    import contextlib
+    where = []
+
+    @contextlib.contextmanager
+    def on(*tensors):
+        where.append([t for t in tensors if t is not None])
+        calls.made.append(("enter", (), {}))
+        yield
+        calls.made.append(("leave", (), {}))
+
+    monkeypatch.setattr(training, "_on", on)
+    x, w = torch.ones(4, 8, requires_grad=True), torch.ones(8, requires_grad=True)
+    y, h = training.add_rms_norm(x, x.detach(), w)
+    (y.sum() + h.sum()).backward()
+    opt = training.Adam([w])
+    opt.step(inv_scale=torch.ones(1))
+    for name in ("dd_rms_norm", "dd_rms_norm_grad", "dd_grad_norm", "dd_adam_step"):
+        names = [c[0] for c in calls.made]
+        before = names[:names.index(name)]
+        assert before.count("enter") == before.count("leave") + 1, name
+    assert [len(t) for t in where] == [3, 4, 1, 2]
+
+
+def test_tensors_of_several_devices_are_refused(monkeypatch):
+    class On:
+        is_cuda = True
+
+        def __init__(self, device):
+            self.device = torch.device(device)
+
+    assert training._on(On("cuda:1"), None, On("cuda:1")).idx == 1
+    with pytest.raises(ValueError, match="cuda:1 and cuda:2"):
+        training._on(On("cuda:1"), None, On("cuda:2"))
+    monkeypatch.setattr(training, "_stream", lambda: 0)
+    with pytest.raises(ValueError, match="GPU"):                  # as the library says it
+        training.add_rms_norm(torch.ones(4, 8))
