@@ -127,6 +127,7 @@ class Adam:
         self._versions = [p._version for p in self.params]
         self.steps = torch.zeros(1, dtype=torch.int64, device=dev)
         self.stats = torch.zeros(3, device=dev)
+        self._free = B.dd_tensors_free      # (at the program's end the module may be gone first)
         with on:
             self._handle = B.dd_tensors_load(tensors, _stream())
 
@@ -163,7 +164,7 @@ class Adam:
 
     def close(self):
         h, self._handle = self._handle, None
-        B.dd_tensors_free(h)
+        self._free(h)
 
     def __del__(self):
         if getattr(self, "_handle", None):

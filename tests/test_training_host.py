@@ -160,3 +160,21 @@ def test_tensors_of_several_devices_are_refused(monkeypatch):
     monkeypatch.setattr(training, "_stream", lambda: 0)
     with pytest.raises(ValueError, match="GPU"):                  # as the library says it
         training.add_rms_norm(torch.ones(4, 8))
+
+
+def test_an_optimizer_that_lives_to_the_end_of_the_program():
+    """Its handle is freed without a word when the interpreter takes the modules
+    apart."""
+    import os
+    import subprocess
+    import sys
+    code = ("import torch\n"
+            "from paper_2006_03318_amd import training\n"
+            "training.B.dd_tensors_load = lambda tensors, stream=None: 7\n"
+            "training.B.dd_tensors_free = lambda handle: None\n"
+            "training._stream = lambda: 0\n"
+            "opt = training.Adam([torch.nn.Parameter(torch.zeros(4))])\n"
+            "step = opt.step\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "Exception" not in r.stderr, r.stderr
