@@ -369,9 +369,10 @@ typedef struct {
  * The tensors stay where they are for the life of the handle.  The handle
  * keeps 64 bytes of device memory for every 8,192 elements of a tensor (or
  * fewer), and working memory of 8 KiB for dd_grad_norm and dd_adam_step: their
- * calls on several streams are put in order by the library (so a graph is
- * captured on the stream the list was loaded on, and its replays are ordered
- * with other calls on the list by the caller).  Waits for `stream`.
+ * calls on several streams are put in order by the library (so those two are
+ * captured into a graph on the stream the list was loaded on, DD_EINVAL on
+ * another, and the replays are ordered with other calls on the list by the
+ * caller).  A list outlives the graphs that work on it.  Waits for `stream`.
  */
 dd_status dd_tensors_load(int32_t count, const dd_tensor *t, void *stream, dd_tensors **out);
 void dd_tensors_free(dd_tensors *t);

@@ -18,6 +18,23 @@ bool float_type(int32_t t) { return t == DD_F32 || t == DD_BF16 || t == DD_F16; 
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
+// Whether work on s goes into a graph.
+hipError_t captured(hipStream_t s, bool *yes) {
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamIsCapturing(s, &st);
+    *yes = st != hipStreamCaptureStatusNone;
+    return e;
+}
+
+// A graph has no place among the calls of other streams: one that uses the
+// working memory is captured on the list's own stream.
+dd_status check_capture(const dd_tensors *t, hipStream_t s) {
+    bool graph = false;
+    const hipError_t e = s == t->stream ? hipSuccess : captured(s, &graph);
+    if (e != hipSuccess) return hip_fail(e, "stream state");
+    return graph ? fail(DD_EINVAL, "captured on another stream than the list was loaded on") : DD_OK;
+}
+
 // The handle's working memory is one, so calls on it run one after the other:
 // its own stream waits for the uses noted on others, and another stream for
 // its own.
@@ -193,6 +210,7 @@ dd_status dd_grad_norm(const dd_tensors *t, float max_norm, const float *d_inv_s
         if (!d_stats) return fail(DD_EINVAL, "d_stats is NULL");
         if (isnan(max_norm)) return fail(DD_EINVAL, "max_norm is not a number");
         hipStream_t s = (hipStream_t)stream;
+        CHECK(check_capture(t, s));
         std::lock_guard<std::mutex> lk(t->mu);
         hipError_t e = take_turn(t, s);
         if (e == hipSuccess) e = dd::launch_grad_norm(t, max_norm, d_inv_scale, d_stats, s);
@@ -207,9 +225,12 @@ dd_status dd_grad_clip(const dd_tensors *src, const dd_tensors *dst, const float
         if (!d_stats) return fail(DD_EINVAL, "d_stats is NULL");
         if (src != dst && src->sizes != dst->sizes) return fail(DD_EMISMATCH, "the lists differ in their tensors' sizes");
         hipStream_t s = (hipStream_t)stream;
-        hipError_t e = dd::launch_grad_clip(src, dst, d_stats, s);
-        if (e == hipSuccess) e = dd::note_use(src->uses, src->stream, s);
-        if (e == hipSuccess) e = dd::note_use(dst->uses, dst->stream, s);
+        bool graph = false;
+        hipError_t e = s == src->stream && s == dst->stream ? hipSuccess : captured(s, &graph);
+        if (e == hipSuccess) e = dd::launch_grad_clip(src, dst, d_stats, s);
+        // (a point inside a graph is none that a stream could wait for)
+        if (e == hipSuccess && !graph) e = dd::note_use(src->uses, src->stream, s);
+        if (e == hipSuccess && !graph) e = dd::note_use(dst->uses, dst->stream, s);
         return e == hipSuccess ? DD_OK : hip_fail(e, "clip gradients");
     });
 }
@@ -226,6 +247,7 @@ dd_status dd_adam_step(const dd_tensors *t, int64_t *d_step, const float *d_stat
             return fail(DD_EINVAL, "beta1 and beta2 must lie in [0, 1)");
         if (decoupled != 0 && decoupled != 1) return fail(DD_EINVAL, "decoupled must be 0 or 1");
         hipStream_t s = (hipStream_t)stream;
+        CHECK(check_capture(t, s));
         const dd::AdamParams p{lr, beta1, beta2, eps, weight_decay, decoupled};
         std::lock_guard<std::mutex> lk(t->mu);
         hipError_t e = take_turn(t, s);
@@ -282,10 +304,10 @@ dd_status dd_rms_norm_grad(const dd_rms_norm_grad_args *a, void *stream) {
         hipError_t e = hipSuccess;
         if (a->dw && !work) {
             // (the block goes back to the cache, a graph would keep writing to it)
-            hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-            e = hipStreamIsCapturing(s, &capture);
+            bool graph = false;
+            e = captured(s, &graph);
             if (e != hipSuccess) return hip_fail(e, "alloc partial sums");
-            if (capture != hipStreamCaptureStatusNone) return fail(DD_EINVAL, "a captured gradient needs work from the caller");
+            if (graph) return fail(DD_EINVAL, "a captured gradient needs work from the caller");
             e = dd::dalloc(&taken, dd::rms_grad_work(a->rows, a->cols), s);
             if (e != hipSuccess) return hip_fail(e, "alloc partial sums");
             work = taken;
