@@ -200,6 +200,16 @@ hipError_t note_use(ForeignUses &u, hipStream_t own, hipStream_t s) {
     return hipEventRecord(ev, s);
 }
 
+hipError_t follow_uses(ForeignUses &u, hipStream_t s) {
+    std::lock_guard<std::mutex> lk(u.mu);
+    for (auto &x : u.ev) {
+        if (x.first == s) continue;
+        const hipError_t e = hipStreamWaitEvent(s, x.second, 0);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 void join_uses(ForeignUses &u, hipStream_t own) {
     std::lock_guard<std::mutex> lk(u.mu);
     for (auto &x : u.ev) {

@@ -46,6 +46,7 @@ struct dd_tensors {
     dd::TensorWork *work = nullptr;   // one block of memory, the chunks behind it
     dd::TensorChunk *chunks = nullptr;
     mutable std::mutex mu;        // held while a call that uses work is queued
+    mutable bool own_turn = false;    // the last of them was on `stream`
     mutable dd::ForeignUses uses;
 };
 
@@ -55,6 +56,9 @@ namespace dd {
 dd_status fail(dd_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 dd_status hip_fail(hipError_t e, const char *what);
 void no_error();
+
+// make s wait for every use recorded on another stream
+hipError_t follow_uses(ForeignUses &u, hipStream_t s);
 
 // weight update over a list of tensors (k_update.hip)
 struct AdamParams {

@@ -35,18 +35,28 @@ dd_status check_capture(const dd_tensors *t, hipStream_t s) {
     return graph ? fail(DD_EINVAL, "captured on another stream than the list was loaded on") : DD_OK;
 }
 
-// The handle's working memory is one, so calls on it run one after the other:
-// its own stream waits for the uses noted on others, and another stream for
-// its own.
+// The handle's working memory is one, so calls on it run one after the other
+// on whatever streams they are made.  Its own stream waits for the uses noted on
+// others; another stream for those, and for the own stream only where that has
+// had a call since (what else is queued there is none of its business).
 hipError_t take_turn(const dd_tensors *t, hipStream_t s) {
-    dd::join_uses(t->uses, t->stream);
-    if (s == t->stream) return hipSuccess;
+    if (s == t->stream) {
+        dd::join_uses(t->uses, s);
+        return hipSuccess;
+    }
+    hipError_t e = dd::follow_uses(t->uses, s);
+    if (e != hipSuccess || !t->own_turn) return e;
     hipEvent_t ev = nullptr;
-    hipError_t e = hipEventCreateWithFlags(&ev, hipEventDisableTiming);
+    e = hipEventCreateWithFlags(&ev, hipEventDisableTiming);
     if (e != hipSuccess) return e;
     e = hipEventRecord(ev, t->stream);
     if (e == hipSuccess) e = hipStreamWaitEvent(s, ev, 0);
     (void)hipEventDestroy(ev);
+    return e;
+}
+hipError_t end_turn(const dd_tensors *t, hipStream_t s) {
+    const hipError_t e = dd::note_use(t->uses, t->stream, s);
+    if (e == hipSuccess) t->own_turn = s == t->stream;
     return e;
 }
 
@@ -214,7 +224,7 @@ dd_status dd_grad_norm(const dd_tensors *t, float max_norm, const float *d_inv_s
         std::lock_guard<std::mutex> lk(t->mu);
         hipError_t e = take_turn(t, s);
         if (e == hipSuccess) e = dd::launch_grad_norm(t, max_norm, d_inv_scale, d_stats, s);
-        if (e == hipSuccess) e = dd::note_use(t->uses, t->stream, s);
+        if (e == hipSuccess) e = end_turn(t, s);
         return e == hipSuccess ? DD_OK : hip_fail(e, "gradient norm");
     });
 }
@@ -252,7 +262,7 @@ dd_status dd_adam_step(const dd_tensors *t, int64_t *d_step, const float *d_stat
         std::lock_guard<std::mutex> lk(t->mu);
         hipError_t e = take_turn(t, s);
         if (e == hipSuccess) e = dd::launch_adam(t, d_step, d_stats, p, s);
-        if (e == hipSuccess) e = dd::note_use(t->uses, t->stream, s);
+        if (e == hipSuccess) e = end_turn(t, s);
         return e == hipSuccess ? DD_OK : hip_fail(e, "adam step");
     });
 }

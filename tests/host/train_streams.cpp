@@ -140,9 +140,24 @@ int main() {
         EXPECT(events == 0);
     }
 
+    // calls on one other stream: it and the list's stream go on independently
     seen.clear();
     const hipStream_t own = stream(1), side = stream(2), third = stream(3);
     dd_tensors *t = load(own);
+    Seen unrelated, on_side;
+    for (int k = 0; k < 5; k++) {
+        unrelated.insert(work_on(own));
+        on_side.insert(works);
+        EXPECT(norm(t, side) == DD_OK);
+        on_side.insert(works);
+        EXPECT(adam(t, side) == DD_OK);
+    }
+    for (int w : unrelated) EXPECT(!seen[side].count(w));
+    for (int w : on_side) EXPECT(!seen[own].count(w));
+    EXPECT(norm(t, third) == DD_OK);                     // a third follows the second alone
+    EXPECT(after(seen[third], on_side));
+    for (int w : unrelated) EXPECT(!seen[third].count(w));
+    EXPECT(norm(t, own) == DD_OK && after(seen[own], on_side));
 
     // a graph takes calls on the list's own stream, and clipping on any
     capturing = own;
