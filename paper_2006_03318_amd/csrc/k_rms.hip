@@ -38,8 +38,7 @@ struct Quotient {
     __device__ __forceinline__ float operator()(float x) const { return (float)((double)x * inv); }
 };
 
-__device__ __forceinline__ uint8_t to_8_bits(float x, int32_t out_type) {
-    if (out_type == DD_E4M3) return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false);
+__device__ __forceinline__ uint8_t to_i8(float x) {
     const float r = rintf(x);
     return (uint8_t)(int8_t)(r < -127.0f ? -127 : r > 127.0f ? 127 : r != r ? 0 : (int)r);
 }
@@ -96,8 +95,8 @@ __device__ __forceinline__ void store_pack_8(uint8_t *p, const float (&x)[8], in
     } else {
 #pragma unroll
         for (int i = 0; i < 2; i++)
-            b[i] = (uint32_t)to_8_bits(x[4 * i], DD_I8) | (uint32_t)to_8_bits(x[4 * i + 1], DD_I8) << 8 |
-                   (uint32_t)to_8_bits(x[4 * i + 2], DD_I8) << 16 | (uint32_t)to_8_bits(x[4 * i + 3], DD_I8) << 24;
+            b[i] = (uint32_t)to_i8(x[4 * i]) | (uint32_t)to_i8(x[4 * i + 1]) << 8 | (uint32_t)to_i8(x[4 * i + 2]) << 16 |
+                   (uint32_t)to_i8(x[4 * i + 3]) << 24;
     }
     if (have >= 8) {
         *(gptr<U>)(p) = b;
