@@ -57,3 +57,23 @@ def test_fused_layers_keep_their_longest_kernel():
                 assert left.size == 1 and g.dur[left[0]] == g.dur[ids].max()
                 assert np.all(gone[g.launch_of[ids[gone[ids]]]])
     assert not np.any(gone[k & ~np.isin(g.layer, layers)])
+
+
+def test_norms_become_one_kernel_a_pass(oracle_mod):
+    """A trace whose layers carry the iteration's own names: each pass through
+    a norm keeps one kernel, and the iteration is shorter for it."""
+    tg = _trace()
+    tg.layer_names = [n.split()[0] + " norm %d" % i if "BatchNorm" in n else n for i, n in enumerate(tg.layer_names)]
+    norms = [i for i, n in enumerate(tg.layer_names) if "norm" in n]
+    g, vs, names = F.what_if(tg)
+    k = R.is_kernel(g)
+    for v, name in enumerate(names):
+        gone = ((vs.remove_bits[:, 0] >> v) & 1).astype(bool)
+        for la in norms:
+            for it in (2, 3):
+                ids = np.nonzero(k & (g.layer == la) & (g.iteration == it))[0]
+                assert ids.size == (2 if tg.layer_names[la].startswith("fwd") else 1)
+                fused = name in ("fused norms", "both", "both, update in one pass")
+                assert int(gone[ids].sum()) == (ids.size - 1 if fused else 0)
+    _, _, ms, _ = oracle_mod.run(g, vs)
+    assert ms[2] < ms[0] and ms[3] < ms[1] and ms[3] < ms[2]
