@@ -78,16 +78,19 @@ def add_rms_norm(x, residual=None, weight=None, eps: float = 1e-6):
 
 
 class Adam:
-    """Adam over all parameters in one launch, gradients clipped to max_norm on
-    the way (0: not clipped), and skipped where one is not finite.
+    """Adam over all parameters at once, gradients clipped to max_norm on the way
+    (0: not clipped), and skipped where one is not finite: two launches a step,
+    three for large lists.
 
     Gradients live in one buffer per type that stays where it is; parameters of
     16 bits get f32 masters.  Weight decay spares parameters of fewer than two
     dimensions.  What else writes a parameter in place (a checkpoint that is
     loaded, a broadcast) is seen at the next step and goes on from there; after
-    writes that torch does not count (through `.data`, by other libraries) call
-    `read_weights()`.  `stats` holds the last step's gradient norm, factor and
-    whether it was skipped, `steps` the steps taken, both on the GPU."""
+    writes that torch does not count (through `.data`, by other libraries), and
+    between replays, call `read_weights()`.  A step is captured into a graph on
+    the stream that was current when the optimizer was made, and replayed with
+    the settings of the capture.  `stats` holds the last step's gradient norm,
+    factor and whether it was skipped, `steps` the steps taken, both on the GPU."""
 
     def __init__(self, params: Iterable[torch.nn.Parameter], lr=1e-3, betas=(0.9, 0.999), eps=1e-8,
                  weight_decay=0.0, decoupled=True, max_norm=0.0):

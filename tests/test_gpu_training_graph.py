@@ -72,3 +72,49 @@ def test_gradient_without_working_memory_is_not_captured():
     graph.replay()
     torch.cuda.synchronize()
     assert bool((dw == float(rows)).all())
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float32"])
+def test_training_step(kind):
+    """Gradients, norm and update of an optimizer that was made on the capture's
+    stream; the same steps taken eagerly."""
+    import torch
+    from paper_2006_03318_amd.training import Adam, add_rms_norm
+    require_gpu()
+    gen = torch.Generator("cuda").manual_seed(5)
+    t = getattr(torch, kind)
+    x = torch.randn(300, 520, generator=gen, device="cuda").to(t)
+    dy = torch.randn(300, 520, generator=gen, device="cuda").to(t)
+    start = (1 + 0.1 * torch.randn(520, generator=gen, device="cuda")).to(t)
+
+    def make():
+        w = torch.nn.Parameter(start.clone())
+        return w, Adam([w], lr=0.01, weight_decay=0.1, max_norm=1.0)
+
+    def step(w, opt):
+        opt.zero_grad()
+        add_rms_norm(x, None, w).backward(dy)
+        opt.step()
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        w, opt = make()
+        step(w, opt)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(w, opt)
+    w2, opt2 = make()
+    step(w2, opt2)
+    for k in range(4):
+        x.mul_(-1.25)
+        step(w2, opt2)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w, w2) and torch.equal(opt.stats, opt2.stats) and int(opt.steps) == int(opt2.steps) == k + 2
+        assert all(torch.equal(a, b) for a, b in zip(opt.masters + opt.m + opt.v, opt2.masters + opt2.m + opt2.v))
+    del graph
+    opt.close()
+    opt2.close()
