@@ -284,7 +284,7 @@ __device__ __forceinline__ void weights_at(const Args &a, int64_t c, int have, f
 }
 // Wider than 32,768 columns: bound by HBM and what the L2 does not keep.
 // 4,000 x 40,000 bf16 with a residual 289 us (4.4 TB/s of what has to move), to
-// 8 bits by 128 columns 267 us (column by column 641 and 1,463).
+// 8 bits by 128 columns 269 us (column by column 641 and 1,463).
 template <class T>
 __global__ void __launch_bounds__(kLoopLanes) k_rms_loop(RmsArgs a) {
     __shared__ float slots[2][16];
@@ -591,11 +591,11 @@ int dw_runs(int64_t rows) {
 // Lanes per row and packs per lane.  Two packs of each input are enough loads
 // under way, and more cost registers, so the fewest lanes that hold the row
 // with two packs (four at the widest), a whole wave or more past 256 columns
-// so that no lanes idle.  Measured on bf16 with a residual, TB/s: 8,192 x
-// 4,096 to 8 bits 4.8 with 256 lanes x 2 (128 x 4: 4.2, 64 x 8: 3.6, 1,024 x
-// 1: 2.7); 16,384 x 1,024 5.0 with 64 x 2 (256 x 1: 4.3); 65,536 x 2,048
-// 5.8 with 256 x 1 (64 x 4: 5.7); 65,536 x 128 to 8 bits 3.6 with 16 x 1
-// (64 x 1: 1.5); 65,536 x 64 3.5 with 8 x 1 (16 x 1: 2.7).  Few rows take the
+// so that no lanes idle.  Measured on bf16 with a residual, TB/s (to 8 bits with
+// the quotients in 32, which takes 3 to 6 % less): 8,192 x 4,096 to 8 bits 4.8
+// with 256 lanes x 2 (128 x 4: 4.2, 64 x 8: 3.6, 1,024 x 1: 2.7); 16,384 x 1,024
+// 5.0 with 64 x 2 (256 x 1: 4.3); 65,536 x 2,048 5.8 with 256 x 1 (64 x 4: 5.7);
+// 65,536 x 128 to 8 bits 3.6 with 16 x 1 (64 x 1: 1.5); 65,536 x 64 3.5 with 8 x 1 (16 x 1: 2.7).  Few rows take the
 // same: 4 to 512 rows of 4,096 are as fast with any of these shapes, the launch
 // bounds them.
 struct Shape {

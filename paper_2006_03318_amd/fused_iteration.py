@@ -14,12 +14,13 @@ torch operations, tensor by tensor; `--fused` runs them with this library.
         python3 -m paper_2006_03318_amd.fused_iteration --plain
     python -m paper_2006_03318_amd.fused_iteration --predict OUT
 
-On one MI355X, 8 blocks of hidden size 2,048 over 16,384 rows: 41.2 ms an
-iteration plain (41.1 traced), 28.8 predicted with the norms fused and the
-update in one pass (31.5 with the paper's rule, which keeps the summed time of
-the update), 29.2 measured fused.  Tracing lengthens every host call, so an
-iteration whose host is the slower side has to be longer on the GPU for the
-trace to show it as it is: more rows.
+On one MI355X, 8 blocks of hidden size 2,048 over 65,536 rows (`--rows 65536`):
+134.4 ms an iteration plain (134.9 while traced, 135.1 simulated from the trace),
+99.8 predicted with the norms fused and the update in one pass (104.4 with the
+paper's rule, which keeps the summed time of the update), 98.2 measured fused.
+Tracing lengthens every host call, so an iteration whose host is the slower side
+has to be longer on the GPU for the trace to show it as it is: 16,384 rows take
+37.2 ms plain, 46.4 while traced, and 25.9 fused where 29.4 are predicted.
 """
 from __future__ import annotations
 
