@@ -477,6 +477,157 @@ typedef struct {
 dd_status dd_rms_norm_grad(const dd_rms_norm_grad_args *a, void *stream);
 size_t dd_rms_norm_grad_work(int64_t rows, int64_t cols);
 
+/* ---------------------------------------------------------------------------
+ * The rest of a training iteration between its norms and its weight update:
+ * the products of a block with what is fused into them, dropout, and the
+ * embedding.  Tensors, streams and rounding as above, and:
+ *
+ *   - Strides count elements and are those of rows; the elements of a row are
+ *     consecutive.  An input's rows may start at any stride (0: the same row
+ *     for all), an output's at least a row apart.
+ *   - Outputs must not overlap inputs or each other but where it is said.
+ *   - work   device memory of the size that the function of that name gives,
+ *            aligned to 16, which the call overwrites, or NULL: the library
+ *            takes it from its cache for the time of the call.  A call that
+ *            needs some and is captured into a graph has to bring it
+ *            (DD_EINVAL): the replays write there too.
+ */
+#define DD_ACT_NONE 0
+#define DD_ACT_RELU 1
+#define DD_ACT_GELU 2        /* z Phi(z) */
+#define DD_ACT_GELU_TANH 3   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define DD_ACT_SILU 4        /* z / (1 + exp(-z)) */
+
+/*
+ * dd_linear -- for rows x [rows][k] and a weight w of k by n, summed in 32 bits:
+ *   z = x w + bias,   y = act(z) + residual
+ * y and z (what the gradient needs of an activation) are each rounded from
+ * these sums.  y may be residual, element for element.
+ */
+typedef struct {
+    int64_t rows, k, n;
+    int64_t x_stride, w_stride, residual_stride, y_stride, z_stride;
+    const void *x, *w;           /* type; w: [k][n], or [n][k] if turned */
+    const void *bias;            /* bias_type [n], or NULL */
+    const void *residual;        /* type [rows][n], or NULL */
+    void *y, *z;                 /* type [rows][n]; z may be NULL */
+    void *work;                  /* dd_linear_work(rows, k, n) bytes, or NULL */
+    int32_t type;                /* DD_BF16 or DD_F16 */
+    int32_t bias_type;           /* DD_F32, or type */
+    int32_t act;                 /* DD_ACT_... */
+    int32_t turned;              /* 0 or 1 */
+} dd_linear_args;
+dd_status dd_linear(const dd_linear_args *a, void *stream);
+size_t dd_linear_work(int64_t rows, int64_t k, int64_t n);
+
+/*
+ * dd_linear_grad -- from the gradient dy [rows][n] of x w + bias (with an
+ * activation: what dd_act_grad makes of y's), each optional (NULL: not wanted):
+ *   dx = (dy w^T) * act'(in_z)   [rows][k]; in_z: x is act(in_z), and dx the
+ *                                gradient of in_z (NULL: that of x)
+ *   dw = x^T dy                  laid out as w is (turned or not)
+ *   db = sum over rows of dy     in bias_type
+ * dw and db of no rows are zeros.  dx may be in_z or x, element for element, if dw
+ * is not wanted.  Sums over many rows are cut into parts whose sums are
+ * joined in order: the same bits on every call.
+ */
+typedef struct {
+    int64_t rows, k, n;
+    int64_t dy_stride, x_stride, w_stride, in_z_stride, dx_stride, dw_stride;
+    const void *dy;              /* type [rows][n] */
+    const void *x;               /* type [rows][k]; needed for dw */
+    const void *w;               /* type, as in dd_linear; needed for dx */
+    const void *in_z;            /* type [rows][k], or NULL */
+    void *dx, *dw, *db;
+    void *work;                  /* dd_linear_grad_work(rows, k, n) bytes, or NULL */
+    int32_t type, bias_type, in_act, turned;
+} dd_linear_grad_args;
+dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream);
+size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n);
+
+/*
+ * dd_act_grad -- dz = dy * act'(z), element by element.  dz may be dy or z.
+ */
+typedef struct {
+    int64_t rows, cols;
+    int64_t dy_stride, z_stride, dz_stride;
+    const void *dy, *z;
+    void *dz;
+    int32_t type;                /* DD_F32, DD_BF16 or DD_F16 */
+    int32_t act;
+} dd_act_grad_args;
+dd_status dd_act_grad(const dd_act_grad_args *a, void *stream);
+
+/*
+ * dd_dropout -- out = residual + (x / (1 - q) where kept, else 0), with q = p to
+ * the nearest 65,536th (halves to even) and the quotient as x times 65536 / (65536
+ * - 65536 q), rounded to 32 bits.  The gradient of x is the same call on out's
+ * gradient without a residual; no mask is stored.
+ *   Element i (row * cols + column) is kept if its number of 16 bits is at least
+ * 65536 q: the (i mod 8)-th half, low halves first, of the four words that
+ * Philox 4x32-10 (Salmon et al., SC 2011) gives for the counter (low and high
+ * word of i / 8, low and high word of c) and the key d_state[0], low word first,
+ * where c = d_state[1] + call.  It depends on nothing else: not on strides, types or where
+ * the call runs.
+ *   d_state   device uint64 [2]: key and counter; read as the work runs, so that
+ *             replays of a captured call go on where the caller has moved it to.
+ *   d_used    device uint64 [2] or NULL, written: key and c, which with call = 0
+ *             give the gradient this mask.  Not d_state.
+ * out may be x or residual, element for element.  What is dropped counts for
+ * nothing, also if it is infinite or not a number.  0 <= p <= 1.
+ */
+typedef struct {
+    int64_t rows, cols;
+    int64_t x_stride, residual_stride, out_stride;
+    const void *x, *residual;    /* type; residual may be NULL */
+    void *out;                   /* type */
+    const uint64_t *d_state;
+    uint64_t *d_used;
+    uint64_t call;
+    double p;
+    int32_t type;                /* DD_F32, DD_BF16 or DD_F16 */
+    int32_t reserved;            /* 0 */
+} dd_dropout_args;
+dd_status dd_dropout(const dd_dropout_args *a, void *stream);
+
+/*
+ * dd_embed -- out[t] = scale * table[ids[t]], for `tokens` rows of cols.  An id
+ * that the table does not have (negative, or vocab and more) gives a row of NaNs.
+ */
+typedef struct {
+    int64_t tokens, vocab, cols;
+    int64_t table_stride, out_stride;
+    const void *ids;             /* int64 or int32 [tokens] */
+    const void *table;           /* type [vocab][cols] */
+    void *out;                   /* type [tokens][cols] */
+    float scale;
+    int32_t type;                /* DD_F32, DD_BF16 or DD_F16 */
+    int32_t id_bytes;            /* 8 or 4 */
+    int32_t reserved;            /* 0 */
+} dd_embed_args;
+dd_status dd_embed(const dd_embed_args *a, void *stream);
+
+/*
+ * dd_embed_grad -- dtable[v] = scale * sum of dy[t] over the tokens with ids[t] =
+ * v, for every row of the table (zeros where there is none), each sum taken in 32 bits
+ * in the tokens' order, in parts of fixed lengths: the same bits on every call.  Tokens
+ * with the id `pad`, and ids that the table does not have, count for nothing.
+ */
+typedef struct {
+    int64_t tokens, vocab, cols;
+    int64_t dy_stride, dtable_stride;
+    const void *ids;             /* int64 or int32 [tokens] */
+    const void *dy;              /* type [tokens][cols] */
+    void *dtable;                /* type [vocab][cols] */
+    void *work;                  /* dd_embed_grad_work(tokens, vocab, cols) bytes, or NULL */
+    int64_t pad;                 /* -1: none */
+    float scale;
+    int32_t type, id_bytes;
+    int32_t reserved;            /* 0 */
+} dd_embed_grad_args;
+dd_status dd_embed_grad(const dd_embed_grad_args *a, void *stream);
+size_t dd_embed_grad_work(int64_t tokens, int64_t vocab, int64_t cols);
+
 /*
  * dd_release_cache -- wait for all work on the current device, then return
  * every block of the library's device-memory cache for that device to the

@@ -85,6 +85,10 @@ def lib():
         "dd_rms_norm": (_i32, [ctypes.c_char_p, _vp]),
         "dd_rms_norm_grad": (_i32, [ctypes.c_char_p, _vp]),
         "dd_rms_norm_grad_work": (ctypes.c_size_t, [_i64, _i64]),
+        **{name: (_i32, [ctypes.c_char_p, _vp]) for name in (
+            "dd_linear", "dd_linear_grad", "dd_act_grad", "dd_dropout", "dd_embed", "dd_embed_grad")},
+        **{name: (ctypes.c_size_t, [_i64, _i64, _i64]) for name in (
+            "dd_linear_work", "dd_linear_grad_work", "dd_embed_grad_work")},
         "dd_graph_free": (None, [_vp]),
         "dd_sched_free": (None, [_vp]),
         "dd_variants_free": (None, [_vp]),
@@ -276,7 +280,7 @@ _NAMED = {}
 def _types():
     if not _DT:
         import torch
-        _NAMED.update(float32=torch.float32, int64=torch.int64)
+        _NAMED.update(float32=torch.float32, int64=torch.int64, int32=torch.int32)
         _DT.update({torch.float32: DD_F32, torch.bfloat16: DD_BF16, torch.float16: DD_F16,
                     torch.float8_e4m3fn: DD_E4M3, torch.int8: DD_I8})
     return _DT
@@ -449,3 +453,221 @@ def dd_rms_norm_grad(dy, h, weight, rstd, dx, dw=None, dh=None, work=None, strea
 
 def dd_rms_norm_grad_work(rows: int, cols: int) -> int:
     return lib().dd_rms_norm_grad_work(int(rows), int(cols))
+
+
+# ---------------------------------------------------------------------------
+# a layer's product, dropout and the embedding
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_LINEAR = struct.Struct("@8q7P4i")
+_LINEAR_GRAD = struct.Struct("@9q8P4i")
+_ACT_GRAD = struct.Struct("@5q3P2i")
+_DROPOUT = struct.Struct("@5q5PQd2i")
+_EMBED = struct.Struct("@5q3Pf3i")
+_EMBED_GRAD = struct.Struct("@5q4Pqf3i")
+
+
+def _act(act):
+    try:
+        return ACTS[act]
+    except KeyError:
+        raise ValueError("act must be one of %s (got %r)" % (", ".join(ACTS), act)) from None
+
+
+def _work(work, need):
+    """Address of a caller's working memory."""
+    if work is None:
+        return 0
+    if not work.is_cuda or not work.is_contiguous() or work.numel() * work.element_size() < need:
+        raise ValueError("work must hold %d bytes on the GPU" % need)
+    return work.data_ptr()
+
+
+def _matrix(name, t, shape, dtype):
+    """(address, stride, turned) of a [k, n] matrix that lies by its rows or, turned, by
+    its columns."""
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.stride(1) == 1 or shape[1] == 1:
+        return t.data_ptr(), t.stride(0), 0
+    if t.stride(0) == 1 or shape[0] == 1:
+        return t.data_ptr(), t.stride(1), 1
+    raise ValueError("%s: the elements of a row, or those of a column, must be consecutive" % name)
+
+
+def _half(name, t):
+    kind = (_DT or _types()).get(t.dtype, -1)
+    if kind != DD_BF16 and kind != DD_F16:
+        raise TypeError("%s must be bfloat16 or float16" % name)
+    if not t.dim() or t.shape[-1] < 1:
+        raise ValueError("%s must have a dimension and not be empty" % name)
+    return kind
+
+
+def _bias(name, t, n, kind):
+    """(address, type)"""
+    if t is None:
+        return 0, DD_F32
+    bk = _DT.get(t.dtype, -1)
+    if bk != DD_F32 and bk != kind:
+        raise TypeError("%s must be float32 or the rows' type" % name)
+    return _gpu(name, t, n, bk), bk
+
+
+def dd_linear(x, w, y, bias=None, residual=None, act="none", z=None, work=None, stream=None):
+    """y = act(x w + bias) + residual, for x [..., k] and w [k, n] in bfloat16 or float16;
+    w by rows, or by columns (the transpose of an [n, k] weight).  z receives x w + bias.
+    work: uint8 of dd_linear_work(rows, k, n), or None (from the library's cache; not
+    under graph capture if it is not 0)."""
+    kind, shape, dt = _half("x", x), x.shape, x.dtype
+    k = shape[-1]
+    if w.dim() != 2 or w.shape[0] != k:
+        raise ValueError("w: expected shape (%d, n), got %s" % (k, tuple(w.shape)))
+    n, rows = w.shape[1], x.numel() // k
+    out = shape[:-1] + (n,)
+    px, sx = _rows("x", x, shape, k, dt)
+    pw, sw, turned = _matrix("w", w, w.shape, dt)
+    pb, bk = _bias("bias", bias, n, kind)
+    pr, sr = _rows("residual", residual, out, n, dt)
+    py, sy = _rows("y", y, out, n, dt)
+    pz, sz = _rows("z", z, out, n, dt)
+    args = _LINEAR.pack(rows, k, n, sx, sw, sr, sy, sz, px, pw, pb, pr, py, pz,
+                        0 if work is None else _work(work, dd_linear_work(rows, k, n)), kind, bk, _act(act), turned)
+    rc = (_lib or lib()).dd_linear(args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_linear_work(rows: int, k: int, n: int) -> int:
+    return lib().dd_linear_work(int(rows), int(k), int(n))
+
+
+def dd_linear_grad(dy, x=None, w=None, dx=None, dw=None, db=None, in_act="none", in_z=None, work=None, stream=None):
+    """dx = (dy w^T) * in_act'(in_z), dw = x^T dy (by rows or by columns) and db = the sum of
+    dy's rows, each if it is given; dx needs w, dw needs x.  work: uint8 of
+    dd_linear_grad_work(rows, k, n), or None (as in dd_linear)."""
+    kind, shape, dt = _half("dy", dy), dy.shape, dy.dtype
+    n = shape[-1]
+    rows = dy.numel() // n
+    if dx is not None and w is None or dw is not None and x is None:
+        raise ValueError("dx needs w, and dw needs x")
+    some = w if dx is not None else dw
+    if some is None:
+        k, wide = 1, None       # (db alone)
+    else:
+        if some.dim() != 2 or some.shape[1] != n:
+            raise ValueError("w, dw: expected shape (k, %d), got %s" % (n, tuple(some.shape)))
+        k, wide = some.shape[0], some.shape
+    pd, sd = _rows("dy", dy, shape, n, dt)
+    rows_of_x = shape[:-1] + (k,)
+    px, sx = _rows("x", x if dw is not None else None, rows_of_x, k, dt)
+    pi, si = _rows("in_z", in_z if dx is not None else None, rows_of_x, k, dt)
+    pdx, sdx = _rows("dx", dx, rows_of_x, k, dt)
+    pw, sw, turned = _matrix("w", w, wide, dt) if dx is not None else (0, 0, 0)
+    pdw, sdw, dturned = _matrix("dw", dw, wide, dt) if dw is not None else (0, 0, 0)
+    pdb, bk = _bias("db", db, n, kind)
+    pwork = 0 if work is None else _work(work, dd_linear_grad_work(rows, k, n))
+    act = _act(in_act) if dx is not None else 0
+    call, s = (_lib or lib()).dd_linear_grad, None if stream is None else _stream(stream)
+    if dx is not None and dw is not None and turned != dturned:
+        # (each by its own layout; dw first, as dx may be x)
+        rc = call(_LINEAR_GRAD.pack(rows, k, n, sd, sx, 0, 0, 0, sdw, pd, px, 0, 0, 0, pdw, pdb, pwork, kind, bk, 0, dturned), s)
+        if rc:
+            _check(rc)
+        pdw = pdb = 0
+    rc = call(_LINEAR_GRAD.pack(rows, k, n, sd, sx, sw, si, sdx, sdw, pd, px, pw, pi, pdx, pdw, pdb, pwork, kind, bk, act,
+                                turned if dx is not None else dturned), s)
+    if rc:
+        _check(rc)
+
+
+def dd_linear_grad_work(rows: int, k: int, n: int) -> int:
+    return lib().dd_linear_grad_work(int(rows), int(k), int(n))
+
+
+def _float_rows(x):
+    kind = (_DT or _types()).get(x.dtype, -1)
+    if not 0 <= kind <= DD_F16:
+        raise TypeError("rows must be float32, bfloat16 or float16")
+    if not x.dim() or x.shape[-1] < 1:
+        raise ValueError("rows must have a dimension and not be empty")
+    return kind, x.shape, x.shape[-1]
+
+
+def dd_act_grad(dy, z, dz, act, stream=None):
+    """dz = dy * act'(z); dz may be dy or z."""
+    kind, shape, cols = _float_rows(dy)
+    pd, sd = _rows("dy", dy, shape, cols, dy.dtype)
+    pz, sz = _rows("z", z, shape, cols, dy.dtype)
+    po, so = _rows("dz", dz, shape, cols, dy.dtype)
+    rc = (_lib or lib()).dd_act_grad(_ACT_GRAD.pack(dy.numel() // cols, cols, sd, sz, so, pd, pz, po, kind, _act(act)),
+                                     None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_dropout(x, residual, p, state, out, call=0, used=None, stream=None):
+    """out = residual + x / (1 - p) where the generator keeps x, else residual (which may be
+    None).  state: int64 [2] on the GPU, the key and the counter, to which `call` is
+    added; used (int64 [2] or None) receives the two, for the gradient."""
+    kind, shape, cols = _float_rows(x)
+    px, sx = _rows("x", x, shape, cols, x.dtype)
+    pr, sr = _rows("residual", residual, shape, cols, x.dtype)
+    po, so = _rows("out", out, shape, cols, x.dtype)
+    args = _DROPOUT.pack(x.numel() // cols, cols, sx, sr, so, px, pr, po, _small("state", state, 2, "int64"),
+                         0 if used is None else _small("used", used, 2, "int64"), call & (1 << 64) - 1, p, kind, 0)
+    rc = (_lib or lib()).dd_dropout(args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def _ids(ids):
+    """(address, tokens, bytes) of whole numbers on the GPU."""
+    if not _DT:
+        _types()
+    size = 8 if ids.dtype is _NAMED["int64"] else 4
+    if size == 4 and ids.dtype is not _NAMED["int32"]:
+        raise TypeError("ids must be int64 or int32, got %s" % ids.dtype)
+    if not ids.is_cuda or not ids.is_contiguous():
+        raise ValueError("ids must be contiguous on the GPU")
+    return ids.data_ptr(), ids.numel(), size
+
+
+def _table(name, t):
+    kind, shape, cols = _float_rows(t)
+    if len(shape) != 2 or shape[0] < 1:
+        raise ValueError("%s must have two dimensions and not be empty" % name)
+    return kind, shape[0], cols, *_rows(name, t, shape, cols, t.dtype)
+
+
+def dd_embed(ids, table, out, scale=1.0, stream=None):
+    """out = scale * table[ids], for ids of any shape and table [vocab, cols]; rows of NaN for
+    ids that the table does not have."""
+    pi, tokens, size = _ids(ids)
+    kind, vocab, cols, pt, st = _table("table", table)
+    po, so = _rows("out", out, ids.shape + (cols,), cols, table.dtype)
+    rc = (_lib or lib()).dd_embed(_EMBED.pack(tokens, vocab, cols, st, so, pi, pt, po, scale, kind, size, 0),
+                                  None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_embed_grad(ids, dy, dtable, scale=1.0, pad=-1, work=None, stream=None):
+    """dtable[v] = scale * the sum of dy's rows whose id is v; ids equal to pad (-1: none), or that
+    the table does not have, count for nothing.  work: uint8 of
+    dd_embed_grad_work(tokens, vocab, cols), or None (as in dd_linear)."""
+    pi, tokens, size = _ids(ids)
+    kind, vocab, cols, pt, st = _table("dtable", dtable)
+    pd, sd = _rows("dy", dy, ids.shape + (cols,), cols, dtable.dtype)
+    args = _EMBED_GRAD.pack(tokens, vocab, cols, sd, st, pi, pd, pt,
+                            0 if work is None else _work(work, dd_embed_grad_work(tokens, vocab, cols)), pad, scale, kind, size, 0)
+    rc = (_lib or lib()).dd_embed_grad(args, None if stream is None else _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def dd_embed_grad_work(tokens: int, vocab: int, cols: int) -> int:
+    return lib().dd_embed_grad_work(int(tokens), int(vocab), int(cols))

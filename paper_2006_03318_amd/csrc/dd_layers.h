@@ -1,0 +1,56 @@
+// Declarations shared by the sources of a layer's product, of dropout and of
+// the embedding.
+#pragma once
+
+#include "dd_train.h"
+
+namespace dd {
+
+typedef dd_linear_args LinearArgs;
+typedef dd_linear_grad_args LinearGradArgs;
+
+// What becomes of a sum s of products before it is stored (k_linear.hip):
+//   t = s + bias,  z = t,  out = act(t) + residual     or
+//   out = s * act'(in_z)
+struct Epilogue {
+    const void *bias, *residual, *in_z;
+    void *z, *out;
+    int64_t residual_stride, in_z_stride, z_stride, out_stride;
+    int32_t bias_type, act, in_act;
+};
+
+// out[i][j] = sum over l of p(i, l) q(l, j).  An operand lies by its rows (i or
+// j: l is consecutive) or by its sums (i or j is consecutive); its stride is
+// between the others.
+struct Product {
+    const void *p, *q;
+    int64_t m, n, k;
+    int64_t p_stride, q_stride;
+    int32_t p_by_rows, q_by_rows;
+    int32_t type;
+    Epilogue e;
+};
+
+// bytes of working memory of an m by n product of k sums (0: none), and the product
+size_t product_work(int64_t m, int64_t n, int64_t k);
+bool product_fits(int64_t m, int64_t n, int64_t k);      // one launch takes it
+hipError_t launch_product(const Product &p, void *work, hipStream_t s);
+
+// sums over the rows of an array (type, rows) into out (out_type), with
+// column_sum_work bytes
+size_t column_sum_work(int64_t rows, int64_t cols);
+hipError_t launch_column_sum(const void *x, int64_t stride, int64_t rows, int64_t cols, int32_t type, void *out, int32_t out_type,
+                             void *work, hipStream_t s);
+
+// dz = dy * act'(z)
+hipError_t launch_act_grad(const dd_act_grad_args &a, hipStream_t s);
+
+// dropout (k_dropout.hip)
+hipError_t launch_dropout(const dd_dropout_args &a, hipStream_t s);
+
+// embedding (k_embed.hip)
+hipError_t launch_embed(const dd_embed_args &a, hipStream_t s);
+size_t embed_grad_work(int64_t tokens, int64_t vocab, int64_t cols);
+hipError_t launch_embed_grad(const dd_embed_grad_args &a, void *work, hipStream_t s);
+
+}  // namespace dd

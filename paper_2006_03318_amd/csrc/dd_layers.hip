@@ -1,0 +1,235 @@
+// C-ABI of a layer's product and its gradient, of dropout and of the embedding:
+// argument checks, working memory, and which passes run.
+
+#include "dd_layers.h"
+
+#include <math.h>
+#include <string.h>
+
+#include "dd_args.h"
+
+namespace {
+
+using dd::aligned;
+using dd::check_rows;
+using dd::fail;
+using dd::float_type;
+using dd::guarded;
+using dd::hip_fail;
+
+constexpr int64_t kMost = int64_t(1) << 31;
+
+bool act_type(int32_t act) { return act >= DD_ACT_NONE && act <= DD_ACT_SILU; }
+
+// f(work) with `need` bytes of the caller's working memory or, if that is NULL, of the
+// library's for the time of the call (a graph would keep writing to it: refused).
+template <class F>
+dd_status with_work(void *given, size_t need, hipStream_t s, const char *what, const F &f) {
+    if (!aligned(given, 16)) return fail(DD_EINVAL, "work is not aligned to 16 bytes");
+    void *taken = nullptr;
+    hipError_t e = hipSuccess;
+    if (need && !given) {
+        bool graph = false;
+        e = dd::captured(s, &graph);
+        if (e != hipSuccess) return hip_fail(e, what);
+        if (graph) return fail(DD_EINVAL, "a captured %s of this size needs work from the caller", what);
+        e = dd::dalloc(&taken, need, s);
+        if (e != hipSuccess) return hip_fail(e, what);
+        given = taken;
+    }
+    e = f(given);
+    dd::dfree(taken, s);
+    return e == hipSuccess ? DD_OK : hip_fail(e, what);
+}
+
+dd_status check_layer(int64_t rows, int64_t k, int64_t n, int32_t type, int32_t bias_type, int32_t turned) {
+    if (rows < 0 || k < 1 || n < 1) return fail(DD_EINVAL, "rows must be at least 0, k and n at least 1");
+    if (rows >= kMost || k >= kMost || n >= kMost) return fail(DD_EINVAL, "rows, k and n must be below 2^31");
+    if (type != DD_BF16 && type != DD_F16) return fail(DD_EINVAL, "type must be DD_BF16 or DD_F16 (got %d)", type);
+    if (bias_type != DD_F32 && bias_type != type) return fail(DD_EINVAL, "bias_type must be DD_F32 or type");
+    if (turned != 0 && turned != 1) return fail(DD_EINVAL, "turned must be 0 or 1");
+    return DD_OK;
+}
+
+dd_status check_product(int64_t m, int64_t n, int64_t k) {
+    return dd::product_fits(m, n, k) ? DD_OK : fail(DD_EINVAL, "a product of %lld by %lld is too large for one launch", (long long)m, (long long)n);
+}
+
+bool sizes_known(int64_t rows, int64_t k, int64_t n) { return rows >= 0 && k >= 1 && n >= 1 && rows < kMost && k < kMost && n < kMost; }
+
+dd_status check_table(int64_t tokens, int64_t vocab, int64_t cols, int32_t type, const void *ids, int32_t id_bytes, float scale, int32_t reserved) {
+    if (tokens < 0 || vocab < 1 || cols < 1) return fail(DD_EINVAL, "tokens must be at least 0, vocab and cols at least 1");
+    if (tokens >= (int64_t(1) << 28) || vocab >= kMost || cols >= kMost)
+        return fail(DD_EINVAL, "tokens must be below 2^28, vocab and cols below 2^31");
+    if (!float_type(type)) return fail(DD_EINVAL, "unknown type %d", type);
+    if (id_bytes != 8 && id_bytes != 4) return fail(DD_EINVAL, "id_bytes must be 8 or 4");
+    if (tokens > 0 && (!ids || !aligned(ids, id_bytes))) return fail(DD_EINVAL, "ids is NULL or not aligned to its elements");
+    if (isnan(scale)) return fail(DD_EINVAL, "scale is not a number");
+    if (reserved) return fail(DD_EINVAL, "reserved must be 0");
+    return DD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dd_linear_work(int64_t rows, int64_t k, int64_t n) { return sizes_known(rows, k, n) && rows > 0 ? dd::product_work(rows, n, k) : 0; }
+
+dd_status dd_linear(const dd_linear_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
+        if (!act_type(a->act)) return fail(DD_EINVAL, "unknown act %d", a->act);
+        if (!aligned(a->bias, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "bias is not aligned to its elements");
+        if (a->rows == 0) return DD_OK;
+        CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
+        CHECK(check_rows("w", a->w, a->turned ? a->n : a->k, a->turned ? a->k : a->n, a->w_stride, a->type, false));
+        if (a->residual) CHECK(check_rows("residual", a->residual, a->rows, a->n, a->residual_stride, a->type, false));
+        CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
+        if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
+        CHECK(check_product(a->rows, a->n, a->k));
+        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, {}};
+        p.e.bias = a->bias;
+        p.e.bias_type = a->bias_type;
+        p.e.act = a->act;
+        p.e.residual = a->residual;
+        p.e.residual_stride = a->residual_stride;
+        p.e.z = a->z;
+        p.e.z_stride = a->z_stride;
+        p.e.out = a->y;
+        p.e.out_stride = a->y_stride;
+        hipStream_t s = (hipStream_t)stream;
+        return with_work(a->work, dd::product_work(a->rows, a->n, a->k), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
+    });
+}
+
+size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
+    if (!sizes_known(rows, k, n)) return 0;
+    size_t most = dd::column_sum_work(rows, n);
+    for (size_t x : {rows > 0 ? dd::product_work(rows, k, n) : 0, dd::product_work(k, n, rows), dd::product_work(n, k, rows)}) most = x > most ? x : most;
+    return most;
+}
+
+dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
+        if (!act_type(a->in_act)) return fail(DD_EINVAL, "unknown in_act %d", a->in_act);
+        if (!a->in_z && a->in_act != DD_ACT_NONE) return fail(DD_EINVAL, "in_act needs in_z");
+        const int64_t wr = a->turned ? a->n : a->k, wc = a->turned ? a->k : a->n;
+        if (a->rows > 0) {
+            if (a->dx || a->dw || a->db) CHECK(check_rows("dy", a->dy, a->rows, a->n, a->dy_stride, a->type, false));
+            if (a->dw) CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
+            if (a->dx) {
+                CHECK(check_rows("w", a->w, wr, wc, a->w_stride, a->type, false));
+                if (a->in_z) CHECK(check_rows("in_z", a->in_z, a->rows, a->k, a->in_z_stride, a->type, false));
+                CHECK(check_rows("dx", a->dx, a->rows, a->k, a->dx_stride, a->type, true));
+                CHECK(check_product(a->rows, a->k, a->n));
+            }
+        }
+        if (a->dw) {
+            CHECK(check_rows("dw", a->dw, wr, wc, a->dw_stride, a->type, true));
+            CHECK(check_product(wr, wc, a->rows));
+        }
+        if (!aligned(a->db, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "db is not aligned to its elements");
+        hipStream_t s = (hipStream_t)stream;
+        size_t need = 0;
+        auto needs = [&](size_t x) { need = x > need ? x : need; };
+        if (a->dw) needs(dd::product_work(wr, wc, a->rows));
+        if (a->db) needs(dd::column_sum_work(a->rows, a->n));
+        if (a->dx && a->rows > 0) needs(dd::product_work(a->rows, a->k, a->n));
+        return with_work(a->work, need, s, "linear gradient", [&](void *work) {
+            hipError_t e = hipSuccess;
+            if (a->dw) {
+                dd::Product p{a->x, a->dy, wr, wc, a->rows, a->x_stride, a->dy_stride, 0, 0, a->type, {}};
+                if (a->turned) {
+                    p.p = a->dy;
+                    p.p_stride = a->dy_stride;
+                    p.q = a->x;
+                    p.q_stride = a->x_stride;
+                }
+                p.e.out = a->dw;
+                p.e.out_stride = a->dw_stride;
+                e = dd::launch_product(p, work, s);
+            }
+            if (e == hipSuccess && a->db) e = dd::launch_column_sum(a->dy, a->dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
+            if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
+                dd::Product p{a->dy, a->w, a->rows, a->k, a->n, a->dy_stride, a->w_stride, 1, !a->turned, a->type, {}};
+                p.e.in_z = a->in_z;
+                p.e.in_z_stride = a->in_z_stride;
+                p.e.in_act = a->in_act;
+                p.e.out = a->dx;
+                p.e.out_stride = a->dx_stride;
+                e = dd::launch_product(p, work, s);
+            }
+            return e;
+        });
+    });
+}
+
+dd_status dd_act_grad(const dd_act_grad_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        if (a->rows < 0 || a->cols < 1) return fail(DD_EINVAL, "rows must be at least 0 and cols at least 1");
+        if (a->rows >= kMost || a->cols >= kMost) return fail(DD_EINVAL, "rows and cols must be below 2^31");
+        if (!float_type(a->type)) return fail(DD_EINVAL, "unknown type %d", a->type);
+        if (!act_type(a->act)) return fail(DD_EINVAL, "unknown act %d", a->act);
+        if (a->rows == 0) return DD_OK;
+        CHECK(check_rows("dy", a->dy, a->rows, a->cols, a->dy_stride, a->type, false));
+        CHECK(check_rows("z", a->z, a->rows, a->cols, a->z_stride, a->type, false));
+        CHECK(check_rows("dz", a->dz, a->rows, a->cols, a->dz_stride, a->type, true));
+        const hipError_t e = dd::launch_act_grad(*a, (hipStream_t)stream);
+        return e == hipSuccess ? DD_OK : hip_fail(e, "activation gradient");
+    });
+}
+
+dd_status dd_dropout(const dd_dropout_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        if (a->rows < 0 || a->cols < 1) return fail(DD_EINVAL, "rows must be at least 0 and cols at least 1");
+        if (a->rows >= kMost || a->cols >= kMost) return fail(DD_EINVAL, "rows and cols must be below 2^31");
+        if (!float_type(a->type)) return fail(DD_EINVAL, "unknown type %d", a->type);
+        if (!(a->p >= 0.0 && a->p <= 1.0)) return fail(DD_EINVAL, "p must lie in [0, 1]");
+        if (!a->d_state || !aligned(a->d_state, 8) || !aligned(a->d_used, 8)) return fail(DD_EINVAL, "d_state is NULL, or it or d_used not aligned to 8 bytes");
+        if (a->d_used == a->d_state) return fail(DD_EINVAL, "d_used is d_state");
+        if (a->reserved) return fail(DD_EINVAL, "reserved must be 0");
+        if (a->rows > 0) {
+            CHECK(check_rows("x", a->x, a->rows, a->cols, a->x_stride, a->type, false));
+            if (a->residual) CHECK(check_rows("residual", a->residual, a->rows, a->cols, a->residual_stride, a->type, false));
+            CHECK(check_rows("out", a->out, a->rows, a->cols, a->out_stride, a->type, true));
+        }
+        const hipError_t e = dd::launch_dropout(*a, (hipStream_t)stream);
+        return e == hipSuccess ? DD_OK : hip_fail(e, "dropout");
+    });
+}
+
+dd_status dd_embed(const dd_embed_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        CHECK(check_table(a->tokens, a->vocab, a->cols, a->type, a->ids, a->id_bytes, a->scale, a->reserved));
+        if (a->tokens == 0) return DD_OK;
+        CHECK(check_rows("table", a->table, a->vocab, a->cols, a->table_stride, a->type, false));
+        CHECK(check_rows("out", a->out, a->tokens, a->cols, a->out_stride, a->type, true));
+        const hipError_t e = dd::launch_embed(*a, (hipStream_t)stream);
+        return e == hipSuccess ? DD_OK : hip_fail(e, "embedding");
+    });
+}
+
+size_t dd_embed_grad_work(int64_t tokens, int64_t vocab, int64_t cols) {
+    return sizes_known(tokens, vocab, cols) && tokens < (int64_t(1) << 28) ? dd::embed_grad_work(tokens, vocab, cols) : 0;
+}
+
+dd_status dd_embed_grad(const dd_embed_grad_args *a, void *stream) {
+    return guarded([&] {
+        if (!a) return fail(DD_EINVAL, "args is NULL");
+        CHECK(check_table(a->tokens, a->vocab, a->cols, a->type, a->ids, a->id_bytes, a->scale, a->reserved));
+        if (a->pad < -1 || a->pad >= a->vocab) return fail(DD_EINVAL, "pad must be -1 or a row of the table");
+        if (a->tokens > 0) CHECK(check_rows("dy", a->dy, a->tokens, a->cols, a->dy_stride, a->type, false));
+        CHECK(check_rows("dtable", a->dtable, a->vocab, a->cols, a->dtable_stride, a->type, true));
+        hipStream_t s = (hipStream_t)stream;
+        return with_work(a->work, dd::embed_grad_work(a->tokens, a->vocab, a->cols), s, "embedding gradient",
+                         [&](void *work) { return dd::launch_embed_grad(*a, work, s); });
+    });
+}
+
+}  // extern "C"

@@ -4,27 +4,17 @@
 #include <math.h>
 #include <string.h>
 
-#include <new>
-
-#include "dd_elem.h"
-#include "dd_train.h"
+#include "dd_args.h"
 
 namespace {
 
+using dd::aligned;
+using dd::captured;
+using dd::check_rows;
 using dd::fail;
+using dd::float_type;
+using dd::guarded;
 using dd::hip_fail;
-
-bool float_type(int32_t t) { return t == DD_F32 || t == DD_BF16 || t == DD_F16; }
-
-bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
-
-// Whether work on s goes into a graph.
-hipError_t captured(hipStream_t s, bool *yes) {
-    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
-    const hipError_t e = hipStreamIsCapturing(s, &st);
-    *yes = st != hipStreamCaptureStatusNone;
-    return e;
-}
 
 // A graph has no place among the calls of other streams: one that uses the
 // working memory is captured on the list's own stream.
@@ -58,19 +48,6 @@ hipError_t end_turn(const dd_tensors *t, hipStream_t s) {
     const hipError_t e = dd::note_use(t->uses, t->stream, s);
     if (e == hipSuccess) t->own_turn = s == t->stream;
     return e;
-}
-
-// What every C entry runs in: nothing thrown gets out.
-template <class F>
-dd_status guarded(const F &f) {
-    dd::no_error();
-    try {
-        return f();
-    } catch (const std::bad_alloc &) {
-        return fail(DD_ENOMEM, "out of host memory");
-    } catch (...) {
-        return fail(DD_EHIP, "unexpected failure in host code");
-    }
 }
 
 dd_status check_tensor(int32_t i, const dd_tensor &t) {
@@ -156,16 +133,6 @@ dd_status load_tensors(int32_t count, const dd_tensor *t, hipStream_t s, dd_tens
     return e == hipSuccess ? DD_OK : hip_fail(e, "copy tensor list");
 }
 
-// Rows of an array: where they start, and how far apart.
-dd_status check_rows(const char *name, const void *p, int64_t rows, int64_t cols, int64_t stride, int32_t type, bool output) {
-    if (!p) return fail(DD_EINVAL, "%s is NULL", name);
-    if (!aligned(p, dd::elem_size(type))) return fail(DD_EINVAL, "%s is not aligned to its elements", name);
-    if (rows <= 1) return DD_OK;
-    if (stride < 0 || (output && stride < cols)) return fail(DD_EINVAL, "%s: stride %lld", name, (long long)stride);
-    if (stride > (int64_t(1) << 60) / rows) return fail(DD_EINVAL, "%s: stride %lld is too large", name, (long long)stride);
-    return DD_OK;
-}
-
 dd_status check_norm(int64_t rows, int64_t cols, int32_t type, int32_t weight_type, const void *weight) {
     if (rows < 0 || cols < 1) return fail(DD_EINVAL, "rows must be at least 0 and cols at least 1");
     if (rows >= (int64_t(1) << 31) || cols >= (int64_t(1) << 31)) return fail(DD_EINVAL, "rows and cols must be below 2^31");
@@ -174,12 +141,6 @@ dd_status check_norm(int64_t rows, int64_t cols, int32_t type, int32_t weight_ty
     if (!aligned(weight, dd::elem_size(weight_type))) return fail(DD_EINVAL, "weight is not aligned to its elements");
     return DD_OK;
 }
-
-#define CHECK(x)                          \
-    do {                                  \
-        const dd_status st_ = (x);        \
-        if (st_ != DD_OK) return st_;     \
-    } while (0)
 
 }  // namespace
 

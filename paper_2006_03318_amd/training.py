@@ -1,11 +1,13 @@
-"""The weight update and the normalization for programs that train with torch.
+"""The weight update, the normalization and a block's other kernels for programs that
+train with torch.
 
-`add_rms_norm` is a differentiable function and `Adam` an optimizer, both on
-the calls of `binding` and on torch's current stream.  They are the fused
-forms that the recipes predict: one kernel for the element-wise work around a
-norm (forward and backward), two or three launches for the update of all
-weights (the paper's fused Adam, Sec. 5.1, with the f32 masters of mixed
-precision).
+`add_rms_norm`, `linear`, `mlp`, `Dropout` and `embed` are differentiable
+functions and `Adam` an optimizer, all on the calls of `binding` and on torch's current
+stream.  They are the fused forms that the recipes predict: one kernel for the
+element-wise work around a norm (forward and backward), the activation,
+bias and residual in the products they belong to, two or three launches for the
+update of all weights (the paper's fused Adam, Sec. 5.1, with the f32 masters
+of mixed precision).
 """
 from __future__ import annotations
 
@@ -75,6 +77,192 @@ def add_rms_norm(x, residual=None, weight=None, eps: float = 1e-6):
     if residual is not None and residual.shape != x.shape:
         residual = residual.expand_as(x)
     return _AddRmsNorm.apply(x, residual, weight, eps)
+
+
+def _matrix(w):
+    return w if w.stride(1) == 1 or w.stride(0) == 1 else w.contiguous()
+
+
+def _workspace(size, like):
+    # (torch's memory: in a captured graph it stays the graph's)
+    return torch.empty(size, dtype=torch.uint8, device=like.device) if size else None
+
+
+def _same(t, what, dtype):
+    if t is not None and t.dtype != dtype:
+        raise TypeError("%s is %s, the rows are %s" % (what, t.dtype, dtype))
+
+
+def _linear(x, weight, bias, residual, act, want_z):
+    """(y, z): z where it is wanted."""
+    k, n = weight.shape
+    shape = x.shape[:-1] + (n,)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device)
+    z = torch.empty_like(y) if want_z else None
+    with _on(x, weight, bias, residual):
+        work = _workspace(B.dd_linear_work(x.numel() // k, k, n), x)
+        B.dd_linear(x, weight, y, bias=bias, residual=residual, act=act, z=z, work=work, stream=_stream())
+    return y, z
+
+
+def _linear_grad(dy, x, weight, bias, wanted, in_act="none", in_z=None):
+    """dx, dw and db, those of the three that are wanted."""
+    k, n = weight.shape
+    dx = torch.empty_like(x, memory_format=torch.contiguous_format) if wanted[0] else None
+    dw = torch.empty_like(weight) if wanted[1] else None
+    db = torch.empty_like(bias) if wanted[2] and bias is not None else None
+    if dx is not None or dw is not None or db is not None:
+        with _on(dy, x, weight, bias):
+            work = _workspace(B.dd_linear_grad_work(dy.numel() // n, k, n), dy)
+            B.dd_linear_grad(dy, x, weight, dx=dx, dw=dw, db=db, in_act=in_act, in_z=in_z, work=work, stream=_stream())
+    return dx, dw, db
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, act):
+        x, weight = _rows(x), _matrix(weight)
+        ctx.act = act
+        y, z = _linear(x, weight, bias, None if residual is None else _rows(residual), act,
+                       act != "none" and any(ctx.needs_input_grad[:3]))
+        ctx.save_for_backward(x, weight, bias, z)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias, z = ctx.saved_tensors
+        dz = dy = _rows(dy)
+        if z is not None:
+            dz = torch.empty_like(z)
+            with _on(dy, z):
+                B.dd_act_grad(dy, z, dz, ctx.act, stream=_stream())
+        return (*_linear_grad(dz, x, weight, bias, ctx.needs_input_grad[:3]), dy if ctx.needs_input_grad[3] else None, None)
+
+
+def linear(x, weight, bias=None, act="none", residual=None):
+    """act(x weight + bias) + residual, for x [..., k] and weight [k, n] in bfloat16 or float16 (the
+    transpose of an [n, k] weight as it is); bias in that type or float32.  act: none,
+    relu, gelu, gelu_tanh or silu."""
+    for t, what in ((weight, "weight"), (residual, "residual")):
+        _same(t, what, x.dtype)
+    if residual is not None:
+        residual = residual.expand(x.shape[:-1] + weight.shape[1:])
+    return _Linear.apply(x, weight, bias, residual, act)
+
+
+class _Mlp(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, up, down, bias_up, bias_down, residual, act):
+        x, up, down = _rows(x), _matrix(up), _matrix(down)
+        ctx.act = act
+        a, z = _linear(x, up, bias_up, None, act, act != "none" and any(ctx.needs_input_grad[:5]))
+        y, _ = _linear(a, down, bias_down, None if residual is None else _rows(residual), "none", False)
+        ctx.save_for_backward(x, up, down, bias_up, bias_down, z, a)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, up, down, bias_up, bias_down, z, a = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dy = _rows(dy)
+        first = need[0] or need[1] or need[3]
+        dz, ddown, dbias_down = _linear_grad(dy, a, down, bias_down, (first, need[2], need[4]), ctx.act, z)
+        dx = dup = dbias_up = None
+        if first:
+            dx, dup, dbias_up = _linear_grad(dz, x, up, bias_up, (need[0], need[1], need[3]))
+        return dx, dup, ddown, dbias_up, dbias_down, dy if need[5] else None, None
+
+
+def mlp(x, up, down, bias_up=None, bias_down=None, act="gelu", residual=None):
+    """linear(linear(x, up, bias_up, act), down, bias_down, residual=residual), whose gradient
+    multiplies with the activation's derivative in the product that comes to it."""
+    for t, what in ((up, "up"), (down, "down"), (residual, "residual")):
+        _same(t, what, x.dtype)
+    if residual is not None:
+        residual = residual.expand(x.shape[:-1] + down.shape[1:])
+    return _Mlp.apply(x, up, down, bias_up, bias_down, residual, act)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, state, call):
+        x = _rows(x)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        used = torch.empty_like(state)
+        with _on(x, residual, state):
+            B.dd_dropout(x, None if residual is None else _rows(residual), p, state, out, call=call, used=used, stream=_stream())
+        ctx.p = p
+        ctx.save_for_backward(used)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        used, = ctx.saved_tensors
+        dx = None
+        if ctx.needs_input_grad[0]:
+            rows = _rows(dy)
+            dx = torch.empty_like(rows, memory_format=torch.contiguous_format)
+            with _on(rows, used):
+                B.dd_dropout(rows, None, ctx.p, used, dx, stream=_stream())
+        return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
+
+
+class Dropout:
+    """The dropouts of a model: drop(x, p, residual) is residual + x / (1 - p) where
+    the generator keeps x.  Every call has a mask of its own, which the gradient makes
+    again; p counts in 65,536ths.  The generator's key and counter are on the GPU
+    (`state`): `step()`, once an iteration, moves the counter behind the calls made
+    so far, and is captured with them where an iteration is captured, so that every replay has
+    other masks."""
+
+    def __init__(self, seed: int = 0, device="cuda"):
+        key = seed & (1 << 64) - 1
+        self.state = torch.tensor([key - (1 << 64) if key >> 63 else key, 0], dtype=torch.int64, device=device)
+        self.calls = 0
+
+    def __call__(self, x, p: float, residual=None):
+        _same(residual, "residual", x.dtype)
+        if residual is not None:
+            residual = residual.expand_as(x)
+        call, self.calls = self.calls, self.calls + 1
+        return _Dropout.apply(x, residual, p, self.state, call)
+
+    def step(self):
+        self.state[1:].add_(self.calls)
+        self.calls = 0
+
+
+class _Embed(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale, pad):
+        ids, table = ids.contiguous(), _rows(table)
+        out = torch.empty(ids.shape + table.shape[1:], dtype=table.dtype, device=table.device)
+        with _on(table, ids):
+            B.dd_embed(ids, table, out, scale=scale, stream=_stream())
+        ctx.save_for_backward(ids)
+        ctx.table = table.shape, scale, pad
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        ids, = ctx.saved_tensors
+        shape, scale, pad = ctx.table
+        dy = _rows(dy)
+        dtable = torch.empty(shape, dtype=dy.dtype, device=dy.device)
+        with _on(dy, ids):
+            work = _workspace(B.dd_embed_grad_work(ids.numel(), *shape), dy)
+            B.dd_embed_grad(ids, dy, dtable, scale=scale, pad=pad, work=work, stream=_stream())
+        return None, dtable, None, None
+
+
+def embed(ids, table, scale: float = 1.0, pad: int = -1):
+    """scale * table[ids], for int64 or int32 ids of any shape.  The row `pad` (-1: none) gets no
+    gradient.  An id that the table does not have gives a row of NaNs, and no gradient."""
+    return _Embed.apply(ids, table, float(scale), int(pad))
 
 
 class Adam:
