@@ -11,11 +11,11 @@ typedef dd_linear_grad_args LinearGradArgs;
 
 // What becomes of a sum s of products before it is stored (k_linear.hip):
 //   t = s + bias,  z = t,  out = act(t) + residual     or
-//   out = s * act'(in_z)
+//   out = s * in_act'(in_z)
 struct Epilogue {
-    const void *bias, *residual, *in_z;
+    const void *bias, *residual, *in_z;     // (the last two: one of them at most)
     void *z, *out;
-    int64_t residual_stride, in_z_stride, z_stride, out_stride;
+    int64_t side_stride, z_stride, out_stride;      // (the first: of residual or in_z)
     int32_t bias_type, act, in_act;
 };
 

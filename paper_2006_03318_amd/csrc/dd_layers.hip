@@ -93,7 +93,7 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         p.e.bias_type = a->bias_type;
         p.e.act = a->act;
         p.e.residual = a->residual;
-        p.e.residual_stride = a->residual_stride;
+        p.e.side_stride = a->residual_stride;
         p.e.z = a->z;
         p.e.z_stride = a->z_stride;
         p.e.out = a->y;
@@ -156,7 +156,7 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
                 dd::Product p{a->dy, a->w, a->rows, a->k, a->n, a->dy_stride, a->w_stride, 1, !a->turned, a->type, {}};
                 p.e.in_z = a->in_z;
-                p.e.in_z_stride = a->in_z_stride;
+                p.e.side_stride = a->in_z_stride;
                 p.e.in_act = a->in_act;
                 p.e.out = a->dx;
                 p.e.out_stride = a->dx_stride;

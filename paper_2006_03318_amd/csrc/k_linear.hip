@@ -87,23 +87,35 @@ __device__ __forceinline__ void by_act(int32_t act, const F &f) {
     else if (act == DD_ACT_SILU) f(std::integral_constant<int, DD_ACT_SILU>{});
 }
 
+// What eight sums of a row need beside them, loaded ahead: the residual's or in_z's (an
+// epilogue has one of them at most).
+template <class T>
+__device__ __forceinline__ void load_side(const Epilogue &e, int64_t i, int64_t j, int have, Pack<T, 8> &side) {
+    const T *p = static_cast<const T *>(e.residual ? e.residual : e.in_z);
+    if (p) side.load(p + i * e.side_stride + j, have);
+}
+template <class T>
+__device__ __forceinline__ void load_bias(const Epilogue &e, int64_t j, int have, float (&x)[8]) {
+    if (!e.bias) {
+#pragma unroll
+        for (int c = 0; c < 8; c++) x[c] = 0.0f;
+    } else if (e.bias_type == DD_F32) {
+        Pack<float, 8> b;
+        b.load(static_cast<const float *>(e.bias) + j, have);
+        b.to(x);
+    } else {
+        Pack<T, 8> b;
+        b.load(static_cast<const T *>(e.bias) + j, have);
+        b.to(x);
+    }
+}
 // Eight sums of row i from column j on, of which `have` are in the output.
 template <class T>
-__device__ __forceinline__ void finish(const Epilogue &e, int64_t i, int64_t j, int have, float (&v)[8]) {
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t i, int64_t j, int have, float (&v)[8], const float (&bias)[8], const Pack<T, 8> &side) {
     Pack<T, 8> p;
     float x[8];
-    if (e.bias) {
-        if (e.bias_type == DD_F32) {
-            Pack<float, 8> b;
-            b.load(static_cast<const float *>(e.bias) + j, have);
-            b.to(x);
-        } else {
-            p.load(static_cast<const T *>(e.bias) + j, have);
-            p.to(x);
-        }
 #pragma unroll
-        for (int c = 0; c < 8; c++) v[c] += x[c];
-    }
+    for (int c = 0; c < 8; c++) v[c] += bias[c];
     if (e.z) {
         p.from(v);
         p.store(static_cast<T *>(e.z) + i * e.z_stride + j, have);
@@ -113,14 +125,11 @@ __device__ __forceinline__ void finish(const Epilogue &e, int64_t i, int64_t j, 
         for (int c = 0; c < 8; c++) v[c] = act_of<decltype(act)::value>(v[c]);
     });
     if (e.residual) {
-        p.load(static_cast<const T *>(e.residual) + i * e.residual_stride + j, have);
-        p.to(x);
+        side.to(x);
 #pragma unroll
         for (int c = 0; c < 8; c++) v[c] += x[c];
-    }
-    if (e.in_z) {
-        p.load(static_cast<const T *>(e.in_z) + i * e.in_z_stride + j, have);
-        p.to(x);
+    } else if (e.in_z) {
+        side.to(x);
         by_act(e.in_act, [&](auto act) {
 #pragma unroll
             for (int c = 0; c < 8; c++) v[c] *= slope_of<decltype(act)::value>(x[c]);
@@ -156,25 +165,39 @@ struct Tile {
         row = ROWS ? line : 8 * c;
         l = ROWS ? 8 * c : line;
     }
-    // 16 rows from `row` on (TURN: matrix instruction s of 32 rows) of sums 32 h to 32 h + 31:
-    // a lane gets row lane % 16, sums 8 (lane / 16) and on
-    static __device__ __forceinline__ s8 fragment(uint32_t at, int lane, int row, int s, int h) {
+    // Fragments: 16 rows (TURN: matrix instruction s of 32) of sums 32 h to 32 h + 31; a lane gets row lane %
+    // 16, sums 8 (lane / 16) and on.  They are numbered from the wave's first row on, which is a
+    // multiple of all their rows; base() is the lane's place in the first.  A later one's place differs by a
+    // constant or, where chunks are permuted by more than the line, in a few bits.
+    static __device__ __forceinline__ uint32_t base(int lane, int first) {
         const int r = lane & 15, g = lane >> 4;
         if (ROWS) {
-            const int line = row + (TURN ? (r >> 2) * 8 + 4 * s + (r & 3) : r);
-            const int c = (4 * h + g) ^ turn(line);
-            return *(lptr<const s8>)(uintptr_t)(at + line * (BK * 2) + c * 16);
+            const int line = first + (TURN ? (r >> 2) * 8 + (r & 3) : r);
+            return line * (BK * 2) + (g ^ turn(line)) * 16;
         }
         // read and transposed: lane 4 a + b of sixteen gives four rows' values of one sum, and
         // gets those of four sums for its row
-        const int line = 32 * h + 8 * g + (r >> 2);
-        const int first = row + (TURN ? 8 * (r & 3) + 4 * s : 4 * (r & 3));
-        const uint32_t p = at + line * (N * 2) + ((first >> 3) ^ turn(line)) * 16 + (first & 7) * 2;
+        const int line = 8 * g + (r >> 2), row = first + (TURN ? 8 : 4) * (r & 3);
+        return line * (N * 2) + ((row >> 3) ^ turn(line)) * 16 + (row & 7) * 2;
+    }
+    static __device__ __forceinline__ s8 fragment(uint32_t at, int i, int s, int h) {
+        if (ROWS) {
+            const uint32_t p = (at ^ h * 64) + (TURN ? i * 32 + s * 4 : i * 16) * (BK * 2);
+            return *(lptr<const s8>)(uintptr_t)(p);
+        }
+        const uint32_t p = (at ^ i * (TURN ? 64 : 32)) + h * 32 * (N * 2) + s * 8;
         const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr<s4>)(uintptr_t)(p));
         const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr<s4>)(uintptr_t)(p + 4 * (N * 2)));
         return s8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
     }
 };
+
+// x, about which the compiler forgets what it knows: what is made of it is not kept
+// in registers from before a loop.
+__device__ __forceinline__ int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
 // A wave's loads of one operand's tiles.  DIRECT: to LDS, without registers; the
 // operand is aligned to 16 bytes, and rows beyond its end and sums beyond l are read at
@@ -189,7 +212,9 @@ struct Loads {
     int64_t stride;
     int rows, lane, wave;        // rows: that the operand has from the tile's first on
 
-    static __device__ __forceinline__ int number(int wave, int j) { return (wave * kCount + j) % TILE::kLoads; }
+    static __device__ __forceinline__ int number(int wave, int j) {
+        return kCount * WAVES == TILE::kLoads ? wave * kCount + j : (wave * kCount + j) % TILE::kLoads;
+    }
     __device__ __forceinline__ void init(const T *p, int64_t ld, int64_t first, int64_t count) {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -197,32 +222,33 @@ struct Loads {
         base = p + (ROWS ? first * ld : first);
         rows = count - first < (1 << 20) ? (int)(count - first) : 1 << 20;
         if (DIRECT) {
+            const int mine = fresh(lane);
 #pragma unroll
             for (int j = 0; j < kCount; j++) {
                 int row, l;
-                TILE::source(number(wave, j), lane, row, l);
+                TILE::source(number(wave, j), mine, row, l);
                 off[j] = row < rows ? (uint32_t)((ROWS ? row * ld + l : l * ld + row) * 2) : 0x80000000u;
             }
         }
     }
     // the last tile has fewer sums: those beyond them read as zeros
     __device__ __forceinline__ void cut(int64_t left) {
+        const int mine = fresh(lane);
 #pragma unroll
         for (int j = 0; j < kCount; j++) {
             int row, l;
-            TILE::source(number(wave, j), lane, row, l);
+            TILE::source(number(wave, j), mine, row, l);
             if (l >= left) off[j] = 0x80000000u;
         }
     }
-    __device__ __forceinline__ i4 buffer(int64_t l0) const {
-        const uint64_t b = (uint64_t)(uintptr_t)(base + (ROWS ? l0 : l0 * stride));
-        return i4{(int)(uint32_t)b, (int)(uint32_t)(b >> 32 & 0xffff), (int)0x80000000u, 0x00020000};
-    }
-    // load j of the tile in `from`, to LDS at `to`
-    __device__ __forceinline__ void direct(const i4 &from, uint32_t to, int j) const {
+    __device__ __forceinline__ uint64_t from(int64_t l0) const { return (uint64_t)(uintptr_t)(base + (ROWS ? l0 : l0 * stride)); }
+    // load j of the tile that begins at `from`, to LDS at `to`
+    __device__ __forceinline__ void direct(uint64_t from, uint32_t to, int j) const {
+        const i4 buffer = {__builtin_amdgcn_readfirstlane((int)(uint32_t)from), __builtin_amdgcn_readfirstlane((int)(uint32_t)(from >> 32)),
+                           (int)0x80000000u, 0x00020000};
         // (m0 is the place in LDS, which nothing else here uses; one wait state before the load that does)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
-                     "v"(off[j]), "s"(from));
+                     "v"(off[j]), "s"(buffer));
     }
     __device__ __forceinline__ void load(int64_t l0, int64_t left) {
 #pragma unroll
@@ -257,187 +283,228 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn, int splits) {
     return {first + t % down, t / down, split};
 }
 
-template <class T, bool PROWS, bool QROWS, int BM, int BN, int BK, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4 > 0 ? PER_CU * WM * WN / 4 : 1)
+// A workgroup has tile blockIdx.x and every gridDim.x-th after it.  Their steps, of BK sums each,
+// are one sequence: while a step's fragments are multiplied, the next one's are read from LDS and a
+// later one's tiles are loaded to it, across the end of a tile too, whose epilogue runs while the
+// next one's loads are under way and the stores of the last go out.
+template <class T, bool PROWS, bool QROWS, int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
     k_product(Product a, float *part, int tm, int tn, int splits, int64_t k_part) {
-    constexpr int kWaves = WM * WN, WTM = BM / WM, WTN = BN / WN, MT = WTM / 16, NT = WTN / 32, H = BK / 32;
+    constexpr int BK = 64, kWaves = WM * WN, WTM = BM / WM, WTN = BN / WN, MT = WTM / 16, NT = WTN / 32;
     typedef Tile<PROWS, false, BM, BK> PTile;
     typedef Tile<QROWS, true, BN, BK> QTile;
     typedef Loads<T, PTile, PROWS, kWaves, DIRECT> PLoads;
     typedef Loads<T, QTile, QROWS, kWaves, DIRECT> QLoads;
-    constexpr int kStage = PTile::kBytes + QTile::kBytes;
+    constexpr int kStage = PTile::kBytes + QTile::kBytes, kOut = 16 * WTN * 4;
+    constexpr int kLoads = PLoads::kCount + QLoads::kCount;
     static_assert(DIRECT || STAGES == 2, "stages");
-    __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage];
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage + kWaves * kOut];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr<char>)(lds);
-
-    const Place at = place_of(blockIdx.x, tm, tn, splits);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    const int64_t m0 = (int64_t)at.m * BM, n0 = (int64_t)at.n * BN;
-    const int64_t k0 = at.split * k_part, k1 = k0 + k_part < a.k ? k0 + k_part : a.k;
-    const int nk = (int)((k1 - k0 + BK - 1) / BK);
+    const int tiles = tm * tn * splits;
+    auto sums_of = [&](const Place &at, int64_t &k0, int64_t &k1) __attribute__((always_inline)) {
+        k0 = at.split * k_part;
+        k1 = k0 + k_part < a.k ? k0 + k_part : a.k;
+        return k1 - k0 > BK ? (int)((k1 - k0 + BK - 1) / BK) : 1;     // steps (one, if there are no sums)
+    };
 
+    // The step whose loads come next: what is left of its tile, and where its operands lie.  Behind the last
+    // tile's last step, zeros are loaded, without a trip to memory.
     PLoads lp;
     QLoads lq;
-    lp.init(static_cast<const T *>(a.p), a.p_stride, m0, a.m);
-    lq.init(static_cast<const T *>(a.q), a.q_stride, n0, a.n);
-
-    f4 acc[MT][NT][2];
-#pragma unroll
-    for (int i = 0; i < MT; i++)
-#pragma unroll
-        for (int j = 0; j < NT; j++) acc[i][j][0] = acc[i][j][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    s8 fp[2][MT], fq[2][NT][2];
-
-    // tile t's loads: all of them, or (direct) part i of n
-    auto issue = [&](int t) __attribute__((always_inline)) {
-        const int64_t l0 = k0 + (int64_t)t * BK;
-        lp.load(l0, k1 - l0);
-        lq.load(l0, k1 - l0);
-    };
-    i4 from_p, from_q;
-    auto begin_issue = [&](int t) __attribute__((always_inline)) {
-        const int64_t l0 = k0 + (int64_t)t * BK;
-        from_p = lp.buffer(l0);
-        from_q = lq.buffer(l0);
-        if (k1 - l0 < BK) {
-            lp.cut(k1 - l0);
-            lq.cut(k1 - l0);
+    uint64_t from_p = 0, from_q = 0;
+    int load_tile = blockIdx.x, load_left = 0;
+    int64_t load_l = 0, load_end = 0;
+    const int64_t by_p = PROWS ? BK * 2 : a.p_stride * (BK * 2), by_q = QROWS ? BK * 2 : a.q_stride * (BK * 2);
+    auto next_load = [&]() __attribute__((always_inline)) {
+        load_left--;
+        load_l += BK;
+        if (DIRECT) {
+            from_p += (uint64_t)by_p;
+            from_q += (uint64_t)by_q;
+        }
+        if (load_left <= 1) {
+            if (load_left <= 0 && load_tile < tiles) {
+                const Place at = place_of(load_tile, tm, tn, splits);
+                load_left = sums_of(at, load_l, load_end);
+                lp.init(static_cast<const T *>(a.p), a.p_stride, (int64_t)at.m * BM, a.m);
+                lq.init(static_cast<const T *>(a.q), a.q_stride, (int64_t)at.n * BN, a.n);
+                load_tile += gridDim.x;
+                if (DIRECT) {
+                    from_p = lp.from(load_l);
+                    from_q = lq.from(load_l);
+                }
+            }
+            if (DIRECT && load_left <= 1) {
+                lp.cut(load_left == 1 ? load_end - load_l : 0);
+                lq.cut(load_left == 1 ? load_end - load_l : 0);
+            }
+        }
+        if (!DIRECT) {
+            const int64_t left = load_left > 0 ? load_end - load_l : 0;
+            lp.load(load_l, left);
+            lq.load(load_l, left);
         }
     };
-    constexpr int kLoads = PLoads::kCount + QLoads::kCount, kReads = MT + 2 * NT;
-    auto part_of_issue = [&](uint32_t slot, int i, int n) __attribute__((always_inline)) {
+
+    // A step is two halves of 32 sums, each of MT chunks: 16 rows of p times the wave's columns.  A chunk's
+    // fragment of p is followed, where it was, by that of the chunk a half later; q's of the half
+    // to come are held beside those in use.  Within the second half the waves meet: all have read the step's
+    // fragments (its slot is free for the loads of a later step), and the next step's tiles are in LDS.
+    f4 acc[MT][NT][2];
+    s8 fp[MT], fq[2][NT][2];
+    const uint32_t base_p = lds0 + PTile::base(lane, wm * WTM), base_q = lds0 + PTile::kBytes + QTile::base(lane, wn * WTN);
+    auto read_p = [&](uint32_t slot, int h, int i) __attribute__((always_inline)) { fp[i] = PTile::fragment(base_p + slot, i, 0, h); };
+    // those of q that go with chunk i of n
+    auto read_q = [&](uint32_t slot, int h, int i, int n) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2 * NT; j++)
+            if (j * n / (2 * NT) == i) fq[h][j / 2][j % 2] = QTile::fragment(base_q + slot, j / 2, j % 2, h);
+    };
+    auto read_first = [&](uint32_t slot) __attribute__((always_inline)) {
+        read_q(slot, 0, 0, 1);
+#pragma unroll
+        for (int i = 0; i < MT; i++) read_p(slot, 0, i);
+    };
+    // the loads that go with chunk i of n
+    auto issue = [&](uint32_t to, int i, int n) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kLoads; j++)
             if (j * n / kLoads == i) {
-                if (j < PLoads::kCount) lp.direct(from_p, lds0 + slot, j);
-                else lq.direct(from_q, lds0 + slot + PTile::kBytes, j - PLoads::kCount);
+                if (j < PLoads::kCount) lp.direct(from_p, lds0 + to, j);
+                else lq.direct(from_q, lds0 + to + PTile::kBytes, j - PLoads::kCount);
             }
     };
-    auto part_of_read = [&](uint32_t slot, int h, int set, int i, int n) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < kReads; j++)
-            if (j * n / kReads == i) {
-                if (j < 2 * NT) fq[set][j / 2][j % 2] = QTile::fragment(lds0 + slot + PTile::kBytes, lane, wn * WTN + 32 * (j / 2), j % 2, h);
-                else fp[set][j - 2 * NT] = PTile::fragment(lds0 + slot, lane, wm * WTM + 16 * (j - 2 * NT), 0, h);
-            }
-    };
-    // The products of one set of fragments; between them the reads of the other set (sums h of the
-    // tile in `slot`) and, where there are some, the loads of a later tile to `to`.
-    auto multiply = [&](int set, uint32_t slot, int h, bool loads, uint32_t to) __attribute__((always_inline)) {
-        constexpr int kSpread = MT > 1 ? MT / 2 : 1;
+    // half h, with the reads of the other (from_h, in slot `from`) and the loads to `to`; `meet` is called
+    // behind the first chunk, when the reads before it have had its time to come back
+    auto half = [&](int h, uint32_t from, int from_h, bool loads, uint32_t to, auto meet) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < MT; i++) {
-            part_of_read(slot, h, set ^ 1, i, kSpread);
-            if (loads) part_of_issue(to, i, MT);
+            if (i > 0) {
+                read_q(from, from_h, i, MT);
+                if (loads) issue(to, i, MT);
+            }
 #pragma unroll
             for (int j = 0; j < NT; j++)
 #pragma unroll
-                for (int s = 0; s < 2; s++) acc[i][j][s] = mfma(T{}, fq[set][j][s], fp[set][i], acc[i][j][s]);
+                for (int s = 0; s < 2; s++) acc[i][j][s] = mfma(T{}, fq[h][j][s], fp[i], acc[i][j][s]);
+            if (i == 0) {
+                meet();
+                read_q(from, from_h, 0, MT);
+                if (loads) issue(to, 0, MT);
+            }
+            read_p(from, from_h, i);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Tiles from the last on are loaded and read as zeros, without a trip to memory, so that every
-    // step is alike.
+
     uint32_t slot = 0;
     if (DIRECT) {
 #pragma unroll
         for (int t = 0; t < STAGES; t++) {
-            begin_issue(t);
-            part_of_issue(t * kStage, 0, 1);
+            next_load();
+            issue(t * kStage, 0, 1);
         }
-        // (the first tile is the oldest load)
+        // (the first step's loads are the oldest)
         asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((STAGES - 1) * kLoads) : "memory");
     } else {
-        issue(0);
+        next_load();
         lp.store(lds0);
         lq.store(lds0 + PTile::kBytes);
         __syncthreads();
-        issue(1);
+        next_load();
     }
-    part_of_read(0, 0, 0, 0, 1);
+    read_first(0);
 
-    auto step = [&](int t, int odd) __attribute__((always_inline)) {      // odd: the set that holds its first fragments
-#pragma unroll
-        for (int h = 0; h < H; h++) {
-            const int set = (odd + h) & 1;
-            if (h + 1 < H) {
-                multiply(set, slot, h + 1, false, 0);
-                continue;
-            }
-            const uint32_t to = slot;
-            slot = slot + kStage == STAGES * kStage ? 0 : slot + kStage;
-            // the next tile is in LDS for all waves, and all have read this one: its slot is free
-            if (DIRECT) {
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
-                begin_issue(t + STAGES);
-            } else {
-                lp.store(lds0 + slot);
-                lq.store(lds0 + slot + PTile::kBytes);
-                __syncthreads();
-                issue(t + 2);
-            }
-            multiply(set, slot, 0, DIRECT, to);
-        }
-    };
-    if (H == 1) {
-        for (int t = 0; t < nk; t += 2) {
-            step(t, 0);
-            step(t + 1, 1);
-        }
-    } else {
-        for (int t = 0; t < nk; t++) step(t, 0);
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-
-    // Sums go through LDS, a few rows of the wave's tile at a time, so that a row's columns
-    // are stored by neighbouring lanes and the epilogue is one loop.
-    constexpr int kWaveBytes = STAGES * kStage / kWaves, kFit = kWaveBytes / (WTN * 4) / 16;
-    constexpr int R = kFit >= MT ? MT : kFit >= 8 ? 8 : kFit >= 4 ? 4 : kFit >= 2 ? 2 : 1;      // row tiles at a time
-    constexpr int kLanes = WTN / 8, kRows = 64 / kLanes;
-    static_assert(MT % R == 0 && kFit >= 1, "epilogue");
-    const uint32_t mine = lds0 + wave * kWaveBytes;
-    const int64_t i0 = m0 + wm * WTM, j0 = n0 + wn * WTN;
-    if (splits > 1) part += at.split * a.m * a.n;
-#pragma unroll 1
-    for (int pass = 0; pass < MT / R; pass++) {
+    constexpr int kLanes = WTN / 8, kRows = 64 / kLanes, kTurns = 16 / kRows;      // of the epilogue
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const Place at = place_of(tile, tm, tn, splits);
+        int64_t k0, k1;
+        const int steps = sums_of(at, k0, k1);
 #pragma unroll
         for (int i = 0; i < MT; i++)
-            if (i / R == pass) {
-                const int r = (i % R) * 16 + (lane & 15);
 #pragma unroll
-                for (int j = 0; j < NT; j++)
-#pragma unroll
-                    for (int s = 0; s < 2; s++) {
-                        const int c = (8 * j + 2 * (lane >> 4) + s) ^ (r & (WTN / 4 - 1));
-                        *(lptr<f4>)(uintptr_t)(mine + r * (WTN * 4) + c * 16) = acc[i][j][s];
-                    }
-            }
-        __builtin_amdgcn_wave_barrier();
-        const int64_t j = j0 + 8 * (lane % kLanes);
-        const int have = a.n - j >= 8 ? 8 : (int)(a.n - j);
-#pragma unroll 1
-        for (int r = lane / kLanes; r < 16 * R; r += kRows) {
-            const int64_t i = i0 + pass * (16 * R) + r;
-            float v[8];
-#pragma unroll
-            for (int s = 0; s < 2; s++) {
-                const int c = (2 * (lane % kLanes) + s) ^ (r & (WTN / 4 - 1));
-                const f4 x = *(lptr<const f4>)(uintptr_t)(mine + r * (WTN * 4) + c * 16);
-#pragma unroll
-                for (int b = 0; b < 4; b++) v[4 * s + b] = x[b];
-            }
-            if (i >= a.m || have <= 0) continue;
-            if (splits > 1) {
-                Pack<float, 8> p;
-                p.from(v);
-                p.store(part + i * a.n + j, have);
-            } else {
-                finish<T>(a.e, i, j, have, v);
-            }
+            for (int j = 0; j < NT; j++) acc[i][j][0] = acc[i][j][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < steps; t++) {
+            half(0, slot, 1, false, 0, [] {});
+            const uint32_t to = slot;
+            slot = slot + kStage == STAGES * kStage ? 0 : slot + kStage;
+            if (DIRECT) next_load();
+            half(1, slot, 0, DIRECT, to, [&]() __attribute__((always_inline)) {
+                if (DIRECT) {
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * kLoads) : "memory");
+                } else {
+                    lp.store(lds0 + slot);
+                    lq.store(lds0 + slot + PTile::kBytes);
+                    __syncthreads();
+                    next_load();
+                }
+            });
         }
-        __builtin_amdgcn_wave_barrier();
+
+        // The sums go through LDS, 16 rows of the wave's tile at a time, so that neighbouring lanes store
+        // neighbouring columns and the epilogue is one loop.  What it reads is loaded a turn ahead: loads
+        // and stores are counted in order, and a wait for a load would be one for the stores before it.
+        const uint32_t mine = lds0 + STAGES * kStage + wave * kOut;
+        const int me = fresh(lane);
+        const int64_t i0 = (int64_t)at.m * BM + wm * WTM + me / kLanes, j = (int64_t)at.n * BN + wn * WTN + 8 * (me % kLanes);
+        const int have = a.n - j >= 8 ? 8 : a.n - j < 0 ? 0 : (int)(a.n - j);
+        float bias[8];
+        Pack<T, 8> side[kTurns];
+        if (splits == 1) {
+            load_bias<T>(a.e, j, have, bias);
+#pragma unroll
+            for (int u = 0; u < kTurns; u++) load_side<T>(a.e, i0 + u * kRows, j, i0 + u * kRows < a.m ? have : 0, side[u]);
+        }
+#pragma unroll 1
+        for (int pass = 0; pass < MT; pass++) {
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+                if (i == pass) {
+                    const int r = me & 15;
+#pragma unroll
+                    for (int x = 0; x < NT; x++)
+#pragma unroll
+                        for (int s = 0; s < 2; s++) {
+                            const int c = (8 * x + 2 * (me >> 4) + s) ^ (r & (WTN / 4 - 1));
+                            *(lptr<f4>)(uintptr_t)(mine + r * (WTN * 4) + c * 16) = acc[i][x][s];
+                        }
+                }
+            Pack<T, 8> now[kTurns];
+#pragma unroll
+            for (int u = 0; u < kTurns; u++) {
+                const int64_t i = i0 + (pass + 1) * 16 + u * kRows;
+                now[u] = side[u];
+                if (splits == 1 && pass + 1 < MT) load_side<T>(a.e, i, j, i < a.m ? have : 0, side[u]);
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int u = 0; u < kTurns; u++) {
+                const int r = me / kLanes + u * kRows;
+                const int64_t i = i0 + pass * 16 + u * kRows;
+                float v[8];
+#pragma unroll
+                for (int s = 0; s < 2; s++) {
+                    const int c = (2 * (me % kLanes) + s) ^ (r & (WTN / 4 - 1));
+                    const f4 x = *(lptr<const f4>)(uintptr_t)(mine + r * (WTN * 4) + c * 16);
+#pragma unroll
+                    for (int b = 0; b < 4; b++) v[4 * s + b] = x[b];
+                }
+                if (i >= a.m || have == 0) continue;
+                if (splits > 1) {
+                    Pack<float, 8> p;
+                    p.from(v);
+                    p.store(part + (at.split * a.m + i) * a.n + j, have);
+                } else {
+                    finish<T>(a.e, i, j, have, v, bias, now[u]);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        read_first(slot);     // (again: held through the epilogue, they would cost it their registers)
     }
+    if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (no load to LDS outlives its workgroup)
 }
 
 // The parts of a product whose sums were cut, joined in order.
@@ -457,7 +524,11 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
 #pragma unroll
             for (int c = 0; c < 8; c++) v[c] += x[c];
         }
-        finish<T>(a.e, i, j, have, v);
+        float bias[8];
+        Pack<T, 8> side;
+        load_bias<T>(a.e, j, have, bias);
+        load_side<T>(a.e, i, j, have, side);
+        finish<T>(a.e, i, j, have, v, bias, side);
     }
 }
 
@@ -505,21 +576,21 @@ bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count,
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (by_rows ? k : count) % 8 == 0 && stride < (int64_t(1) << 22);
 }
 
-template <class T, bool PROWS, bool QROWS, int BM, int BN, int BK, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
+template <class T, bool PROWS, bool QROWS, int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
 void run_product(const Product &a, const Plan &p, float *part, hipStream_t s) {
-    k_product<T, PROWS, QROWS, BM, BN, BK, WM, WN, STAGES, PER_CU, DIRECT>
-        <<<(unsigned)((int64_t)p.tm * p.tn * p.splits), 64 * WM * WN, 0, s>>>(a, part, p.tm, p.tn, p.splits, p.k_part);
+    const int tiles = p.tm * p.tn * p.splits, grid = tiles < PER_CU * kUnits ? tiles : PER_CU * kUnits;
+    k_product<T, PROWS, QROWS, BM, BN, WM, WN, STAGES, PER_CU, DIRECT><<<grid, 64 * WM * WN, 0, s>>>(a, part, p.tm, p.tn, p.splits, p.k_part);
 }
 template <class T, bool PROWS, bool QROWS>
 void product(const Product &a, const Plan &p, bool direct, float *part, hipStream_t s) {
     if (direct) {
-        if (p.tile == 16) run_product<T, PROWS, QROWS, 16, 128, 64, 1, 4, 2, 4, true>(a, p, part, s);
-        else if (p.tile == 128) run_product<T, PROWS, QROWS, 128, 128, 64, 2, 2, 2, 2, true>(a, p, part, s);
-        else run_product<T, PROWS, QROWS, 256, 256, 64, 2, 4, 2, 1, true>(a, p, part, s);
+        if (p.tile == 16) run_product<T, PROWS, QROWS, 16, 128, 1, 4, 2, 3, true>(a, p, part, s);
+        else if (p.tile == 128) run_product<T, PROWS, QROWS, 128, 128, 2, 2, 2, 2, true>(a, p, part, s);
+        else run_product<T, PROWS, QROWS, 256, 256, 2, 4, 2, 1, true>(a, p, part, s);
     } else if (p.tile == 16) {
-        run_product<T, PROWS, QROWS, 16, 128, 64, 1, 4, 2, 4, false>(a, p, part, s);
+        run_product<T, PROWS, QROWS, 16, 128, 1, 4, 2, 3, false>(a, p, part, s);
     } else {
-        run_product<T, PROWS, QROWS, 128, 128, 64, 2, 2, 2, 2, false>(a, p, part, s);
+        run_product<T, PROWS, QROWS, 128, 128, 2, 2, 2, 2, false>(a, p, part, s);
     }
 }
 template <class T>
@@ -650,9 +721,9 @@ size_t product_work(int64_t m, int64_t n, int64_t k) {
 }
 
 bool product_fits(int64_t m, int64_t n, int64_t k) {
-    for (bool direct : {true, false}) {       // (fewer than 2^32 threads, and tiles)
+    for (bool direct : {true, false}) {       // (tiles are counted in 32 bits)
         const Plan p = plan_of(m, n, k, direct);
-        if (tiles_of(m, p.tile) * (int64_t)p.tn * p.splits >= (int64_t(1) << 23)) return false;
+        if (tiles_of(m, p.tile) * (int64_t)p.tn * p.splits >= (int64_t(1) << 30)) return false;
     }
     return true;
 }
