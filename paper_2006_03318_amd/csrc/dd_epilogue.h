@@ -1,0 +1,117 @@
+// What becomes of a product's sums: the activations and the epilogue.
+#pragma once
+
+#include <type_traits>
+
+#include "dd_elem.h"
+#include "dd_layers.h"
+
+namespace dd {
+
+// --- activations --------------------------------------------------------------
+// Phi(x) and exp(-x^2 / 2), from Abramowitz and Stegun 7.1.26 (off by 1.5e-7
+// at most).
+__device__ __forceinline__ void normal(float x, float &phi, float &e) {
+    const float a = fabsf(x) * 0.70710678f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.0f));
+    e = __builtin_amdgcn_exp2f(a * a * -1.44269504f);
+    const float s = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
+                                     0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
+    phi = x < 0.0f ? s : 1.0f - s;
+}
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504f));
+}
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+    if (ACT == DD_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;
+    if (ACT == DD_ACT_GELU) {
+        float phi, e;
+        normal(z, phi, e);
+        return z * phi;
+    }
+    if (ACT == DD_ACT_GELU_TANH) return z * sigmoid(z * fmaf(2.0f * 0.7978845608f * 0.044715f, z * z, 2.0f * 0.7978845608f));
+    if (ACT == DD_ACT_SILU) return z * sigmoid(z);
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ float slope_of(float z) {
+    if (ACT == DD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == DD_ACT_GELU) {
+        float phi, e;
+        normal(z, phi, e);
+        return fmaf(z * e, 0.3989422804f, phi);
+    }
+    if (ACT == DD_ACT_GELU_TANH) {
+        const float x = z > 20.0f ? 20.0f : z < -20.0f ? -20.0f : z;     // (x^2 in range; the slope is 0 or 1 there)
+        const float s = sigmoid(x * fmaf(2.0f * 0.7978845608f * 0.044715f, x * x, 2.0f * 0.7978845608f));
+        return fmaf(x * s * (1.0f - s), fmaf(6.0f * 0.7978845608f * 0.044715f, x * x, 2.0f * 0.7978845608f), s);
+    }
+    if (ACT == DD_ACT_SILU) {
+        const float s = sigmoid(z);
+        return s * fmaf(z, 1.0f - s, 1.0f);
+    }
+    return 1.0f;
+}
+// f<ACT>() of the eight values, chosen once for all
+template <class F>
+__device__ __forceinline__ void by_act(int32_t act, const F &f) {
+    if (act == DD_ACT_RELU) f(std::integral_constant<int, DD_ACT_RELU>{});
+    else if (act == DD_ACT_GELU) f(std::integral_constant<int, DD_ACT_GELU>{});
+    else if (act == DD_ACT_GELU_TANH) f(std::integral_constant<int, DD_ACT_GELU_TANH>{});
+    else if (act == DD_ACT_SILU) f(std::integral_constant<int, DD_ACT_SILU>{});
+}
+
+// What eight sums of a row need beside them, loaded ahead: the residual's or in_z's (an
+// epilogue has one of them at most).
+template <class T>
+__device__ __forceinline__ void load_side(const Epilogue &e, int64_t i, int64_t j, int have, Pack<T, 8> &side) {
+    const T *p = static_cast<const T *>(e.residual ? e.residual : e.in_z);
+    if (p) side.load(p + i * e.side_stride + j, have);
+}
+template <class T>
+__device__ __forceinline__ void load_bias(const Epilogue &e, int64_t j, int have, float (&x)[8]) {
+    if (!e.bias) {
+#pragma unroll
+        for (int c = 0; c < 8; c++) x[c] = 0.0f;
+    } else if (e.bias_type == DD_F32) {
+        Pack<float, 8> b;
+        b.load(static_cast<const float *>(e.bias) + j, have);
+        b.to(x);
+    } else {
+        Pack<T, 8> b;
+        b.load(static_cast<const T *>(e.bias) + j, have);
+        b.to(x);
+    }
+}
+// Eight sums of row i from column j on, of which `have` are in the output.
+template <class T>
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t i, int64_t j, int have, float (&v)[8], const float (&bias)[8], const Pack<T, 8> &side) {
+    Pack<T, 8> p;
+    float x[8];
+#pragma unroll
+    for (int c = 0; c < 8; c++) v[c] += bias[c];
+    if (e.z) {
+        p.from(v);
+        p.store(static_cast<T *>(e.z) + i * e.z_stride + j, have);
+    }
+    by_act(e.act, [&](auto act) {
+#pragma unroll
+        for (int c = 0; c < 8; c++) v[c] = act_of<decltype(act)::value>(v[c]);
+    });
+    if (e.residual) {
+        side.to(x);
+#pragma unroll
+        for (int c = 0; c < 8; c++) v[c] += x[c];
+    } else if (e.in_z) {
+        side.to(x);
+        by_act(e.in_act, [&](auto act) {
+#pragma unroll
+            for (int c = 0; c < 8; c++) v[c] *= slope_of<decltype(act)::value>(x[c]);
+        });
+    }
+    p.from(v);
+    p.store(static_cast<T *>(e.out) + i * e.out_stride + j, have);
+}
+
+}  // namespace dd
