@@ -32,8 +32,8 @@ struct Product {
 };
 
 // bytes of working memory of an m by n product of k sums (0: none), and the product
-size_t product_work(int64_t m, int64_t n, int64_t k);
-bool product_fits(int64_t m, int64_t n, int64_t k);      // one launch takes it
+size_t product_work(int64_t m, int64_t n, int64_t k, bool p_by_rows);
+bool product_fits(int64_t m, int64_t n, int64_t k, bool p_by_rows);      // one launch takes it
 hipError_t launch_product(const Product &p, void *work, hipStream_t s);
 
 // sums over the rows of an array (type, rows) into out (out_type), with

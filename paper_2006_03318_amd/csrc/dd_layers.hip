@@ -51,8 +51,8 @@ dd_status check_layer(int64_t rows, int64_t k, int64_t n, int32_t type, int32_t 
     return DD_OK;
 }
 
-dd_status check_product(int64_t m, int64_t n, int64_t k) {
-    return dd::product_fits(m, n, k) ? DD_OK : fail(DD_EINVAL, "a product of %lld by %lld is too large for one launch", (long long)m, (long long)n);
+dd_status check_product(int64_t m, int64_t n, int64_t k, bool p_by_rows) {
+    return dd::product_fits(m, n, k, p_by_rows) ? DD_OK : fail(DD_EINVAL, "a product of %lld by %lld is too large for one launch", (long long)m, (long long)n);
 }
 
 bool sizes_known(int64_t rows, int64_t k, int64_t n) { return rows >= 0 && k >= 1 && n >= 1 && rows < kMost && k < kMost && n < kMost; }
@@ -73,7 +73,7 @@ dd_status check_table(int64_t tokens, int64_t vocab, int64_t cols, int32_t type,
 
 extern "C" {
 
-size_t dd_linear_work(int64_t rows, int64_t k, int64_t n) { return sizes_known(rows, k, n) && rows > 0 ? dd::product_work(rows, n, k) : 0; }
+size_t dd_linear_work(int64_t rows, int64_t k, int64_t n) { return sizes_known(rows, k, n) && rows > 0 ? dd::product_work(rows, n, k, true) : 0; }
 
 dd_status dd_linear(const dd_linear_args *a, void *stream) {
     return guarded([&] {
@@ -87,7 +87,7 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         if (a->residual) CHECK(check_rows("residual", a->residual, a->rows, a->n, a->residual_stride, a->type, false));
         CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
         if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
-        CHECK(check_product(a->rows, a->n, a->k));
+        CHECK(check_product(a->rows, a->n, a->k, true));
         dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, {}};
         p.e.bias = a->bias;
         p.e.bias_type = a->bias_type;
@@ -99,14 +99,14 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         p.e.out = a->y;
         p.e.out_stride = a->y_stride;
         hipStream_t s = (hipStream_t)stream;
-        return with_work(a->work, dd::product_work(a->rows, a->n, a->k), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
+        return with_work(a->work, dd::product_work(a->rows, a->n, a->k, true), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
     });
 }
 
 size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
     if (!sizes_known(rows, k, n)) return 0;
     size_t most = dd::column_sum_work(rows, n);
-    for (size_t x : {rows > 0 ? dd::product_work(rows, k, n) : 0, dd::product_work(k, n, rows), dd::product_work(n, k, rows)}) most = x > most ? x : most;
+    for (size_t x : {rows > 0 ? dd::product_work(rows, k, n, true) : 0, dd::product_work(k, n, rows, false), dd::product_work(n, k, rows, false)}) most = x > most ? x : most;
     return most;
 }
 
@@ -124,20 +124,20 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
                 CHECK(check_rows("w", a->w, wr, wc, a->w_stride, a->type, false));
                 if (a->in_z) CHECK(check_rows("in_z", a->in_z, a->rows, a->k, a->in_z_stride, a->type, false));
                 CHECK(check_rows("dx", a->dx, a->rows, a->k, a->dx_stride, a->type, true));
-                CHECK(check_product(a->rows, a->k, a->n));
+                CHECK(check_product(a->rows, a->k, a->n, true));
             }
         }
         if (a->dw) {
             CHECK(check_rows("dw", a->dw, wr, wc, a->dw_stride, a->type, true));
-            CHECK(check_product(wr, wc, a->rows));
+            CHECK(check_product(wr, wc, a->rows, false));
         }
         if (!aligned(a->db, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "db is not aligned to its elements");
         hipStream_t s = (hipStream_t)stream;
         size_t need = 0;
         auto needs = [&](size_t x) { need = x > need ? x : need; };
-        if (a->dw) needs(dd::product_work(wr, wc, a->rows));
+        if (a->dw) needs(dd::product_work(wr, wc, a->rows, false));
         if (a->db) needs(dd::column_sum_work(a->rows, a->n));
-        if (a->dx && a->rows > 0) needs(dd::product_work(a->rows, a->k, a->n));
+        if (a->dx && a->rows > 0) needs(dd::product_work(a->rows, a->k, a->n, true));
         return with_work(a->work, need, s, "linear gradient", [&](void *work) {
             hipError_t e = hipSuccess;
             if (a->dw) {

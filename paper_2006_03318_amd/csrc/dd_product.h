@@ -10,7 +10,8 @@ namespace dd {
 
 // Which tiles, and how the sums are cut.
 struct Plan {
-    int tile;                   // rows of p a workgroup has: 16, 64, 128 or 256
+    int tile;                   // rows of p a workgroup has: 16 (few), 64, 128 or 256
+    bool few;                   // all of them, and the waves share the sums of 64 columns
     int tm, tn, splits;
     int64_t k_part;             // sums of a part: a multiple of 64
 };
@@ -121,9 +122,10 @@ struct Loads {
     static __device__ __forceinline__ int number(int wave, int j) {
         return kCount * WAVES == TILE::kLoads ? wave * kCount + j : (wave * kCount + j) % TILE::kLoads;
     }
-    __device__ __forceinline__ void init(const T *p, int64_t ld, int64_t first, int64_t count) {
+    // (wave: among those that share the tiles)
+    __device__ __forceinline__ void init(const T *p, int64_t ld, int64_t first, int64_t count, int of_wave) {
         lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wave = of_wave;
         stride = ld;
         base = p + (ROWS ? first * ld : first);
         rows = count - first < (1 << 20) ? (int)(count - first) : 1 << 20;
@@ -243,8 +245,8 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
             if (load_left <= 0 && load_tile < tiles) {
                 const Place at = place_of(load_tile, tm, tn, splits);
                 load_left = sums_of(at, load_l, load_end);
-                lp.init(static_cast<const T *>(a.p), a.p_stride, (int64_t)at.m * BM, a.m);
-                lq.init(static_cast<const T *>(a.q), a.q_stride, (int64_t)at.n * BN, a.n);
+                lp.init(static_cast<const T *>(a.p), a.p_stride, (int64_t)at.m * BM, a.m, wave);
+                lq.init(static_cast<const T *>(a.q), a.q_stride, (int64_t)at.n * BN, a.n, wave);
                 load_tile += gridDim.x;
                 if (DIRECT) {
                     from_p = lp.from(load_l);
@@ -422,6 +424,120 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
     if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (no load to LDS outlives its workgroup)
 }
 
+// Few rows: the weight's bytes are the bound.  A workgroup has 64 columns, and each of its waves a run of
+// the sums with tiles of its own in LDS, so that no wave waits for another until the waves' sums are joined in
+// order at the end.  Of p there are 16 MT rows.
+template <class T, bool QROWS, int MT, int WAVES, bool DIRECT>
+__global__ void __launch_bounds__(64 * WAVES) k_product_few(Product a, float *part, int splits, int64_t k_part) {
+    constexpr int BK = 64, BN = 64, NT = BN / 32, STAGES = DIRECT ? 2 : 1;
+    typedef Tile<true, false, 16 * MT, BK> PTile;
+    typedef Tile<QROWS, true, BN, BK> QTile;
+    typedef Loads<T, PTile, true, 1, DIRECT> PLoads;
+    typedef Loads<T, QTile, QROWS, 1, DIRECT> QLoads;
+    constexpr int kStage = PTile::kBytes + QTile::kBytes, kLoads = PLoads::kCount + QLoads::kCount, kSums = 16 * MT * BN * 4;
+    static_assert(kSums <= STAGES * kStage, "room for the sums");
+    __shared__ __attribute__((aligned(1024))) char lds[WAVES * STAGES * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr<char>)(lds), mine = lds0 + wave * (STAGES * kStage);
+    const int64_t tiles = (a.n + BN - 1) / BN, n0 = blockIdx.x % tiles * BN;
+    const int split = (int)(blockIdx.x / tiles);
+    const int64_t s0 = split * k_part, s1 = s0 + k_part < a.k ? s0 + k_part : a.k;
+    const int64_t each = ((s1 - s0 + WAVES * BK - 1) / (WAVES * BK)) * BK;
+    const int64_t k0 = s0 + wave * each, k1 = k0 + each < s1 ? k0 + each : s1;
+    const int steps = k1 > k0 ? (int)((k1 - k0 + BK - 1) / BK) : 0;
+
+    PLoads lp;
+    QLoads lq;
+    lp.init(static_cast<const T *>(a.p), a.p_stride, 0, a.m, 0);
+    lq.init(static_cast<const T *>(a.q), a.q_stride, n0, a.n, 0);
+    f4 acc[MT][NT][2] = {};
+    auto load = [&](int t) __attribute__((always_inline)) {
+        const int64_t l0 = k0 + (int64_t)t * BK, left = k1 - l0 > 0 ? k1 - l0 : 0;
+        if (DIRECT) {
+            if (left < BK) {
+                lp.cut(left);
+                lq.cut(left);
+            }
+            const uint32_t to = mine + (t & 1) * kStage;
+            const uint64_t fp = lp.from(l0), fq = lq.from(l0);
+#pragma unroll
+            for (int j = 0; j < QLoads::kCount; j++) lq.direct(fq, to + PTile::kBytes, j);
+#pragma unroll
+            for (int j = 0; j < PLoads::kCount; j++) lp.direct(fp, to, j);
+        } else {
+            lp.load(l0, left, BK);
+            lq.load(l0, left, BK);
+        }
+    };
+    load(0);
+    if (DIRECT) load(1);
+    for (int t = 0; t < steps; t++) {
+        const uint32_t from = mine + (DIRECT ? (t & 1) * kStage : 0);
+        if (DIRECT) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        } else {
+            lp.store(from);
+            lq.store(from + PTile::kBytes);
+            load(t + 1);
+        }
+        const uint32_t base_p = from + PTile::base(lane, 0), base_q = from + PTile::kBytes + QTile::base(lane, 0);
+        s8 fp[2][MT], fq[2][NT][2];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+#pragma unroll
+            for (int j = 0; j < 2 * NT; j++) fq[h][j / 2][j % 2] = QTile::fragment(base_q, j / 2, j % 2, h);
+#pragma unroll
+            for (int i = 0; i < MT; i++) fp[h][i] = PTile::fragment(base_p, i, 0, h);
+        }
+        if (DIRECT) {       // (all read: the slot is free)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            load(t + 2);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int i = 0; i < MT; i++)
+#pragma unroll
+                for (int j = 0; j < 2 * NT; j++) acc[i][j / 2][j % 2] = mfma(T{}, fq[h][j / 2][j % 2], fp[h][i], acc[i][j / 2][j % 2]);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    // the waves' sums, chunks of a row permuted as in k_product
+#pragma unroll
+    for (int i = 0; i < MT; i++)
+#pragma unroll
+        for (int j = 0; j < 2 * NT; j++) {
+            const int r = lane & 15, c = (8 * (j / 2) + 2 * (lane >> 4) + j % 2) ^ r;
+            *(lptr<f4>)(uintptr_t)(lds0 + wave * kSums + (16 * i + r) * (BN * 4) + c * 16) = acc[i][j / 2][j % 2];
+        }
+    __syncthreads();
+    for (int t = threadIdx.x; t < 16 * MT * (BN / 8); t += 64 * WAVES) {
+        const int r = t / (BN / 8);
+        const int64_t j = n0 + 8 * (t % (BN / 8));
+        const int have = r < a.m ? a.n - j >= 8 ? 8 : a.n - j < 0 ? 0 : (int)(a.n - j) : 0;
+        if (have == 0) continue;
+        float v[8] = {};
+        for (int w = 0; w < WAVES; w++)
+#pragma unroll
+            for (int s = 0; s < 2; s++) {
+                const f4 x = *(lptr<const f4>)(uintptr_t)(lds0 + w * kSums + r * (BN * 4) + ((2 * (t % (BN / 8)) + s) ^ (r & 15)) * 16);
+#pragma unroll
+                for (int b = 0; b < 4; b++) v[4 * s + b] += x[b];
+            }
+        if (splits > 1) {
+            Pack<float, 8> p;
+            p.from(v);
+            p.store(part + (split * a.m + r) * a.n + j, have);
+        } else {
+            float bias[8];
+            Pack<T, 8> side;
+            load_bias<T>(a.e, j, have, bias);
+            load_side<T>(a.e, r, j, have, side);
+            finish<T>(a.e, r, j, have, v, bias, side);
+        }
+    }
+}
+
 template <class T, bool PROWS, bool QROWS, int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
 void run_product(const Product &a, const Plan &p, float *part, hipStream_t s) {
     const int tiles = p.tm * p.tn * p.splits, grid = tiles < PER_CU * kUnits ? tiles : PER_CU * kUnits;
@@ -429,8 +545,7 @@ void run_product(const Product &a, const Plan &p, float *part, hipStream_t s) {
 }
 template <class T, bool DIRECT, bool PROWS, bool QROWS>
 void run_plan(const Product &a, const Plan &p, float *part, hipStream_t s) {
-    if (p.tile == 16) run_product<T, PROWS, QROWS, 16, 128, 1, 4, 2, 3, DIRECT>(a, p, part, s);
-    else if (p.tile == 64) run_product<T, PROWS, QROWS, 64, 64, 2, 2, 2, DIRECT ? 4 : 3, DIRECT>(a, p, part, s);
+    if (p.tile == 64) run_product<T, PROWS, QROWS, 64, 64, 2, 2, 2, DIRECT ? 4 : 3, DIRECT>(a, p, part, s);
     else if (!DIRECT || p.tile == 128) run_product<T, PROWS, QROWS, 128, 128, 2, 4, DIRECT ? 4 : 2, 1, DIRECT>(a, p, part, s);
     else run_product<T, PROWS, QROWS, 256, 256, 2, 4, 2, 1, true>(a, p, part, s);
 }
@@ -439,7 +554,13 @@ void run_plan(const Product &a, const Plan &p, float *part, hipStream_t s) {
 
 template <class T, bool DIRECT>
 void launch_tiles(const Product &a, const Plan &p, float *part, hipStream_t s) {
-    if (a.p_by_rows && a.q_by_rows) run_plan<T, DIRECT, true, true>(a, p, part, s);
+    if (p.few) {
+        const unsigned grid = (unsigned)(p.tn * p.splits);
+        if (p.tile == 16 && a.q_by_rows) k_product_few<T, true, 1, 8, DIRECT><<<grid, 512, 0, s>>>(a, part, p.splits, p.k_part);
+        else if (p.tile == 16) k_product_few<T, false, 1, 8, DIRECT><<<grid, 512, 0, s>>>(a, part, p.splits, p.k_part);
+        else if (a.q_by_rows) k_product_few<T, true, 4, 4, DIRECT><<<grid, 256, 0, s>>>(a, part, p.splits, p.k_part);
+        else k_product_few<T, false, 4, 4, DIRECT><<<grid, 256, 0, s>>>(a, part, p.splits, p.k_part);
+    } else if (a.p_by_rows && a.q_by_rows) run_plan<T, DIRECT, true, true>(a, p, part, s);
     else if (a.p_by_rows) run_plan<T, DIRECT, true, false>(a, p, part, s);
     else run_plan<T, DIRECT, false, false>(a, p, part, s);
 }

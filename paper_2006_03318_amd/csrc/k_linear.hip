@@ -21,19 +21,22 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
         const int64_t i = t / packs, j = (t - i * packs) * 8;
         const int have = a.n - j >= 8 ? 8 : (int)(a.n - j);
         const float *p = part + i * a.n + j;
-        float v[8] = {};
-        for (int s = 0; s < splits; s++, p += a.m * a.n) {
-            Pack<float, 8> b;
-            float x[8];
-            b.load(p, have);
-            b.to(x);
-#pragma unroll
-            for (int c = 0; c < 8; c++) v[c] += x[c];
-        }
-        float bias[8];
+        float v[8] = {}, bias[8];
         Pack<T, 8> side;
         load_bias<T>(a.e, j, have, bias);
         load_side<T>(a.e, i, j, have, side);
+        for (int s = 0; s < splits; s += 4) {       // (four loads at a time)
+            Pack<float, 8> b[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) b[u].load(p + (s + u) * a.m * a.n, s + u < splits ? have : 0);
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                float x[8];
+                b[u].to(x);
+#pragma unroll
+                for (int c = 0; c < 8; c++) v[c] += x[c];
+            }
+        }
         finish<T>(a.e, i, j, have, v, bias, side);
     }
 }
@@ -46,18 +49,28 @@ int64_t tiles_of(int64_t x, int64_t n) { return (x + n - 1) / n; }
 // 1,024 in 37, 48 with two such tiles of four waves at a time), 0.30 with 64 x 64 (1,021 x 1,240 -> 776 in 9.9,
 // 14.5 with 128); operands of any alignment 0.83, and 0.27 but 0.63 at least; an epilogue 7.5, 2 and 0.6 (its
 // stores); joining parts another launch and its traffic.
-Plan plan_of(int64_t m, int64_t n, int64_t k, bool direct) {
-    Plan p{0, 0, 0, 1, 0};
+Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
+    Plan p{0, false, 0, 0, 1, 0};
     double least = 0.0;
     const int64_t steps = tiles_of(k, 64) > 0 ? tiles_of(k, 64) : 1;
-    for (int tile : {256, 128, 64, 16}) {
-        if (m <= 16 ? tile != 16 : tile == 16 || (tile == 256 && !direct)) continue;
-        const int64_t tm = tiles_of(m, tile), tn = tiles_of(n, tile == 16 ? 128 : tile);
+    if (p_rows && m <= 64) {
+        // (a workgroup for each 64 columns, parts of the sums where those are fewer than half the compute units)
+        p.tile = m <= 16 ? 16 : 64;
+        p.few = true;
+        p.tm = 1;
+        p.tn = (int)tiles_of(n, 64);
+        const int64_t waves = m <= 16 ? 8 : 4, most = tiles_of(steps, waves), want = p.tn >= kUnits / 2 ? 1 : tiles_of(kUnits, p.tn);
+        p.k_part = tiles_of(tiles_of(steps, want < most ? want : most), waves) * waves * 64;
+        p.splits = (int)tiles_of(k > 0 ? k : 1, p.k_part);
+        return p;
+    }
+    for (int tile : {256, 128, 64}) {
+        if (tile == 256 && !direct) continue;
+        const int64_t tm = tiles_of(m, tile), tn = tiles_of(n, tile);
         for (int64_t s = 1; s <= steps; s *= 2) {
             const int64_t each = tiles_of(steps, s), rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
-            double step = tile == 256 ? 1.44 * rounds : tile == 128 ? (direct ? 0.53 : 0.83) * rounds : tile == 64 ? 0.30 * rounds : 0.2 * rounds;
-            if (!direct && tile <= 64) step = 0.27 * rounds > 0.63 ? 0.27 * rounds : 0.63;
-            if (tile == 16 && step < 0.4) step = 0.4;
+            double step = tile == 256 ? 1.44 * rounds : tile == 128 ? (direct ? 0.53 : 0.83) * rounds : 0.30 * rounds;
+            if (!direct && tile == 64) step = 0.27 * rounds > 0.63 ? 0.27 * rounds : 0.63;
             double us = each * step + rounds * (tile == 256 ? 7.5 : tile == 128 ? 2.0 : 0.6);
             if (s > 1) us += 4.0 + 4e-6 / 3.0 * (double)(2 * s) * (double)m * (double)n;
             if (p.tile && us >= least) continue;
@@ -83,7 +96,7 @@ bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count,
 template <class T>
 hipError_t product(const Product &a, float *part, hipStream_t s) {
     const bool direct = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k) && aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k);
-    const Plan p = plan_of(a.m, a.n, a.k, direct);
+    const Plan p = plan_of(a.m, a.n, a.k, a.p_by_rows, direct);
     if (direct) launch_tiles<T, true>(a, p, part, s);
     else launch_tiles<T, false>(a, p, part, s);
     if (p.splits > 1) {
@@ -201,15 +214,15 @@ __global__ void __launch_bounds__(256) k_act_grad(dd_act_grad_args a) {
 
 }  // namespace
 
-size_t product_work(int64_t m, int64_t n, int64_t k) {
-    const size_t a = plan_work(plan_of(m, n, k, true), m, n), b = plan_work(plan_of(m, n, k, false), m, n);
+size_t product_work(int64_t m, int64_t n, int64_t k, bool p_rows) {
+    const size_t a = plan_work(plan_of(m, n, k, p_rows, true), m, n), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
     return a > b ? a : b;
 }
 
-bool product_fits(int64_t m, int64_t n, int64_t k) {
+bool product_fits(int64_t m, int64_t n, int64_t k, bool p_rows) {
     for (bool direct : {true, false}) {       // (tiles are counted in 32 bits)
-        const Plan p = plan_of(m, n, k, direct);
-        if (tiles_of(m, p.tile) * (int64_t)p.tn * p.splits >= (int64_t(1) << 30)) return false;
+        const Plan p = plan_of(m, n, k, p_rows, direct);
+        if ((int64_t)p.tm * p.tn * p.splits >= (int64_t(1) << 30)) return false;
     }
     return true;
 }

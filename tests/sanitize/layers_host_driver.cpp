@@ -9,8 +9,8 @@
 
 namespace dd {
 #define STUB return hipErrorNoDevice
-size_t product_work(int64_t m, int64_t n, int64_t k) { return k > 1000 ? (size_t)m * (size_t)n * 8 : 0; }
-bool product_fits(int64_t m, int64_t n, int64_t) { return m < (1 << 30) && n < (1 << 30); }
+size_t product_work(int64_t m, int64_t n, int64_t k, bool) { return k > 1000 ? (size_t)m * (size_t)n * 8 : 0; }
+bool product_fits(int64_t m, int64_t n, int64_t, bool) { return m < (1 << 30) && n < (1 << 30); }
 hipError_t launch_product(const Product &, void *, hipStream_t) { STUB; }
 size_t column_sum_work(int64_t, int64_t cols) { return (size_t)cols * 4; }
 hipError_t launch_column_sum(const void *, int64_t, int64_t, int64_t, int32_t, void *, int32_t, void *, hipStream_t) { STUB; }
