@@ -10,12 +10,13 @@ namespace dd {
 
 // Which tiles, and how the sums are cut.
 struct Plan {
-    int tile;                   // rows of p a workgroup has: 16 (few), 64, 128 or 256
-    bool few;                   // all of them, and the waves share the sums of 64 columns
+    int tile;                   // rows of p a workgroup has: 128 or 256; 16 or 64 with waves that share the sums
     int tm, tn, splits;
     int64_t k_part;             // sums of a part: a multiple of 64
 };
 constexpr int kUnits = 256;     // compute units
+template <bool DIRECT>
+constexpr int kApart = DIRECT ? 4 : 8;      // waves that share the sums of a tile of 64 rows
 
 // the tiles' passes; of a plan for aligned operands (DIRECT) or any
 template <class T, bool DIRECT>
@@ -160,13 +161,16 @@ struct Loads {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
                      "v"(off[j]), "s"(buffer));
     }
-    __device__ __forceinline__ void load(int64_t l0, int64_t left, int full) {
-        if (plain && (left > full || (left == full && (ROWS || rows >= TILE::kN)))) {
-            const char *b = reinterpret_cast<const char *>(base + (ROWS ? l0 : l0 * stride));
+    // whether a step of `full` sums, of those `left`, is loaded without a look at what is there
+    __device__ __forceinline__ bool quick(int64_t left, int full) const {
+        return plain && (left > full || (left == full && (ROWS || rows >= TILE::kN)));
+    }
+    __device__ __forceinline__ void load_quick(int64_t l0) {
+        const char *b = reinterpret_cast<const char *>(base + (ROWS ? l0 : l0 * stride));
 #pragma unroll
-            for (int j = 0; j < kCount; j++) v[j].load(reinterpret_cast<const T *>(b + off[j]));
-            return;
-        }
+        for (int j = 0; j < kCount; j++) v[j].load(reinterpret_cast<const T *>(b + off[j]));
+    }
+    __device__ __forceinline__ void load_slowly(int64_t l0, int64_t left) {
         const int mine = fresh(lane);
 #pragma unroll
         for (int j = 0; j < kCount; j++) {
@@ -183,6 +187,18 @@ struct Loads {
             *(lptr<typename Pack<T, 8>::vec>)(uintptr_t)(to + number(wave, j) * 1024 + lane * 16) = v[j].v;
     }
 };
+
+// (one branch for both operands: loads under way in one of two ways would be waited for before those of the next)
+template <class P, class Q>
+__device__ __forceinline__ void load_step(P &p, Q &q, int64_t l0, int64_t left, int full) {
+    if (p.quick(left, full) && q.quick(left, full)) {
+        p.load_quick(l0);
+        q.load_quick(l0);
+    } else {
+        p.load_slowly(l0, left);
+        q.load_slowly(l0, left);
+    }
+}
 
 // Tile of workgroup b: workgroups go round the eight XCDs, so each gets a run of tiles
 // that share rows and columns in its L2: eight tiles down, then the next column.
@@ -260,8 +276,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
         }
         if (!DIRECT) {
             const int64_t left = load_left > 0 ? load_end - load_l : 0;
-            lp.load(load_l, left, BK);
-            lq.load(load_l, left, BK);
+            load_step(lp, lq, load_l, left, BK);
         }
     };
 
@@ -424,31 +439,30 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
     if (DIRECT) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (no load to LDS outlives its workgroup)
 }
 
-// Few rows: the weight's bytes are the bound.  A workgroup has 64 columns, and each of its waves a run of
-// the sums with tiles of its own in LDS, so that no wave waits for another until the waves' sums are joined in
-// order at the end.  Of p there are 16 MT rows.
-template <class T, bool QROWS, int MT, int WAVES, bool DIRECT>
-__global__ void __launch_bounds__(64 * WAVES) k_product_few(Product a, float *part, int splits, int64_t k_part) {
+// Small products, whose bound are the weight's bytes or the latency of a step's loads.  A workgroup has one
+// tile of 16 MT rows by 64 columns, and each of its waves a run of the sums with tiles of its own in LDS, so that
+// no wave waits for another until the waves' sums are joined in order at the end.
+template <class T, bool PROWS, bool QROWS, int MT, int WAVES, bool DIRECT>
+__global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *part, int tm, int tn, int splits, int64_t k_part) {
     constexpr int BK = 64, BN = 64, NT = BN / 32, STAGES = DIRECT ? 2 : 1;
-    typedef Tile<true, false, 16 * MT, BK> PTile;
+    typedef Tile<PROWS, false, 16 * MT, BK> PTile;
     typedef Tile<QROWS, true, BN, BK> QTile;
-    typedef Loads<T, PTile, true, 1, DIRECT> PLoads;
+    typedef Loads<T, PTile, PROWS, 1, DIRECT> PLoads;
     typedef Loads<T, QTile, QROWS, 1, DIRECT> QLoads;
     constexpr int kStage = PTile::kBytes + QTile::kBytes, kLoads = PLoads::kCount + QLoads::kCount, kSums = 16 * MT * BN * 4;
     static_assert(kSums <= STAGES * kStage, "room for the sums");
     __shared__ __attribute__((aligned(1024))) char lds[WAVES * STAGES * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr<char>)(lds), mine = lds0 + wave * (STAGES * kStage);
-    const int64_t tiles = (a.n + BN - 1) / BN, n0 = blockIdx.x % tiles * BN;
-    const int split = (int)(blockIdx.x / tiles);
-    const int64_t s0 = split * k_part, s1 = s0 + k_part < a.k ? s0 + k_part : a.k;
+    const Place at = place_of(blockIdx.x, tm, tn, splits);
+    const int64_t m0 = (int64_t)at.m * (16 * MT), n0 = (int64_t)at.n * BN, s0 = at.split * k_part, s1 = s0 + k_part < a.k ? s0 + k_part : a.k;
     const int64_t each = ((s1 - s0 + WAVES * BK - 1) / (WAVES * BK)) * BK;
     const int64_t k0 = s0 + wave * each, k1 = k0 + each < s1 ? k0 + each : s1;
     const int steps = k1 > k0 ? (int)((k1 - k0 + BK - 1) / BK) : 0;
 
     PLoads lp;
     QLoads lq;
-    lp.init(static_cast<const T *>(a.p), a.p_stride, 0, a.m, 0);
+    lp.init(static_cast<const T *>(a.p), a.p_stride, m0, a.m, 0);
     lq.init(static_cast<const T *>(a.q), a.q_stride, n0, a.n, 0);
     f4 acc[MT][NT][2] = {};
     auto load = [&](int t) __attribute__((always_inline)) {
@@ -465,8 +479,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_product_few(Product a, float *pa
 #pragma unroll
             for (int j = 0; j < PLoads::kCount; j++) lp.direct(fp, to, j);
         } else {
-            lp.load(l0, left, BK);
-            lq.load(l0, left, BK);
+            load_step(lp, lq, l0, left, BK);
         }
     };
     load(0);
@@ -513,8 +526,8 @@ __global__ void __launch_bounds__(64 * WAVES) k_product_few(Product a, float *pa
     __syncthreads();
     for (int t = threadIdx.x; t < 16 * MT * (BN / 8); t += 64 * WAVES) {
         const int r = t / (BN / 8);
-        const int64_t j = n0 + 8 * (t % (BN / 8));
-        const int have = r < a.m ? a.n - j >= 8 ? 8 : a.n - j < 0 ? 0 : (int)(a.n - j) : 0;
+        const int64_t i = m0 + r, j = n0 + 8 * (t % (BN / 8));
+        const int have = i < a.m ? a.n - j >= 8 ? 8 : a.n - j < 0 ? 0 : (int)(a.n - j) : 0;
         if (have == 0) continue;
         float v[8] = {};
         for (int w = 0; w < WAVES; w++)
@@ -527,13 +540,13 @@ __global__ void __launch_bounds__(64 * WAVES) k_product_few(Product a, float *pa
         if (splits > 1) {
             Pack<float, 8> p;
             p.from(v);
-            p.store(part + (split * a.m + r) * a.n + j, have);
+            p.store(part + (at.split * a.m + i) * a.n + j, have);
         } else {
             float bias[8];
             Pack<T, 8> side;
             load_bias<T>(a.e, j, have, bias);
-            load_side<T>(a.e, r, j, have, side);
-            finish<T>(a.e, r, j, have, v, bias, side);
+            load_side<T>(a.e, i, j, have, side);
+            finish<T>(a.e, i, j, have, v, bias, side);
         }
     }
 }
@@ -545,7 +558,9 @@ void run_product(const Product &a, const Plan &p, float *part, hipStream_t s) {
 }
 template <class T, bool DIRECT, bool PROWS, bool QROWS>
 void run_plan(const Product &a, const Plan &p, float *part, hipStream_t s) {
-    if (p.tile == 64) run_product<T, PROWS, QROWS, 64, 64, 2, 2, 2, DIRECT ? 4 : 3, DIRECT>(a, p, part, s);
+    const int tiles = p.tm * p.tn * p.splits;
+    if (PROWS && p.tile == 16) k_product_apart<T, true, QROWS, 1, 8, DIRECT><<<tiles, 512, 0, s>>>(a, part, p.tm, p.tn, p.splits, p.k_part);
+    else if (p.tile <= 64) k_product_apart<T, PROWS, QROWS, 4, kApart<DIRECT>, DIRECT><<<tiles, 64 * kApart<DIRECT>, 0, s>>>(a, part, p.tm, p.tn, p.splits, p.k_part);
     else if (!DIRECT || p.tile == 128) run_product<T, PROWS, QROWS, 128, 128, 2, 4, DIRECT ? 4 : 2, 1, DIRECT>(a, p, part, s);
     else run_product<T, PROWS, QROWS, 256, 256, 2, 4, 2, 1, true>(a, p, part, s);
 }
@@ -554,13 +569,7 @@ void run_plan(const Product &a, const Plan &p, float *part, hipStream_t s) {
 
 template <class T, bool DIRECT>
 void launch_tiles(const Product &a, const Plan &p, float *part, hipStream_t s) {
-    if (p.few) {
-        const unsigned grid = (unsigned)(p.tn * p.splits);
-        if (p.tile == 16 && a.q_by_rows) k_product_few<T, true, 1, 8, DIRECT><<<grid, 512, 0, s>>>(a, part, p.splits, p.k_part);
-        else if (p.tile == 16) k_product_few<T, false, 1, 8, DIRECT><<<grid, 512, 0, s>>>(a, part, p.splits, p.k_part);
-        else if (a.q_by_rows) k_product_few<T, true, 4, 4, DIRECT><<<grid, 256, 0, s>>>(a, part, p.splits, p.k_part);
-        else k_product_few<T, false, 4, 4, DIRECT><<<grid, 256, 0, s>>>(a, part, p.splits, p.k_part);
-    } else if (a.p_by_rows && a.q_by_rows) run_plan<T, DIRECT, true, true>(a, p, part, s);
+    if (a.p_by_rows && a.q_by_rows) run_plan<T, DIRECT, true, true>(a, p, part, s);
     else if (a.p_by_rows) run_plan<T, DIRECT, true, false>(a, p, part, s);
     else run_plan<T, DIRECT, false, false>(a, p, part, s);
 }

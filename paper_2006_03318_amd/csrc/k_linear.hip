@@ -44,34 +44,23 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
 // --- which tiles, and how sums are cut -------------------------------------------
 int64_t tiles_of(int64_t x, int64_t n) { return (x + n - 1) / n; }
 
+constexpr double kStepApart[2] = {1.0, 0.6}, kEndApart = 2.0;
 // Tile and parts that are expected to take least, from what was measured (us): a step of 64 sums of one
-// tile per compute unit takes 1.44 with 256 x 256 (8,192^3 bf16 in 768), 0.53 with 128 x 128 (4,096 x 4,096 ->
-// 1,024 in 37, 48 with two such tiles of four waves at a time), 0.30 with 64 x 64 (1,021 x 1,240 -> 776 in 9.9,
-// 14.5 with 128); operands of any alignment 0.83, and 0.27 but 0.63 at least; an epilogue 7.5, 2 and 0.6 (its
-// stores); joining parts another launch and its traffic.
+// tile per compute unit takes 1.44 with 256 x 256 (8,192^3 bf16 in 768) and 0.53 with 128 x 128 (4,096 x 4,096 ->
+// 1,024 in 37), 0.83 with operands of any alignment; an epilogue 7.5 and 2 (its stores); joining
+// parts another launch and its traffic.
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
-    Plan p{0, false, 0, 0, 1, 0};
+    Plan p{0, 0, 0, 1, 0};
     double least = 0.0;
     const int64_t steps = tiles_of(k, 64) > 0 ? tiles_of(k, 64) : 1;
-    if (p_rows && m <= 64) {
-        // (a workgroup for each 64 columns, parts of the sums where those are fewer than half the compute units)
-        p.tile = m <= 16 ? 16 : 64;
-        p.few = true;
-        p.tm = 1;
-        p.tn = (int)tiles_of(n, 64);
-        const int64_t waves = m <= 16 ? 8 : 4, most = tiles_of(steps, waves), want = p.tn >= kUnits / 2 ? 1 : tiles_of(kUnits, p.tn);
-        p.k_part = tiles_of(tiles_of(steps, want < most ? want : most), waves) * waves * 64;
-        p.splits = (int)tiles_of(k > 0 ? k : 1, p.k_part);
-        return p;
-    }
-    for (int tile : {256, 128, 64}) {
-        if (tile == 256 && !direct) continue;
-        const int64_t tm = tiles_of(m, tile), tn = tiles_of(n, tile);
-        for (int64_t s = 1; s <= steps; s *= 2) {
-            const int64_t each = tiles_of(steps, s), rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
-            double step = tile == 256 ? 1.44 * rounds : tile == 128 ? (direct ? 0.53 : 0.83) * rounds : 0.30 * rounds;
-            if (!direct && tile == 64) step = 0.27 * rounds > 0.63 ? 0.27 * rounds : 0.63;
-            double us = each * step + rounds * (tile == 256 ? 7.5 : tile == 128 ? 2.0 : 0.6);
+    for (int tile : {256, 128, 64, 16}) {
+        if ((tile == 256 && !direct) || (tile == 16 && (m > 16 || !p_rows))) continue;
+        const int64_t tm = tiles_of(m, tile), tn = tiles_of(n, tile <= 64 ? 64 : tile);
+        const int64_t waves = tile == 16 ? 8 : tile == 64 ? (direct ? kApart<true> : kApart<false>) : 1;
+        for (int64_t s = 1; s <= tiles_of(steps, waves); s *= 2) {
+            const int64_t each = tiles_of(tiles_of(steps, waves), s) * waves, rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
+            double us = tile == 256 ? (each * 1.44 + 7.5) * rounds : tile == 128 ? (each * (direct ? 0.53 : 0.83) + 2.0) * rounds
+                      : (each / waves * kStepApart[direct] + kEndApart) * rounds;
             if (s > 1) us += 4.0 + 4e-6 / 3.0 * (double)(2 * s) * (double)m * (double)n;
             if (p.tile && us >= least) continue;
             least = us;
@@ -93,10 +82,54 @@ bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count,
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (by_rows ? k : count) % 8 == 0 && stride < (int64_t(1) << 22);
 }
 
+// --- operands of odd sizes --------------------------------------------------------
+// Rows that are not multiples of 16 bytes cannot be loaded to LDS directly, which makes a step half as fast and
+// more.  Where the sizes themselves are odd and an operand is read many times, it is copied first, rows padded with
+// zeros to 16 bytes.  4,099 x 1,237 -> 777 f16 24 us (32 without), 1,021 x 777 x 1,237 14 (18 to 25).
+struct Rows {
+    const bf16_t *from;          // (16 bits, whatever they mean)
+    bf16_t *to;
+    int64_t stride, rows, cols;
+    __host__ __device__ int64_t packs() const { return (cols + 7) / 8; }
+};
+__global__ void __launch_bounds__(256) k_pad_rows(Rows x, Rows y) {
+    const Rows &r = blockIdx.y ? y : x;
+    const int64_t packs = r.packs(), total = packs * r.rows;
+    for (int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
+        const int64_t i = t / packs, j = (t - i * packs) * 8;
+        Pack<bf16_t, 8> v;
+        v.load(r.from + i * r.stride + j, r.cols - j >= 8 ? 8 : (int)(r.cols - j));
+        v.store(r.to + t * 8);
+    }
+}
+bool pads(int64_t m, int64_t n, int64_t k) { return (m % 8 || n % 8 || k % 8) && m > 64 && n > 64; }
+size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
+    auto most = [&](int64_t i) { return i * tiles_of(k, 8) > k * tiles_of(i, 8) ? i * tiles_of(k, 8) : k * tiles_of(i, 8); };
+    return pads(m, n, k) ? (size_t)(most(m) + most(n)) * 16 : 0;
+}
+
 template <class T>
-hipError_t product(const Product &a, float *part, hipStream_t s) {
-    const bool direct = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k) && aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k);
+hipError_t product(const Product &args, char *work, hipStream_t s) {
+    Product a = args;
+    const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k), aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k);
+    const bool pad = !(ap && aq) && pads(a.m, a.n, a.k), direct = (ap && aq) || pad;
     const Plan p = plan_of(a.m, a.n, a.k, a.p_by_rows, direct);
+    float *part = reinterpret_cast<float *>(work);
+    if (pad) {
+        bf16_t *to = reinterpret_cast<bf16_t *>(work + (plan_work(p, a.m, a.n) + 15) / 16 * 16);
+        auto padded = [&](const void *&x, int64_t &stride, int64_t rows, int64_t cols) {
+            const Rows r{static_cast<const bf16_t *>(x), to, stride, rows, cols};
+            x = to;
+            stride = r.packs() * 8;
+            to += rows * stride;
+            return r;
+        };
+        Rows x{}, y{};
+        if (!ap) x = a.p_by_rows ? padded(a.p, a.p_stride, a.m, a.k) : padded(a.p, a.p_stride, a.k, a.m);
+        if (!aq) (ap ? x : y) = a.q_by_rows ? padded(a.q, a.q_stride, a.n, a.k) : padded(a.q, a.q_stride, a.k, a.n);
+        const int64_t need = tiles_of(x.packs() * x.rows > y.packs() * y.rows ? x.packs() * x.rows : y.packs() * y.rows, 256);
+        k_pad_rows<<<dim3((unsigned)(need < 8 * kUnits ? need : 8 * kUnits), y.rows ? 2 : 1), 256, 0, s>>>(x, y);
+    }
     if (direct) launch_tiles<T, true>(a, p, part, s);
     else launch_tiles<T, false>(a, p, part, s);
     if (p.splits > 1) {
@@ -215,7 +248,7 @@ __global__ void __launch_bounds__(256) k_act_grad(dd_act_grad_args a) {
 }  // namespace
 
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_rows) {
-    const size_t a = plan_work(plan_of(m, n, k, p_rows, true), m, n), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
+    const size_t a = (plan_work(plan_of(m, n, k, p_rows, true), m, n) + 15) / 16 * 16 + pad_work(m, n, k), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
     return a > b ? a : b;
 }
 
@@ -228,7 +261,7 @@ bool product_fits(int64_t m, int64_t n, int64_t k, bool p_rows) {
 }
 
 hipError_t launch_product(const Product &p, void *work, hipStream_t s) {
-    return p.type == DD_BF16 ? product<bf16_t>(p, static_cast<float *>(work), s) : product<f16_t>(p, static_cast<float *>(work), s);
+    return p.type == DD_BF16 ? product<bf16_t>(p, static_cast<char *>(work), s) : product<f16_t>(p, static_cast<char *>(work), s);
 }
 
 size_t column_sum_work(int64_t rows, int64_t cols) {
