@@ -43,10 +43,9 @@ __global__ void __launch_bounds__(256) k_embed(dd_embed_args a, uint32_t packs) 
 }
 
 // --- the tokens in the order of their ids -------------------------------------------
-// Least significant digits of eight bits first.  A workgroup has kSortBlock places in a row
-// and a wave a run of them, so ranks count waves, then lanes, in order (stable).  Ids
-// that do not count (pad, or not in the table) are `vocab`, behind all others.
-constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kSortEach = 8, kSortBlock = kSortThreads * kSortEach, kDigits = 256;
+// Least significant digits of eight bits first, stable.  Ids that do not count (pad, or not in
+// the table) are `vocab`, behind all others.
+constexpr int kDigits = 256;
 
 struct Sorted {
     uint32_t *key, *place;       // id and token
@@ -57,38 +56,158 @@ __device__ __forceinline__ uint32_t key_of(const dd_embed_grad_args &a, int64_t 
     return id < 0 || id >= a.vocab || id == a.pad ? (uint32_t)a.vocab : (uint32_t)id;
 }
 
-// counts[digit][workgroup]: a workgroup's places with each digit
-template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args a, Sorted from, int shift, uint32_t *counts) {
+// Lanes of the wave, among those that are in, with this lane's digit.
+__device__ __forceinline__ uint64_t peers_of(uint32_t digit, bool in) {
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 8; b++) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
+    }
+    return same;
+}
+__device__ __forceinline__ int rank_among(uint64_t peers) { return __popcll(peers & ((uint64_t(1) << (threadIdx.x & 63)) - 1)); }
+
+// Exclusive running sum over the first 256 threads (a multiple of 64, all of whose waves call), by `room` of LDS.
+__device__ __forceinline__ uint32_t digits_before(uint32_t x, uint32_t *room) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t run = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(run, o, 64);
+        if (lane >= o) run += y;
+    }
+    if (lane == 63) room[wave] = run;
+    __syncthreads();
+    run -= x;
+    for (int w = 0; w < wave; w++) run += room[w];
+    return run;
+}
+
+// Zeros in the whole table, eight columns a thread, by the workgroups from `first` on of a launch.
+template <class T>
+__device__ __forceinline__ void fill_table(const dd_embed_grad_args &a, int64_t first) {
+    Pack<T, 8> zero;
+    zero.v = 0;
+    const int64_t me = (blockIdx.x - first) * (int64_t)blockDim.x + threadIdx.x, all = (gridDim.x - first) * (int64_t)blockDim.x;
+    T *to = static_cast<T *>(a.dtable);
+    if (a.dtable_stride == a.cols) {
+        const int64_t n = a.vocab * a.cols;
+        for (int64_t i = 8 * me; i < n; i += 8 * all) zero.store(to + i, have_of(n, i));
+        return;
+    }
+    const int64_t packs = (a.cols + 7) / 8, n = a.vocab * packs;
+    for (int64_t i = me; i < n; i += all) {
+        const int64_t r = i / packs, c = (i - r * packs) * 8;
+        zero.store(to + r * a.dtable_stride + c, have_of(a.cols, c));
+    }
+}
+
+// Few tokens: one workgroup sorts them in LDS, EACH to a thread.  2,047 tokens 6 us, in which
+// the others may fill the table.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+template <class T, int EACH>
+__global__ void __launch_bounds__(kSmallThreads) k_embed_sort(dd_embed_grad_args a, Sorted to, int passes) {
+    if (blockIdx.x > 0) {
+        fill_table<T>(a, 1);
+        return;
+    }
+    __shared__ uint32_t keys[kSmallThreads * EACH], next[kSmallWaves][kDigits], room[kSmallWaves];
+    __shared__ uint16_t places[kSmallThreads * EACH];
+    const int n = (int)a.tokens, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = wave * (64 * EACH);
+    uint32_t key[EACH], place[EACH], before[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; i++) {
+        place[i] = first + i * 64 + lane;
+        key[i] = (int)place[i] < n ? key_of(a, place[i]) : 0;
+    }
+    for (int pass = 0; pass < passes; pass++) {
+        for (int d = lane; d < kDigits; d += 64) next[wave][d] = 0;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            const bool in = first + i * 64 + lane < n;
+            const uint32_t d = key[i] >> (8 * pass) & (kDigits - 1);
+            const uint64_t peers = peers_of(d, in);
+            const int rank = rank_among(peers);
+            before[i] = next[wave][d] + rank;
+            __builtin_amdgcn_wave_barrier();
+            if (in && rank == 0) next[wave][d] += __popcll(peers);
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+        uint32_t all = 0;
+        if (threadIdx.x < kDigits)
+            for (int w = 0; w < kSmallWaves; w++) all += next[w][threadIdx.x];
+        uint32_t at = digits_before(threadIdx.x < kDigits ? all : 0, room);
+        if (threadIdx.x < kDigits)
+            for (int w = 0; w < kSmallWaves; w++) {
+                const uint32_t x = next[w][threadIdx.x];
+                next[w][threadIdx.x] = at;
+                at += x;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            if (first + i * 64 + lane >= n) continue;
+            const uint32_t p = next[wave][key[i] >> (8 * pass) & (kDigits - 1)] + before[i];
+            if (pass + 1 == passes) {
+                to.key[p] = key[i];
+                to.place[p] = place[i];
+            } else {
+                keys[p] = key[i];
+                places[p] = (uint16_t)place[i];
+            }
+        }
+        if (pass + 1 == passes) return;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < EACH; i++) {
+            const int p = first + i * 64 + lane;
+            key[i] = p < n ? keys[p] : 0;
+            place[i] = p < n ? places[p] : 0;
+        }
+        __syncthreads();
+    }
+}
+
+// More: a workgroup has kSortBlock places in a row and a wave a run of them, so ranks count waves, then lanes.
+constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kSortEach = 8, kSortBlock = kSortThreads * kSortEach;
+static_assert(kSortThreads == kDigits, "a thread has a digit");
+
+// counts[digit][workgroup]: a workgroup's places with each digit; the workgroups behind fill the table
+template <class T, bool FIRST>
+__global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args a, Sorted from, int shift, int blocks, uint32_t *counts) {
+    if ((int)blockIdx.x >= blocks) {
+        fill_table<T>(a, blocks);
+        return;
+    }
     __shared__ uint32_t n[kDigits];
     n[threadIdx.x] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kSortBlock;
+    uint32_t key[kSortEach];
 #pragma unroll
     for (int i = 0; i < kSortEach; i++) {
         const int64_t t = first + i * kSortThreads + threadIdx.x;
-        if (t < a.tokens) atomicAdd(&n[(FIRST ? key_of(a, t) : from.key[t]) >> shift & (kDigits - 1)], 1u);
+        key[i] = t >= a.tokens ? 0 : FIRST ? key_of(a, t) : from.key[t];
     }
+#pragma unroll
+    for (int i = 0; i < kSortEach; i++)
+        if (first + i * kSortThreads + threadIdx.x < a.tokens) atomicAdd(&n[key[i] >> shift & (kDigits - 1)], 1u);
     __syncthreads();
-    counts[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = n[threadIdx.x];
+    counts[(int64_t)threadIdx.x * blocks + blockIdx.x] = n[threadIdx.x];
 }
 
-// Running sums of all counts, in place: each of 1,024 threads has a run of them.
+// Running sums of all counts, in place, where there are too many workgroups for each to sum them by itself:
+// each of 1,024 threads has a run of them.
+constexpr int kManyBlocks = 512;
 __global__ void __launch_bounds__(1024) k_embed_scan(uint32_t *counts, int64_t n) {
-    __shared__ uint32_t of_wave[16];
+    __shared__ uint32_t room[16];
     const int64_t each = (n + 1023) / 1024, i0 = threadIdx.x * each, i1 = i0 + each < n ? i0 + each : n;
     uint32_t sum = 0;
     for (int64_t i = i0; i < i1; i++) sum += counts[i];
-    uint32_t run = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(run, o, 64);
-        if ((threadIdx.x & 63) >= (unsigned)o) run += x;
-    }
-    if ((threadIdx.x & 63) == 63) of_wave[threadIdx.x >> 6] = run;
-    __syncthreads();
-    uint32_t before = run - sum;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); w++) before += of_wave[w];
+    uint32_t before = digits_before(sum, room);
     for (int64_t i = i0; i < i1; i++) {
         const uint32_t x = counts[i];
         counts[i] = before;
@@ -96,13 +215,13 @@ __global__ void __launch_bounds__(1024) k_embed_scan(uint32_t *counts, int64_t n
     }
 }
 
-// Every place to where the running sums and its rank in the workgroup say.
+// Every place to where the counts and its rank in the workgroup say.  (Counting the next pass's digits here, by
+// atomics where the places go, takes 85 us of 65,536 words of a language, whose high digits are mostly one.)
 template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_args a, Sorted from, Sorted to, int shift, const uint32_t *sums) {
-    __shared__ uint32_t next[kSortWaves][kDigits];      // first counts, then places to come
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_args a, Sorted from, Sorted to, int shift, const uint32_t *counts, bool summed) {
+    __shared__ uint32_t next[kSortWaves][kDigits], room[kSortWaves];      // next: first counts, then places to come
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = gridDim.x;
     for (int i = lane; i < kDigits; i += 64) next[wave][i] = 0;
-    __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kSortBlock + wave * (kSortBlock / kSortWaves);
     uint32_t key[kSortEach], place[kSortEach], before[kSortEach];
 #pragma unroll
@@ -112,24 +231,38 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
         key[i] = !in ? 0 : FIRST ? key_of(a, t) : from.key[t];
         place[i] = !in ? 0 : FIRST ? (uint32_t)t : from.place[t];
     }
+    // this thread's digit: places of earlier digits, and of earlier workgroups
+    uint32_t at = 0;
+    const uint32_t *row = counts + (int64_t)threadIdx.x * blocks;
+    if (summed) {
+        at = row[blockIdx.x];
+    } else {
+        uint32_t all = 0, mine = 0;
+        for (int b = 0; b < blocks; b += 8) {
+            uint32_t x[8];
+#pragma unroll
+            for (int u = 0; u < 8; u++) x[u] = b + u < blocks ? row[b + u] : 0;
+#pragma unroll
+            for (int u = 0; u < 8; u++) {
+                all += x[u];
+                mine += b + u < (int)blockIdx.x ? x[u] : 0;
+            }
+        }
+        at = digits_before(all, room) + mine;
+    }
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < kSortEach; i++) {
         const bool in = first + i * 64 + lane < a.tokens;
         const uint32_t d = key[i] >> shift & (kDigits - 1);
-        uint64_t same = __ballot(in);
-#pragma unroll
-        for (int b = 0; b < 8; b++) {
-            const uint64_t set = __ballot(d >> b & 1);
-            same &= d >> b & 1 ? set : ~set;
-        }
-        const uint32_t rank = __popcll(same & ((uint64_t(1) << lane) - 1));
+        const uint64_t peers = peers_of(d, in);
+        const int rank = rank_among(peers);
         before[i] = next[wave][d] + rank;
         __builtin_amdgcn_wave_barrier();
-        if (in && rank == 0) next[wave][d] += __popcll(same);
+        if (in && rank == 0) next[wave][d] += __popcll(peers);
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    uint32_t at = sums[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
 #pragma unroll
     for (int w = 0; w < kSortWaves; w++) {
         const uint32_t x = next[w][threadIdx.x];
@@ -147,11 +280,10 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
 }
 
 // --- sums of runs --------------------------------------------------------------------
-// LANES lanes have a chunk of kChunk sorted places and 8 LANES columns.  A run of one id
+// LANES lanes have a chunk of CHUNK sorted places and 8 LANES columns.  A run of one id
 // that lies in the chunk is stored; the part of a run that begins before the chunk goes to
 // part 0 of the chunk, that of a run which goes on behind it to part 1 (a run that does
 // both, to part 0).
-constexpr int kChunk = 32;
 
 template <int LANES>
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int i) {
@@ -169,7 +301,7 @@ __device__ __forceinline__ void store_scaled(const dd_embed_grad_args &a, int64_
     p.store(static_cast<T *>(a.dtable) + id * a.dtable_stride + c, have);
 }
 
-template <class T, int LANES>
+template <class T, int LANES, int CHUNK>
 __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted in, float *part, int64_t chunks, int64_t blocks_of_runs, int64_t strips) {
     constexpr int kGroups = 256 / LANES;
     const int lane = threadIdx.x % LANES;
@@ -203,9 +335,9 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
     if (chunk >= chunks) return;
     const int64_t c = (task - chunk * strips) * (8 * LANES) + 8 * lane;
     const int have = have_of(a.cols, c);
-    const int64_t p0 = chunk * kChunk;
-    const int n = a.tokens - p0 < kChunk ? (int)(a.tokens - p0) : kChunk;
-    constexpr int kHold = kChunk > LANES ? kChunk / LANES : 1;
+    const int64_t p0 = chunk * CHUNK;
+    const int n = a.tokens - p0 < CHUNK ? (int)(a.tokens - p0) : CHUNK;
+    constexpr int kHold = CHUNK > LANES ? CHUNK / LANES : 1;
     uint32_t key[kHold], place[kHold];
 #pragma unroll
     for (int h = 0; h < kHold; h++) {
@@ -215,12 +347,12 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
     }
     auto key_at = [&](int i) { return of_lane<LANES>(key[i / LANES % kHold], i % LANES); };
     const bool from_before = p0 > 0 && in.key[p0 - 1] == key_at(0);
-    const bool goes_on = p0 + n < a.tokens && in.key[p0 + n] == of_lane<LANES>(key[(kChunk - 1) / LANES], (kChunk - 1) % LANES);
+    const bool goes_on = p0 + n < a.tokens && in.key[p0 + n] == of_lane<LANES>(key[(CHUNK - 1) / LANES], (CHUNK - 1) % LANES);
     const T *dy = static_cast<const T *>(a.dy) + c;
     float s[8] = {};
     bool whole = !from_before;      // the run began in this chunk
 #pragma unroll
-    for (int b = 0; b < kChunk; b += 8) {
+    for (int b = 0; b < CHUNK; b += 8) {
         if (b >= n) break;
         Pack<T, 8> p[8];
 #pragma unroll
@@ -238,7 +370,7 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
 #pragma unroll
             for (int j = 0; j < 8; j++) s[j] += x[j];
             const bool last = b + i + 1 == n;
-            if (!last && key_at(b + i + 1 < kChunk ? b + i + 1 : b + i) == k) continue;
+            if (!last && key_at(b + i + 1 < CHUNK ? b + i + 1 : b + i) == k) continue;
             // the run ends, or the chunk does
             if (have > 0 && k < (uint32_t)a.vocab) {
                 if (whole && !(last && goes_on)) {
@@ -256,19 +388,18 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
     }
 }
 
-// Runs over several chunks.  A workgroup has the chunk a run begins in and 64 columns: its 32
-// groups of eight lanes sum every 32nd of the run's parts, and the groups are joined in
-// order.
-template <class T>
-__global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part, int64_t chunks) {
-    __shared__ float lds[32][64];
+// Runs over several chunks.  A workgroup has the chunk a run begins in and 256 columns: its eight groups of
+// 32 lanes sum every eighth of the run's parts, and the groups are joined in order.
+template <class T, int CHUNK>
+__global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part) {
+    __shared__ float lds[8][256];
     __shared__ int64_t last_chunk;
-    const int64_t chunk = blockIdx.x, end = (chunk + 1) * kChunk;
+    const int64_t chunk = blockIdx.x, end = (chunk + 1) * CHUNK;
     if (end >= a.tokens) return;
     const uint32_t k = in.key[end - 1];
     if (k >= (uint32_t)a.vocab || in.key[end] != k) return;
     // (begun in this chunk: its first place has another id, or follows one)
-    if (in.key[end - kChunk] == k && chunk > 0 && in.key[end - kChunk - 1] == k) return;
+    if (in.key[end - CHUNK] == k && chunk > 0 && in.key[end - CHUNK - 1] == k) return;
     if (threadIdx.x == 0) {
         int64_t lo = end, hi = a.tokens;        // the first place behind the run
         while (lo < hi) {
@@ -276,22 +407,26 @@ __global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted
             if (in.key[mid] == k) lo = mid + 1;
             else hi = mid;
         }
-        last_chunk = (lo - 1) / kChunk;
+        last_chunk = (lo - 1) / CHUNK;
     }
     __syncthreads();
     const int64_t last = last_chunk;
-    const int x = threadIdx.x & 7, y = threadIdx.x >> 3;
-    for (int64_t c0 = (int64_t)blockIdx.y * 64; c0 < a.cols; c0 += (int64_t)gridDim.y * 64) {
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.cols; c0 += (int64_t)gridDim.y * 256) {
         const int64_t c = c0 + 8 * x;
         const int have = have_of(a.cols, c);
         float s[8] = {};
         for (int64_t i = chunk + y; i <= last; i += 32) {
-            Pack<float, 8> f;
-            float v[8];
-            f.load(part + (2 * i + (i == chunk ? 1 : 0)) * a.cols + c, have);
-            f.to(v);
+            Pack<float, 8> f[4];
 #pragma unroll
-            for (int j = 0; j < 8; j++) s[j] += v[j];
+            for (int u = 0; u < 4; u++) f[u].load(part + (2 * (i + 8 * u) + (i + 8 * u == chunk ? 1 : 0)) * a.cols + c, i + 8 * u <= last ? have : 0);
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                float v[8];
+                f[u].to(v);
+#pragma unroll
+                for (int j = 0; j < 8; j++) s[j] += v[j];
+            }
         }
         __syncthreads();
 #pragma unroll
@@ -300,7 +435,8 @@ __global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted
         if (y == 0) {
 #pragma unroll
             for (int j = 0; j < 8; j++) s[j] = 0.0f;
-            for (int g = 0; g < 32; g++)
+#pragma unroll
+            for (int g = 0; g < 8; g++)
 #pragma unroll
                 for (int j = 0; j < 8; j++) s[j] += lds[g][8 * x + j];
             if (have > 0) store_scaled<T>(a, k, c, have, s);
@@ -309,6 +445,10 @@ __global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted
 }
 
 // Working memory of the gradient: two lists of sorted tokens, counts, parts.
+// A chunk of few tokens is short: there is little to go round, and what counts is how long one takes
+// (2,047 tokens: 8 us a chunk of 32, 5 of 8).
+constexpr int64_t kSmallTokens = kSmallThreads * 8;
+int chunk_of(int64_t tokens) { return tokens <= kSmallTokens ? 8 : 32; }
 struct Room {
     int64_t blocks, chunks, counts, part, bytes;     // places in bytes
     int passes;
@@ -316,7 +456,7 @@ struct Room {
 Room room_of(int64_t tokens, int64_t vocab, int64_t cols) {
     Room r;
     r.blocks = (tokens + kSortBlock - 1) / kSortBlock;
-    r.chunks = (tokens + kChunk - 1) / kChunk;
+    r.chunks = (tokens + chunk_of(tokens) - 1) / chunk_of(tokens);
     r.passes = 1;
     while (r.passes < 4 && (uint64_t)vocab >> (8 * r.passes)) r.passes++;
     r.counts = (tokens * 16 + 15) / 16 * 16;
@@ -325,34 +465,53 @@ Room room_of(int64_t tokens, int64_t vocab, int64_t cols) {
     return r;
 }
 
-template <class T, int LANES>
-void runs(const dd_embed_grad_args &a, const Sorted &in, float *part, const Room &r, hipStream_t s) {
+// rows: those that no token has are looked up and written too
+template <class T, int LANES, int CHUNK>
+void runs(const dd_embed_grad_args &a, const Sorted &in, float *part, const Room &r, bool rows, hipStream_t s) {
     const int64_t strips = (a.cols + 8 * LANES - 1) / (8 * LANES), groups = 256 / LANES;
-    const int64_t of_runs = (r.chunks * strips + groups - 1) / groups, of_rows = (a.vocab + 255) / 256;
-    k_embed_runs<T, LANES><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, of_runs, strips);
-    if (r.chunks > 1)
-        k_embed_join<T><<<dim3((unsigned)r.chunks, (unsigned)((a.cols + 63) / 64 < 1024 ? (a.cols + 63) / 64 : 1024)), 256, 0, s>>>(a, in, part, r.chunks);
+    const int64_t of_runs = (r.chunks * strips + groups - 1) / groups, of_rows = rows ? (a.vocab + 255) / 256 : 0;
+    k_embed_runs<T, LANES, CHUNK><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, of_runs, strips);
+    if (r.chunks > 1) {
+        const int64_t y = (a.cols + 255) / 256;
+        k_embed_join<T, CHUNK><<<dim3((unsigned)r.chunks, (unsigned)(y < 1024 ? y : 1024)), 256, 0, s>>>(a, in, part);
+    }
 }
 
 template <class T>
 void embed_grad(const dd_embed_grad_args &a, void *work, hipStream_t s) {
     const Room r = room_of(a.tokens, a.vocab, a.cols);
     char *w = static_cast<char *>(work);
-    uint32_t *list = reinterpret_cast<uint32_t *>(w), *counts = reinterpret_cast<uint32_t *>(w + r.counts);
+    uint32_t *list = reinterpret_cast<uint32_t *>(w);
     float *part = reinterpret_cast<float *>(w + r.part);
     Sorted from{list, list + a.tokens}, to{list + 2 * a.tokens, list + 3 * a.tokens};
-    for (int i = 0; i < r.passes && a.tokens > 0; i++) {
-        if (i == 0) k_embed_count<true><<<(unsigned)r.blocks, kSortThreads, 0, s>>>(a, from, 8 * i, counts);
-        else k_embed_count<false><<<(unsigned)r.blocks, kSortThreads, 0, s>>>(a, from, 8 * i, counts);
-        k_embed_scan<<<1, 1024, 0, s>>>(counts, r.blocks * kDigits);
-        if (i == 0) k_embed_scatter<true><<<(unsigned)r.blocks, kSortThreads, 0, s>>>(a, from, to, 8 * i, counts);
-        else k_embed_scatter<false><<<(unsigned)r.blocks, kSortThreads, 0, s>>>(a, from, to, 8 * i, counts);
-        const Sorted x = from;
-        from = to;
-        to = x;
+    // Few tokens in a large table: nearly all of it is zeros, which are written while the tokens are sorted (a row
+    // that a token has twice then).  Many: the rows that no token has are looked up and written with the
+    // sums (65,536 tokens of 32,000 x 1,024 bf16 would write 40 MB twice).
+    const bool fill = a.tokens > 0 && a.tokens < a.vocab / 8;
+    const int64_t packs = a.vocab * ((a.cols + 7) / 8);
+    auto fillers = [&](int threads) { return fill ? (packs + 4 * threads - 1) / (4 * threads) < 2048 ? (packs + 4 * threads - 1) / (4 * threads) : 2048 : 0; };
+    if (a.tokens > 0 && a.tokens <= kSmallTokens) {
+        const unsigned grid = (unsigned)(1 + fillers(kSmallThreads));
+        if (a.tokens <= 2 * kSmallThreads) k_embed_sort<T, 2><<<grid, kSmallThreads, 0, s>>>(a, from, r.passes);
+        else k_embed_sort<T, 8><<<grid, kSmallThreads, 0, s>>>(a, from, r.passes);
+    } else if (a.tokens > 0) {
+        uint32_t *counts = reinterpret_cast<uint32_t *>(w + r.counts);
+        const unsigned blocks = (unsigned)r.blocks;
+        const bool summed = r.blocks > kManyBlocks;
+        for (int i = 0; i < r.passes; i++) {
+            if (i == 0) k_embed_count<T, true><<<(unsigned)(r.blocks + fillers(kSortThreads)), kSortThreads, 0, s>>>(a, from, 0, (int)r.blocks, counts);
+            else k_embed_count<T, false><<<blocks, kSortThreads, 0, s>>>(a, from, 8 * i, (int)r.blocks, counts);
+            if (summed) k_embed_scan<<<1, 1024, 0, s>>>(counts, r.blocks * kDigits);
+            if (i == 0) k_embed_scatter<true><<<blocks, kSortThreads, 0, s>>>(a, from, to, 0, counts, summed);
+            else k_embed_scatter<false><<<blocks, kSortThreads, 0, s>>>(a, from, to, 8 * i, counts, summed);
+            const Sorted x = from;
+            from = to;
+            to = x;
+        }
     }
-    if (a.cols <= 128) runs<T, 16>(a, from, part, r, s);
-    else runs<T, 64>(a, from, part, r, s);
+    const bool small = a.tokens <= kSmallTokens;
+    if (a.cols <= 128) small ? runs<T, 16, 8>(a, from, part, r, !fill, s) : runs<T, 16, 32>(a, from, part, r, !fill, s);
+    else small ? runs<T, 64, 8>(a, from, part, r, !fill, s) : runs<T, 64, 32>(a, from, part, r, !fill, s);
 }
 
 }  // namespace
