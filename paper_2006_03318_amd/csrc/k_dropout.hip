@@ -35,7 +35,8 @@ __device__ __forceinline__ Words philox(uint64_t i, uint64_t c, uint64_t key) {
 }
 
 // Where the eight elements from number 8 i on lie: in a row (FLAT: all of the array
-// is one), in one row of several (ROWS: cols is a multiple of 8), or anywhere.
+// is one), in one row of several (ROWS: cols is a multiple of 8), or (ANY) at the end of one row and the
+// beginning of others too.
 enum { FLAT, ROWS, ANY };
 
 template <int WHERE>
@@ -50,7 +51,7 @@ struct At {
     }
     template <class T>
     __device__ __forceinline__ void load(const T *p, int64_t stride, int have, Pack<T, 8> &v) const {
-        if (WHERE != ANY) {
+        if (WHERE != ANY || col + have <= a.cols) {
             v.load(p + row * stride + col, have);
             return;
         }
@@ -66,7 +67,7 @@ struct At {
     }
     template <class T>
     __device__ __forceinline__ void store(T *p, int64_t stride, int have, const Pack<T, 8> &v) const {
-        if (WHERE != ANY) {
+        if (WHERE != ANY || col + have <= a.cols) {
             v.store(p + row * stride + col, have);
             return;
         }

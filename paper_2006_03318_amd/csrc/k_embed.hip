@@ -175,7 +175,14 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_sort(dd_embed_grad_args
 constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kSortEach = 8, kSortBlock = kSortThreads * kSortEach;
 static_assert(kSortThreads == kDigits, "a thread has a digit");
 
-// counts[digit][workgroup]: a workgroup's places with each digit; the workgroups behind fill the table
+// A workgroup's places with each digit lie digit by digit (those to be summed by a scan) or workgroup by
+// workgroup (which threads of a digit each read side by side).
+constexpr int kManyBlocks = 512;
+__device__ __forceinline__ int64_t count_at(int digit, int64_t block, int64_t blocks) {
+    return blocks > kManyBlocks ? digit * blocks + block : block * kDigits + digit;
+}
+
+// the counts; the workgroups behind fill the table
 template <class T, bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args a, Sorted from, int shift, int blocks, uint32_t *counts) {
     if ((int)blockIdx.x >= blocks) {
@@ -196,29 +203,35 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args
     for (int i = 0; i < kSortEach; i++)
         if (first + i * kSortThreads + threadIdx.x < a.tokens) atomicAdd(&n[key[i] >> shift & (kDigits - 1)], 1u);
     __syncthreads();
-    counts[(int64_t)threadIdx.x * blocks + blockIdx.x] = n[threadIdx.x];
+    counts[count_at(threadIdx.x, blockIdx.x, blocks)] = n[threadIdx.x];
 }
 
-// Running sums of all counts, in place, where there are too many workgroups for each to sum them by itself:
-// each of 1,024 threads has a run of them.
-constexpr int kManyBlocks = 512;
-__global__ void __launch_bounds__(1024) k_embed_scan(uint32_t *counts, int64_t n) {
-    __shared__ uint32_t room[16];
-    const int64_t each = (n + 1023) / 1024, i0 = threadIdx.x * each, i1 = i0 + each < n ? i0 + each : n;
-    uint32_t sum = 0;
-    for (int64_t i = i0; i < i1; i++) sum += counts[i];
-    uint32_t before = digits_before(sum, room);
-    for (int64_t i = i0; i < i1; i++) {
-        const uint32_t x = counts[i];
-        counts[i] = before;
-        before += x;
+// Where there are too many workgroups for each to sum the others' counts: a workgroup has a digit, makes running sums of its
+// counts in place, and puts their sum behind all counts.
+__global__ void __launch_bounds__(256) k_embed_scan(uint32_t *counts, int64_t blocks) {
+    __shared__ uint32_t room[4];
+    uint32_t *row = counts + blockIdx.x * blocks, sum = 0;
+    for (int64_t i0 = 0; i0 < blocks; i0 += 1024) {
+        const int64_t i = i0 + 4 * threadIdx.x;
+        uint32_t x[4], each = 0;
+#pragma unroll
+        for (int u = 0; u < 4; u++) each += x[u] = i + u < blocks ? row[i + u] : 0;
+        uint32_t before = sum + digits_before(each, room);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            if (i + u < blocks) row[i + u] = before;
+            before += x[u];
+        }
+        sum += room[0] + room[1] + room[2] + room[3];
+        __syncthreads();
     }
+    if (threadIdx.x == 0) counts[kDigits * blocks + blockIdx.x] = sum;
 }
 
 // Every place to where the counts and its rank in the workgroup say.  (Counting the next pass's digits here, by
 // atomics where the places go, takes 85 us of 65,536 words of a language, whose high digits are mostly one.)
 template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_args a, Sorted from, Sorted to, int shift, const uint32_t *counts, bool summed) {
+__global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_args a, Sorted from, Sorted to, int shift, const uint32_t *counts) {
     __shared__ uint32_t next[kSortWaves][kDigits], room[kSortWaves];      // next: first counts, then places to come
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = gridDim.x;
     for (int i = lane; i < kDigits; i += 64) next[wave][i] = 0;
@@ -233,15 +246,14 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
     }
     // this thread's digit: places of earlier digits, and of earlier workgroups
     uint32_t at = 0;
-    const uint32_t *row = counts + (int64_t)threadIdx.x * blocks;
-    if (summed) {
-        at = row[blockIdx.x];
+    if (blocks > kManyBlocks) {
+        at = digits_before(counts[(int64_t)kDigits * blocks + threadIdx.x], room) + counts[count_at(threadIdx.x, blockIdx.x, blocks)];
     } else {
         uint32_t all = 0, mine = 0;
         for (int b = 0; b < blocks; b += 8) {
             uint32_t x[8];
 #pragma unroll
-            for (int u = 0; u < 8; u++) x[u] = b + u < blocks ? row[b + u] : 0;
+            for (int u = 0; u < 8; u++) x[u] = b + u < blocks ? counts[count_at(threadIdx.x, b + u, blocks)] : 0;
 #pragma unroll
             for (int u = 0; u < 8; u++) {
                 all += x[u];
@@ -460,7 +472,7 @@ Room room_of(int64_t tokens, int64_t vocab, int64_t cols) {
     r.passes = 1;
     while (r.passes < 4 && (uint64_t)vocab >> (8 * r.passes)) r.passes++;
     r.counts = (tokens * 16 + 15) / 16 * 16;
-    r.part = r.counts + r.blocks * kDigits * 4;
+    r.part = r.counts + (r.blocks + 1) * kDigits * 4;
     r.bytes = r.part + r.chunks * 2 * cols * 4;
     return r;
 }
@@ -497,13 +509,12 @@ void embed_grad(const dd_embed_grad_args &a, void *work, hipStream_t s) {
     } else if (a.tokens > 0) {
         uint32_t *counts = reinterpret_cast<uint32_t *>(w + r.counts);
         const unsigned blocks = (unsigned)r.blocks;
-        const bool summed = r.blocks > kManyBlocks;
         for (int i = 0; i < r.passes; i++) {
             if (i == 0) k_embed_count<T, true><<<(unsigned)(r.blocks + fillers(kSortThreads)), kSortThreads, 0, s>>>(a, from, 0, (int)r.blocks, counts);
             else k_embed_count<T, false><<<blocks, kSortThreads, 0, s>>>(a, from, 8 * i, (int)r.blocks, counts);
-            if (summed) k_embed_scan<<<1, 1024, 0, s>>>(counts, r.blocks * kDigits);
-            if (i == 0) k_embed_scatter<true><<<blocks, kSortThreads, 0, s>>>(a, from, to, 0, counts, summed);
-            else k_embed_scatter<false><<<blocks, kSortThreads, 0, s>>>(a, from, to, 8 * i, counts, summed);
+            if (r.blocks > kManyBlocks) k_embed_scan<<<kDigits, 256, 0, s>>>(counts, r.blocks);
+            if (i == 0) k_embed_scatter<true><<<blocks, kSortThreads, 0, s>>>(a, from, to, 0, counts);
+            else k_embed_scatter<false><<<blocks, kSortThreads, 0, s>>>(a, from, to, 8 * i, counts);
             const Sorted x = from;
             from = to;
             to = x;
