@@ -28,8 +28,21 @@ struct Product {
     int64_t p_stride, q_stride;
     int32_t p_by_rows, q_by_rows;
     int32_t type;
+    int32_t padded;             // 1: p's, 2: q's rows are padded with zeros to 16 bytes, whatever their length
     Epilogue e;
 };
+
+// Rows of 16-bit elements copied end to end, padded with zeros to 16 bytes (no rows: nothing).
+struct PadRows {
+    const void *from;
+    void *to;
+    int64_t stride, rows, cols;
+};
+size_t padded_size(int64_t rows, int64_t cols);
+// x and its stride become those of the copy in `to`; the size of the copy
+size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, void *to, PadRows *r);
+hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, hipStream_t s);
+
 
 // bytes of working memory of an m by n product of k sums (0: none), and the product
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_by_rows);

@@ -88,7 +88,7 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
         if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
         CHECK(check_product(a->rows, a->n, a->k, true));
-        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, {}};
+        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, 0, {}};
         p.e.bias = a->bias;
         p.e.bias_type = a->bias_type;
         p.e.act = a->act;
@@ -103,11 +103,19 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
     });
 }
 
+// Whether the gradients of the weight and of the rows are taken from copies padded once for both (dy's rows
+// cannot be loaded as they are, and each is read many times).
+static bool pads_once(int64_t rows, int64_t k, int64_t n) { return n % 8 && rows > 64 && k > 64 && n > 64; }
+static size_t pads_once_size(int64_t rows, int64_t k, int64_t n) {
+    const size_t w = dd::padded_size(k, n), turned = dd::padded_size(n, k);
+    return dd::padded_size(rows, n) + dd::padded_size(rows, k) + (w > turned ? w : turned);
+}
+
 size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
     if (!sizes_known(rows, k, n)) return 0;
     size_t most = dd::column_sum_work(rows, n);
     for (size_t x : {rows > 0 ? dd::product_work(rows, k, n, true) : 0, dd::product_work(k, n, rows, false), dd::product_work(n, k, rows, false)}) most = x > most ? x : most;
-    return most;
+    return most + (pads_once(rows, k, n) ? pads_once_size(rows, k, n) : 0);
 }
 
 dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
@@ -138,23 +146,35 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
         if (a->dw) needs(dd::product_work(wr, wc, a->rows, false));
         if (a->db) needs(dd::column_sum_work(a->rows, a->n));
         if (a->dx && a->rows > 0) needs(dd::product_work(a->rows, a->k, a->n, true));
-        return with_work(a->work, need, s, "linear gradient", [&](void *work) {
+        const bool pad = a->dw && a->dx && pads_once(a->rows, a->k, a->n);
+        if (pad) need += pads_once_size(a->rows, a->k, a->n);
+        return with_work(a->work, need, s, "linear gradient", [&](void *given) {
+            char *work = static_cast<char *>(given);
+            const void *dy = a->dy, *x = a->x, *w = a->w;
+            int64_t dy_stride = a->dy_stride, x_stride = a->x_stride, w_stride = a->w_stride;
             hipError_t e = hipSuccess;
-            if (a->dw) {
-                dd::Product p{a->x, a->dy, wr, wc, a->rows, a->x_stride, a->dy_stride, 0, 0, a->type, {}};
+            if (pad) {
+                dd::PadRows r[3];
+                work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, &r[0]);
+                work += dd::pad_rows(x, x_stride, a->rows, a->k, work, &r[1]);
+                work += dd::pad_rows(w, w_stride, wr, wc, work, &r[2]);
+                e = dd::launch_pad_rows(r[0], r[1], r[2], s);
+            }
+            if (e == hipSuccess && a->dw) {
+                dd::Product p{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, pad ? 3 : 0, {}};
                 if (a->turned) {
-                    p.p = a->dy;
-                    p.p_stride = a->dy_stride;
-                    p.q = a->x;
-                    p.q_stride = a->x_stride;
+                    p.p = dy;
+                    p.p_stride = dy_stride;
+                    p.q = x;
+                    p.q_stride = x_stride;
                 }
                 p.e.out = a->dw;
                 p.e.out_stride = a->dw_stride;
                 e = dd::launch_product(p, work, s);
             }
-            if (e == hipSuccess && a->db) e = dd::launch_column_sum(a->dy, a->dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
+            if (e == hipSuccess && a->db) e = dd::launch_column_sum(dy, dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
             if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
-                dd::Product p{a->dy, a->w, a->rows, a->k, a->n, a->dy_stride, a->w_stride, 1, !a->turned, a->type, {}};
+                dd::Product p{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, pad ? 3 : 0, {}};
                 p.e.in_z = a->in_z;
                 p.e.side_stride = a->in_z_stride;
                 p.e.in_act = a->in_act;

@@ -44,11 +44,11 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
 // --- which tiles, and how sums are cut -------------------------------------------
 int64_t tiles_of(int64_t x, int64_t n) { return (x + n - 1) / n; }
 
-constexpr double kStepApart[2] = {1.0, 0.6}, kEndApart = 2.0;
 // Tile and parts that are expected to take least, from what was measured (us): a step of 64 sums of one
 // tile per compute unit takes 1.44 with 256 x 256 (8,192^3 bf16 in 768) and 0.53 with 128 x 128 (4,096 x 4,096 ->
-// 1,024 in 37), 0.83 with operands of any alignment; an epilogue 7.5 and 2 (its stores); joining
-// parts another launch and its traffic.
+// 1,024 in 37), 0.83 with operands of any alignment; an epilogue 7.5 and 2 (its stores).  Where waves share
+// the sums of 64 x 64, a wave's step takes 0.75 of four waves and the end 2.4 (1,024 x 1,024 -> 768 in 8, of
+// any alignment 2.5 of eight waves, and 4).  Joining parts takes another launch and its traffic.
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
     Plan p{0, 0, 0, 1, 0};
     double least = 0.0;
@@ -60,7 +60,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
         for (int64_t s = 1; s <= tiles_of(steps, waves); s *= 2) {
             const int64_t each = tiles_of(tiles_of(steps, waves), s) * waves, rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
             double us = tile == 256 ? (each * 1.44 + 7.5) * rounds : tile == 128 ? (each * (direct ? 0.53 : 0.83) + 2.0) * rounds
-                      : (each / waves * kStepApart[direct] + kEndApart) * rounds;
+                      : (each / waves * (direct ? 0.75 : 2.5) + (direct ? 2.4 : 4.0)) * rounds;
             if (s > 1) us += 4.0 + 4e-6 / 3.0 * (double)(2 * s) * (double)m * (double)n;
             if (p.tile && us >= least) continue;
             least = us;
@@ -78,28 +78,23 @@ size_t plan_work(const Plan &p, int64_t m, int64_t n) { return p.splits > 1 ? (s
 
 // An operand that loads go to LDS directly from: 16 bytes in a row lie aligned, all of
 // one row (or one l), and a tile spans less than 2 GiB.
-bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (by_rows ? k : count) % 8 == 0 && stride < (int64_t(1) << 22);
+bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k, bool padded) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (padded || (by_rows ? k : count) % 8 == 0) && stride < (int64_t(1) << 22);
 }
 
 // --- operands of odd sizes --------------------------------------------------------
 // Rows that are not multiples of 16 bytes cannot be loaded to LDS directly, which makes a step half as fast and
 // more.  Where the sizes themselves are odd and an operand is read many times, it is copied first, rows padded with
 // zeros to 16 bytes.  4,099 x 1,237 -> 777 f16 24 us (32 without), 1,021 x 777 x 1,237 14 (18 to 25).
-struct Rows {
-    const bf16_t *from;          // (16 bits, whatever they mean)
-    bf16_t *to;
-    int64_t stride, rows, cols;
-    __host__ __device__ int64_t packs() const { return (cols + 7) / 8; }
-};
-__global__ void __launch_bounds__(256) k_pad_rows(Rows x, Rows y) {
-    const Rows &r = blockIdx.y ? y : x;
-    const int64_t packs = r.packs(), total = packs * r.rows;
+__global__ void __launch_bounds__(256) k_pad_rows(PadRows x, PadRows y, PadRows z) {
+    const PadRows &r = blockIdx.y == 0 ? x : blockIdx.y == 1 ? y : z;
+    const int64_t packs = (r.cols + 7) / 8, total = packs * r.rows;
+    const bf16_t *from = static_cast<const bf16_t *>(r.from);       // (16 bits, whatever they mean)
     for (int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
         const int64_t i = t / packs, j = (t - i * packs) * 8;
         Pack<bf16_t, 8> v;
-        v.load(r.from + i * r.stride + j, r.cols - j >= 8 ? 8 : (int)(r.cols - j));
-        v.store(r.to + t * 8);
+        v.load(from + i * r.stride + j, r.cols - j >= 8 ? 8 : (int)(r.cols - j));
+        v.store(static_cast<bf16_t *>(r.to) + t * 8);
     }
 }
 bool pads(int64_t m, int64_t n, int64_t k) { return (m % 8 || n % 8 || k % 8) && m > 64 && n > 64; }
@@ -111,24 +106,18 @@ size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
 template <class T>
 hipError_t product(const Product &args, char *work, hipStream_t s) {
     Product a = args;
-    const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k), aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k);
+    const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k, a.padded & 1);
+    const bool aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k, a.padded & 2);
     const bool pad = !(ap && aq) && pads(a.m, a.n, a.k), direct = (ap && aq) || pad;
     const Plan p = plan_of(a.m, a.n, a.k, a.p_by_rows, direct);
     float *part = reinterpret_cast<float *>(work);
     if (pad) {
-        bf16_t *to = reinterpret_cast<bf16_t *>(work + (plan_work(p, a.m, a.n) + 15) / 16 * 16);
-        auto padded = [&](const void *&x, int64_t &stride, int64_t rows, int64_t cols) {
-            const Rows r{static_cast<const bf16_t *>(x), to, stride, rows, cols};
-            x = to;
-            stride = r.packs() * 8;
-            to += rows * stride;
-            return r;
-        };
-        Rows x{}, y{};
-        if (!ap) x = a.p_by_rows ? padded(a.p, a.p_stride, a.m, a.k) : padded(a.p, a.p_stride, a.k, a.m);
-        if (!aq) (ap ? x : y) = a.q_by_rows ? padded(a.q, a.q_stride, a.n, a.k) : padded(a.q, a.q_stride, a.k, a.n);
-        const int64_t need = tiles_of(x.packs() * x.rows > y.packs() * y.rows ? x.packs() * x.rows : y.packs() * y.rows, 256);
-        k_pad_rows<<<dim3((unsigned)(need < 8 * kUnits ? need : 8 * kUnits), y.rows ? 2 : 1), 256, 0, s>>>(x, y);
+        char *to = work + (plan_work(p, a.m, a.n) + 15) / 16 * 16;
+        PadRows x{}, y{};
+        if (!ap) to += pad_rows(a.p, a.p_stride, a.p_by_rows ? a.m : a.k, a.p_by_rows ? a.k : a.m, to, &x);
+        if (!aq) pad_rows(a.q, a.q_stride, a.q_by_rows ? a.n : a.k, a.q_by_rows ? a.k : a.n, to, &y);
+        const hipError_t e = launch_pad_rows(x, y, PadRows{}, s);
+        if (e != hipSuccess) return e;
     }
     if (direct) launch_tiles<T, true>(a, p, part, s);
     else launch_tiles<T, false>(a, p, part, s);
@@ -214,8 +203,48 @@ __global__ void __launch_bounds__(1024) k_column_join(const float *part, int n, 
     store_as(out, out_type, c, s);
 }
 
+// Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  1,021 x 1,237 f16 4.4 us
+// (7.5 with parts).
+constexpr int kFewRows = 4096;
+template <class T>
+__global__ void __launch_bounds__(1024) k_column_sum_few(const T *x, int64_t stride, int rows, int64_t cols, void *out, int32_t out_type) {
+    __shared__ float lds[128][65];
+    const int cx = threadIdx.x % 8, cy = threadIdx.x / 8;
+    const int64_t c = (int64_t)blockIdx.x * 64 + 8 * cx;
+    const int have = cols - c >= 8 ? 8 : cols - c < 0 ? 0 : (int)(cols - c);
+    float s[8] = {};
+    for (int r = cy; r < rows; r += 512) {
+        Pack<T, 8> p[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i].load(x + (r + i * 128) * stride + c, r + i * 128 < rows ? have : 0);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float v[8];
+            p[i].to(v);
+#pragma unroll
+            for (int j = 0; j < 8; j++) s[j] += v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds[cy][8 * cx + j] = s[j];
+    __syncthreads();
+    const int y = threadIdx.x / 64, mine = threadIdx.x % 64;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) t += lds[y * 8 + i][mine];
+    __syncthreads();
+    lds[y][mine] = t;
+    __syncthreads();
+    if (y || (int64_t)blockIdx.x * 64 + mine >= cols) return;
+    t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t += lds[i][mine];
+    store_as(out, out_type, (int64_t)blockIdx.x * 64 + mine, t);
+}
+
 // parts of the rows: enough workgroups to fill the card, of 32 rows at least
 int sum_parts(int64_t rows, int64_t cols) {
+    if (rows <= kFewRows) return 1;
     const int64_t blocks = tiles_of(cols, kSumCols);
     int64_t n = tiles_of(4 * kUnits, blocks), most = rows / 32;
     if (n > most) n = most;
@@ -247,6 +276,22 @@ __global__ void __launch_bounds__(256) k_act_grad(dd_act_grad_args a) {
 
 }  // namespace
 
+size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, void *to, PadRows *r) {
+    *r = PadRows{x, to, stride, rows, cols};
+    x = to;
+    stride = tiles_of(cols, 8) * 8;
+    return padded_size(rows, cols);
+}
+
+size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)tiles_of(cols, 8) * 16; }
+
+hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, hipStream_t s) {
+    int64_t most = 1;
+    for (const PadRows *r : {&x, &y, &z}) most = tiles_of(tiles_of(r->cols, 8) * r->rows, 256) > most ? tiles_of(tiles_of(r->cols, 8) * r->rows, 256) : most;
+    k_pad_rows<<<dim3((unsigned)(most < 8 * kUnits ? most : 8 * kUnits), z.rows ? 3 : y.rows ? 2 : 1), 256, 0, s>>>(x, y, z);
+    return hipGetLastError();
+}
+
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_rows) {
     const size_t a = (plan_work(plan_of(m, n, k, p_rows, true), m, n) + 15) / 16 * 16 + pad_work(m, n, k), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
     return a > b ? a : b;
@@ -271,6 +316,12 @@ size_t column_sum_work(int64_t rows, int64_t cols) {
 
 hipError_t launch_column_sum(const void *x, int64_t stride, int64_t rows, int64_t cols, int32_t type, void *out, int32_t out_type, void *work,
                              hipStream_t s) {
+    if (rows <= kFewRows) {
+        const unsigned grid = (unsigned)tiles_of(cols, 64);
+        if (type == DD_BF16) k_column_sum_few<bf16_t><<<grid, 1024, 0, s>>>(static_cast<const bf16_t *>(x), stride, (int)rows, cols, out, out_type);
+        else k_column_sum_few<f16_t><<<grid, 1024, 0, s>>>(static_cast<const f16_t *>(x), stride, (int)rows, cols, out, out_type);
+        return hipGetLastError();
+    }
     const int n = sum_parts(rows, cols);
     const int64_t run = tiles_of(rows, n);
     float *part = static_cast<float *>(work);

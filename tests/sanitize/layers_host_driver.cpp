@@ -12,6 +12,12 @@ namespace dd {
 size_t product_work(int64_t m, int64_t n, int64_t k, bool) { return k > 1000 ? (size_t)m * (size_t)n * 8 : 0; }
 bool product_fits(int64_t m, int64_t n, int64_t, bool) { return m < (1 << 30) && n < (1 << 30); }
 hipError_t launch_product(const Product &, void *, hipStream_t) { STUB; }
+size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)cols * 2; }
+size_t pad_rows(const void *&, int64_t &, int64_t rows, int64_t cols, void *, PadRows *r) {
+    *r = PadRows{};
+    return padded_size(rows, cols);
+}
+hipError_t launch_pad_rows(const PadRows &, const PadRows &, const PadRows &, hipStream_t) { STUB; }
 size_t column_sum_work(int64_t, int64_t cols) { return (size_t)cols * 4; }
 hipError_t launch_column_sum(const void *, int64_t, int64_t, int64_t, int32_t, void *, int32_t, void *, hipStream_t) { STUB; }
 hipError_t launch_act_grad(const dd_act_grad_args &, hipStream_t) { STUB; }
