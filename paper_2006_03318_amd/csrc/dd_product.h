@@ -454,7 +454,8 @@ __global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *
     __shared__ __attribute__((aligned(1024))) char lds[WAVES * STAGES * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr<char>)(lds), mine = lds0 + wave * (STAGES * kStage);
-    const Place at = place_of(blockIdx.x, tm, tn, splits);
+    // (few rows: what is read is the weight, a part of it by each workgroup alone)
+    const Place at = MT == 1 ? Place{0, (int)(blockIdx.x % tn), (int)(blockIdx.x / tn)} : place_of(blockIdx.x, tm, tn, splits);
     const int64_t m0 = (int64_t)at.m * (16 * MT), n0 = (int64_t)at.n * BN, s0 = at.split * k_part, s1 = s0 + k_part < a.k ? s0 + k_part : a.k;
     const int64_t each = ((s1 - s0 + WAVES * BK - 1) / (WAVES * BK)) * BK;
     const int64_t k0 = s0 + wave * each, k1 = k0 + each < s1 ? k0 + each : s1;

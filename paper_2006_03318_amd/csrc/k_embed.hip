@@ -400,11 +400,12 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
     }
 }
 
-// Runs over several chunks.  A workgroup has the chunk a run begins in and 256 columns: its eight groups of
-// 32 lanes sum every eighth of the run's parts, and the groups are joined in order.
+// Runs over several chunks.  A workgroup has the chunk a run begins in and 256 columns: its four groups of
+// 32 lanes sum every fourth of the run's parts, and the groups are joined in order.
+constexpr int kJoinGroups = 4;
 template <class T, int CHUNK>
-__global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part) {
-    __shared__ float lds[8][256];
+__global__ void __launch_bounds__(32 * kJoinGroups) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part) {
+    __shared__ float lds[kJoinGroups][256];
     __shared__ int64_t last_chunk;
     const int64_t chunk = blockIdx.x, end = (chunk + 1) * CHUNK;
     if (end >= a.tokens) return;
@@ -428,10 +429,10 @@ __global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted
         const int64_t c = c0 + 8 * x;
         const int have = have_of(a.cols, c);
         float s[8] = {};
-        for (int64_t i = chunk + y; i <= last; i += 32) {
+        for (int64_t i = chunk + y; i <= last; i += 4 * kJoinGroups) {
             Pack<float, 8> f[4];
 #pragma unroll
-            for (int u = 0; u < 4; u++) f[u].load(part + (2 * (i + 8 * u) + (i + 8 * u == chunk ? 1 : 0)) * a.cols + c, i + 8 * u <= last ? have : 0);
+            for (int u = 0; u < 4; u++) f[u].load(part + (2 * (i + kJoinGroups * u) + (i + kJoinGroups * u == chunk ? 1 : 0)) * a.cols + c, i + kJoinGroups * u <= last ? have : 0);
 #pragma unroll
             for (int u = 0; u < 4; u++) {
                 float v[8];
@@ -448,7 +449,7 @@ __global__ void __launch_bounds__(256) k_embed_join(dd_embed_grad_args a, Sorted
 #pragma unroll
             for (int j = 0; j < 8; j++) s[j] = 0.0f;
 #pragma unroll
-            for (int g = 0; g < 8; g++)
+            for (int g = 0; g < kJoinGroups; g++)
 #pragma unroll
                 for (int j = 0; j < 8; j++) s[j] += lds[g][8 * x + j];
             if (have > 0) store_scaled<T>(a, k, c, have, s);
@@ -485,7 +486,7 @@ void runs(const dd_embed_grad_args &a, const Sorted &in, float *part, const Room
     k_embed_runs<T, LANES, CHUNK><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, of_runs, strips);
     if (r.chunks > 1) {
         const int64_t y = (a.cols + 255) / 256;
-        k_embed_join<T, CHUNK><<<dim3((unsigned)r.chunks, (unsigned)(y < 1024 ? y : 1024)), 256, 0, s>>>(a, in, part);
+        k_embed_join<T, CHUNK><<<dim3((unsigned)r.chunks, (unsigned)(y < 1024 ? y : 1024)), 32 * kJoinGroups, 0, s>>>(a, in, part);
     }
 }
 
