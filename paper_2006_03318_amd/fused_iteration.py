@@ -5,10 +5,12 @@ as it is, the trace is transformed and simulated, and the prediction is held
 against the optimization itself.  The iteration here is a stack of residual
 blocks in bf16 (norm, two products with a GELU between them) with Adam on f32
 masters and clipped gradients.  `--plain` runs norms and updates as single
-torch operations, tensor by tensor; `--fused` runs them with this library.
+torch operations, tensor by tensor; `--fused` runs them with this library, and
+`--products` the products too, with the activation and its derivative in them.
 
     python -m paper_2006_03318_amd.fused_iteration --plain
     python -m paper_2006_03318_amd.fused_iteration --fused
+    python -m paper_2006_03318_amd.fused_iteration --fused --products
     rocprofv3 --kernel-trace --hip-runtime-trace --memory-copy-trace --marker-trace \\
         --output-format csv -d OUT -o run -- \\
         python3 -m paper_2006_03318_amd.fused_iteration --plain
@@ -41,7 +43,7 @@ ADAM = dict(lr=1e-4, betas=(0.9, 0.95), eps=1e-8, weight_decay=0.1, max_norm=1.0
 
 # ---------------------------------------------------------------------------
 # the iteration
-def make_stack(hidden: int, layers: int, fused: bool, seed: int = 0, device="cuda"):
+def make_stack(hidden: int, layers: int, fused: bool, seed: int = 0, device="cuda", products: bool = False):
     """The blocks as a module: forward(x) of [rows, hidden] in bf16."""
     import torch
     from torch import nn
@@ -69,6 +71,8 @@ def make_stack(hidden: int, layers: int, fused: bool, seed: int = 0, device="cud
             self.up, self.down = w(hidden, 4 * hidden), w(4 * hidden, hidden)
 
         def forward(self, x):
+            if products:
+                return training.mlp(x, self.up, self.down, act="gelu")
             return torch.nn.functional.gelu(x @ self.up) @ self.down
 
     class Stack(nn.Module):
@@ -142,11 +146,11 @@ def mark(stack):
             mod.register_full_backward_hook(end)
 
 
-def train(hidden: int, layers: int, rows: int, steps: int, fused: bool, marked: bool = False):
+def train(hidden: int, layers: int, rows: int, steps: int, fused: bool, marked: bool = False, products: bool = False):
     """Milliseconds of an iteration after three to warm up, and the losses."""
     import torch
     from . import training
-    stack = make_stack(hidden, layers, fused)
+    stack = make_stack(hidden, layers, fused, products=products)
     if marked:
         mark(stack)
     opt = (training.Adam if fused else PlainAdam)(stack.parameters(), **ADAM)
@@ -192,6 +196,16 @@ class FuseLayers(R.Recipe):
         R.remove_tasks(plan, g, gone)
 
 
+@dataclasses.dataclass
+class FuseIntoProducts(R.Recipe):
+    """The element-wise kernels of these layers go, with their launch calls: what
+    they do becomes part of the matrix products beside them, which take as long."""
+    layers: Sequence[int]
+
+    def apply(self, g, plan):
+        R.remove_tasks(plan, g, (g.kind == W.K_ELEM) & R.in_layers(g, self.layers) & ~plan.removed)
+
+
 def what_if(tg: TR.TraceGraph):
     """(graph, variants, their names): the iteration as traced, with its weight
     update fused, with its norms fused, with both, and both with the update at
@@ -208,11 +222,23 @@ def what_if(tg: TR.TraceGraph):
     return g2, vs, names
 
 
-def predict(directory: str, iterations: Sequence[int]):
+def what_if_products(tg: TR.TraceGraph):
+    """(graph, variants, their names): the activations fused into the products, and
+    all of it (norms, update in one pass, activations)."""
+    g = tg.graph
+    update = [i for i, n in enumerate(tg.layer_names) if n == "weight update"]
+    norms = [i for i, n in enumerate(tg.layer_names) if "norm " in n]
+    mlps = FuseIntoProducts([i for i, n in enumerate(tg.layer_names) if "mlp " in n])
+    g.kind[R.is_kernel(g) & R.in_layers(g, update)] = W.K_OPT
+    g2, vs = R.compile_sweep(g, [[mlps], [R.ScaleLayers(update, 1, 4), R.FusedAdam(), FuseLayers(norms), mlps]])
+    return g2, vs, ["activations in the products", "all, update in one pass"]
+
+
+def predict(directory: str, iterations: Sequence[int], ask=what_if):
     """Milliseconds of each variant, simulated on the GPU; and as measured."""
     from . import batch
     tg = TR.build_graph(TR.read_rocprof_csv(directory), iterations=iterations)
-    g, vs, names = what_if(tg)
+    g, vs, names = ask(tg)
     ms = np.concatenate([m.cpu().numpy() for _, _, _, _, m in batch.simulate(batch.to_device(g, vs))])
     return [(n, t / 1e6 / len(iterations)) for n, t in zip(names, ms)], tg.measured_span / 1e6 / len(iterations)
 
@@ -223,6 +249,7 @@ def main():
     how.add_argument("--plain", action="store_true")
     how.add_argument("--fused", action="store_true")
     how.add_argument("--predict", metavar="DIR", help="the trace that rocprofv3 wrote of a --plain run")
+    ap.add_argument("--products", action="store_true", help="the products by this library too")
     ap.add_argument("--hidden", type=int, default=2048)
     ap.add_argument("--layers", type=int, default=8)
     ap.add_argument("--rows", type=int, default=16384)
@@ -231,11 +258,12 @@ def main():
     if a.predict:
         rows, measured = predict(a.predict, [6, 7])
         print("traced iteration: %.3f ms" % measured)
-        for name, ms in rows:
+        for name, ms in rows + predict(a.predict, [6, 7], what_if_products)[0]:
             print("%-28s %8.3f ms" % (name, ms))
         return
-    ms, losses = train(a.hidden, a.layers, a.rows, a.steps, a.fused, marked=True)
-    print("%s: %.3f ms an iteration, loss %.5f -> %.5f" % ("fused" if a.fused else "plain", ms, losses[0], losses[-1]))
+    ms, losses = train(a.hidden, a.layers, a.rows, a.steps, a.fused, marked=True, products=a.products)
+    print("%s%s: %.3f ms an iteration, loss %.5f -> %.5f" % ("fused" if a.fused else "plain", ", products" if a.products else "", ms,
+                                                         losses[0], losses[-1]))
 
 
 if __name__ == "__main__":
