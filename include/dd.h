@@ -527,9 +527,11 @@ size_t dd_linear_work(int64_t rows, int64_t k, int64_t n);
  *                                gradient of in_z (NULL: that of x)
  *   dw = x^T dy                  laid out as w is (turned or not)
  *   db = sum over rows of dy     in bias_type
- * dw and db of no rows are zeros.  dx may be in_z or x, element for element, if dw
- * is not wanted.  Sums over many rows are cut into parts whose sums are
- * joined in order: the same bits on every call.
+ * dw and db of no rows are zeros.  dx may be in_z or x, element for element.
+ * Sums over many rows are cut into parts whose sums are joined in order: the same
+ * bits on every call.
+ *   work holds these parts and, where rows, k or n is no multiple of 8, copies of
+ * operands with rows padded to 16 bytes (in dd_linear too).
  */
 typedef struct {
     int64_t rows, k, n;
@@ -572,7 +574,7 @@ dd_status dd_act_grad(const dd_act_grad_args *a, void *stream);
  *   d_state   device uint64 [2]: key and counter; read as the work runs, so that
  *             replays of a captured call go on where the caller has moved it to.
  *   d_used    device uint64 [2] or NULL, written: key and c, which with call = 0
- *             give the gradient this mask.  Not d_state.
+ *             give the gradient this mask.  Apart from d_state.
  * out may be x or residual, element for element.  What is dropped counts for
  * nothing, also if it is infinite or not a number.  0 <= p <= 1.
  */
@@ -611,7 +613,8 @@ dd_status dd_embed(const dd_embed_args *a, void *stream);
  * dd_embed_grad -- dtable[v] = scale * sum of dy[t] over the tokens with ids[t] =
  * v, for every row of the table (zeros where there is none), each sum taken in 32 bits
  * in the tokens' order, in parts of fixed lengths: the same bits on every call.  Tokens
- * with the id `pad`, and ids that the table does not have, count for nothing.
+ * with the id `pad`, and ids that the table does not have, count for nothing.  Fewer
+ * than 2^28 tokens (dd_embed too) and 2^29 rows.
  */
 typedef struct {
     int64_t tokens, vocab, cols;

@@ -570,7 +570,7 @@ def dd_linear_grad(dy, x=None, w=None, dx=None, dw=None, db=None, in_act="none",
     pdw, sdw, dturned = _matrix("dw", dw, wide, dt) if dw is not None else (0, 0, 0)
     pdb, bk = _bias("db", db, n, kind)
     pwork = 0 if work is None else _work(work, dd_linear_grad_work(rows, k, n))
-    act = _act(in_act) if dx is not None else 0
+    act = _act(in_act) if dx is not None and not (rows == 0 and in_z is not None) else 0      # (tensors without rows have no address)
     call, s = (_lib or lib()).dd_linear_grad, None if stream is None else _stream(stream)
     if dx is not None and dw is not None and turned != dturned:
         # (each by its own layout; dw first, as dx may be x)

@@ -211,7 +211,7 @@ dd_status dd_dropout(const dd_dropout_args *a, void *stream) {
         if (!float_type(a->type)) return fail(DD_EINVAL, "unknown type %d", a->type);
         if (!(a->p >= 0.0 && a->p <= 1.0)) return fail(DD_EINVAL, "p must lie in [0, 1]");
         if (!a->d_state || !aligned(a->d_state, 8) || !aligned(a->d_used, 8)) return fail(DD_EINVAL, "d_state is NULL, or it or d_used not aligned to 8 bytes");
-        if (a->d_used == a->d_state) return fail(DD_EINVAL, "d_used is d_state");
+        if (a->d_used && a->d_used < a->d_state + 2 && a->d_state < a->d_used + 2) return fail(DD_EINVAL, "d_used is d_state, or overlaps it");
         if (a->reserved) return fail(DD_EINVAL, "reserved must be 0");
         if (a->rows > 0) {
             CHECK(check_rows("x", a->x, a->rows, a->cols, a->x_stride, a->type, false));
@@ -236,13 +236,14 @@ dd_status dd_embed(const dd_embed_args *a, void *stream) {
 }
 
 size_t dd_embed_grad_work(int64_t tokens, int64_t vocab, int64_t cols) {
-    return sizes_known(tokens, vocab, cols) && tokens < (int64_t(1) << 28) ? dd::embed_grad_work(tokens, vocab, cols) : 0;
+    return sizes_known(tokens, vocab, cols) && tokens < (int64_t(1) << 28) && vocab < (int64_t(1) << 29) ? dd::embed_grad_work(tokens, vocab, cols) : 0;
 }
 
 dd_status dd_embed_grad(const dd_embed_grad_args *a, void *stream) {
     return guarded([&] {
         if (!a) return fail(DD_EINVAL, "args is NULL");
         CHECK(check_table(a->tokens, a->vocab, a->cols, a->type, a->ids, a->id_bytes, a->scale, a->reserved));
+        if (a->vocab >= (int64_t(1) << 29)) return fail(DD_EINVAL, "vocab must be below 2^29");
         if (a->pad < -1 || a->pad >= a->vocab) return fail(DD_EINVAL, "pad must be -1 or a row of the table");
         if (a->tokens > 0) CHECK(check_rows("dy", a->dy, a->tokens, a->cols, a->dy_stride, a->type, false));
         CHECK(check_rows("dtable", a->dtable, a->vocab, a->cols, a->dtable_stride, a->type, true));

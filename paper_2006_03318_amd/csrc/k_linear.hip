@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
 
 // --- which tiles, and how sums are cut -------------------------------------------
 int64_t tiles_of(int64_t x, int64_t n) { return (x + n - 1) / n; }
+constexpr int64_t kMostApart = int64_t(1) << 22;        // a workgroup of 512 threads each: a launch has fewer than 2^32
 
 // Tile and parts that are expected to take least, from what was measured (us): a step of 64 sums of one
 // tile per compute unit takes 1.44 with 256 x 256 (8,192^3 bf16 in 768) and 0.53 with 128 x 128 (4,096 x 4,096 ->
@@ -59,6 +60,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
         const int64_t waves = tile == 16 ? 8 : tile == 64 ? (direct ? kApart<true> : kApart<false>) : 1;
         for (int64_t s = 1; s <= tiles_of(steps, waves); s *= 2) {
             const int64_t each = tiles_of(tiles_of(steps, waves), s) * waves, rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
+            if (tile <= 64 && tm * tn * tiles_of(steps, each) >= kMostApart) break;
             double us = tile == 256 ? (each * 1.44 + 7.5) * rounds : tile == 128 ? (each * (direct ? 0.53 : 0.83) + 2.0) * rounds
                       : (each / waves * (direct ? 0.75 : 2.5) + (direct ? 2.4 : 4.0)) * rounds;
             if (s > 1) us += 4.0 + 4e-6 / 3.0 * (double)(2 * s) * (double)m * (double)n;
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(1024) k_column_join(const float *part, int n, 
 // Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  1,021 x 1,237 f16 4.4 us
 // (7.5 with parts).
 constexpr int kFewRows = 4096;
+bool few_rows(int64_t rows, int64_t cols) { return rows <= kFewRows && cols < (int64_t(1) << 27); }     // (16 threads a column)
 template <class T>
 __global__ void __launch_bounds__(1024) k_column_sum_few(const T *x, int64_t stride, int rows, int64_t cols, void *out, int32_t out_type) {
     __shared__ float lds[128][65];
@@ -244,7 +247,7 @@ __global__ void __launch_bounds__(1024) k_column_sum_few(const T *x, int64_t str
 
 // parts of the rows: enough workgroups to fill the card, of 32 rows at least
 int sum_parts(int64_t rows, int64_t cols) {
-    if (rows <= kFewRows) return 1;
+    if (few_rows(rows, cols)) return 1;
     const int64_t blocks = tiles_of(cols, kSumCols);
     int64_t n = tiles_of(4 * kUnits, blocks), most = rows / 32;
     if (n > most) n = most;
@@ -316,7 +319,7 @@ size_t column_sum_work(int64_t rows, int64_t cols) {
 
 hipError_t launch_column_sum(const void *x, int64_t stride, int64_t rows, int64_t cols, int32_t type, void *out, int32_t out_type, void *work,
                              hipStream_t s) {
-    if (rows <= kFewRows) {
+    if (few_rows(rows, cols)) {
         const unsigned grid = (unsigned)tiles_of(cols, 64);
         if (type == DD_BF16) k_column_sum_few<bf16_t><<<grid, 1024, 0, s>>>(static_cast<const bf16_t *>(x), stride, (int)rows, cols, out, out_type);
         else k_column_sum_few<f16_t><<<grid, 1024, 0, s>>>(static_cast<const f16_t *>(x), stride, (int)rows, cols, out, out_type);

@@ -80,6 +80,8 @@ def add_rms_norm(x, residual=None, weight=None, eps: float = 1e-6):
 
 
 def _matrix(w):
+    if w.dim() != 2 or 0 in w.shape:
+        raise ValueError("a weight or table must have two dimensions and not be empty, got %s" % (tuple(w.shape),))
     return w if w.stride(1) == 1 or w.stride(0) == 1 else w.contiguous()
 
 
@@ -121,7 +123,7 @@ def _linear_grad(dy, x, weight, bias, wanted, in_act="none", in_z=None):
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, act):
-        x, weight = _rows(x), _matrix(weight)
+        x = _rows(x)
         ctx.act = act
         y, z = _linear(x, weight, bias, None if residual is None else _rows(residual), act,
                        act != "none" and any(ctx.needs_input_grad[:3]))
@@ -146,6 +148,7 @@ def linear(x, weight, bias=None, act="none", residual=None):
     relu, gelu, gelu_tanh or silu."""
     for t, what in ((weight, "weight"), (residual, "residual")):
         _same(t, what, x.dtype)
+    weight = _matrix(weight)
     if residual is not None:
         residual = residual.expand(x.shape[:-1] + weight.shape[1:])
     return _Linear.apply(x, weight, bias, residual, act)
@@ -154,7 +157,7 @@ def linear(x, weight, bias=None, act="none", residual=None):
 class _Mlp(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, up, down, bias_up, bias_down, residual, act):
-        x, up, down = _rows(x), _matrix(up), _matrix(down)
+        x = _rows(x)
         ctx.act = act
         a, z = _linear(x, up, bias_up, None, act, act != "none" and any(ctx.needs_input_grad[:5]))
         y, _ = _linear(a, down, bias_down, None if residual is None else _rows(residual), "none", False)
@@ -180,6 +183,7 @@ def mlp(x, up, down, bias_up=None, bias_down=None, act="gelu", residual=None):
     multiplies with the activation's derivative in the product that comes to it."""
     for t, what in ((up, "up"), (down, "down"), (residual, "residual")):
         _same(t, what, x.dtype)
+    up, down = _matrix(up), _matrix(down)
     if residual is not None:
         residual = residual.expand(x.shape[:-1] + down.shape[1:])
     return _Mlp.apply(x, up, down, bias_up, bias_down, residual, act)
@@ -262,6 +266,9 @@ class _Embed(torch.autograd.Function):
 def embed(ids, table, scale: float = 1.0, pad: int = -1):
     """scale * table[ids], for int64 or int32 ids of any shape.  The row `pad` (-1: none) gets no
     gradient.  An id that the table does not have gives a row of NaNs, and no gradient."""
+    _matrix(table)
+    if not -1 <= pad < table.shape[0]:
+        raise ValueError("pad must be -1 or a row of the table, got %d" % pad)
     return _Embed.apply(ids, table, float(scale), int(pad))
 
 

@@ -164,3 +164,20 @@ def test_offsets_past_32_bits():
     B.dd_embed_grad(ids, out, table)
     torch.cuda.synchronize()
     assert bool((table[-1] == 6).all()) and bool((table[-2] == 5).all()) and not table[:-2].any()
+
+
+@pytest.mark.parametrize("tokens,vocab,cols", [(9, 300, 40), (3000, 40, 136), (8192, 600, 24), (20000, 300, 513), (1100000, 70000, 8)])
+def test_nothing_behind_the_working_memory(tokens, vocab, cols):
+    """Exactly the bytes that are asked for, at the end of a buffer of which the rest stays as it was."""
+    import torch
+    require_gpu()
+    gen = torch.Generator("cuda").manual_seed(3)
+    ids = torch.randint(0, vocab, (tokens,), generator=gen, device="cuda")
+    dy = torch.ones(tokens, cols, device="cuda")
+    out = torch.empty(vocab, cols, device="cuda")
+    need = B.dd_embed_grad_work(tokens, vocab, cols)
+    room = torch.full((1024 + need + 4096,), 171, device="cuda", dtype=torch.uint8)
+    B.dd_embed_grad(ids, dy, out, work=room[1024:1024 + need])
+    torch.cuda.synchronize()
+    assert bool((room[:1024] == 171).all()) and bool((room[1024 + need:] == 171).all())
+    assert torch.equal(out, torch.bincount(ids, minlength=vocab).float()[:, None].expand(vocab, cols))

@@ -137,12 +137,20 @@ def test_refusals():
         linear(x, w, residual=x.float())
     with pytest.raises(ValueError, match="act"):
         linear(x, w, act="tanh")
+    with pytest.raises(ValueError, match="empty"):
+        linear(x[:, :0], w[:0])
     with pytest.raises(ValueError, match="device"):
         linear(x, w.cpu())
     with pytest.raises(B.DDError, match="p must"):
         Dropout()(x, 1.5)
     with pytest.raises(TypeError, match="ids"):
         embed(torch.zeros(3, device="cuda"), w)
+    ids = torch.zeros(3, dtype=torch.int64, device="cuda")
+    with pytest.raises(ValueError, match="pad"):
+        embed(ids, w, pad=8)
+    for table in (w[0], w[None], w[:0]):
+        with pytest.raises(ValueError, match="two dimensions"):
+            embed(ids, table)
     y = linear(x.requires_grad_(), w)
     g, = torch.autograd.grad(y.sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
@@ -350,3 +358,18 @@ def test_two_streams_at_once():
     for x, y, i, d in zip(xs, ys, ids, ds):
         assert torch.equal(y, (x.double() @ w.double()).to(t))
         assert torch.equal(d.double(), torch.zeros(100, 72, dtype=torch.float64, device="cuda").index_add_(0, i, dy.double()))
+
+
+def test_no_rows():
+    """Batches without rows: outputs without rows, gradients that are zeros."""
+    import torch
+    from paper_2006_03318_amd.training import Dropout, embed, linear, mlp
+    require_gpu()
+    t = torch.bfloat16
+    w, v, b = (torch.ones(s, device="cuda", dtype=t, requires_grad=True) for s in ((24, 40), (40, 24), (40,)))
+    x = torch.ones(3, 0, 24, device="cuda", dtype=t, requires_grad=True)
+    ids = torch.zeros(0, 5, dtype=torch.int64, device="cuda")
+    for y, leaves_ in ((linear(x, w, b, "gelu"), (x, w, b)), (mlp(x, w, v, b), (x, w, v, b)), (embed(ids, w), (w,)), (Dropout()(x, 0.5), (x,))):
+        assert y.numel() == 0
+        for p, g in zip(leaves_, torch.autograd.grad(y.sum(), leaves_)):
+            assert g.shape == p.shape and not g.any()

@@ -80,6 +80,7 @@ SHAPES = [
     (1, 1, 1, 0), (1, 8, 8, 0), (3, 64, 128, 8), (16, 200, 136, 0), (17, 72, 40, 8), (15, 333, 7, 3), (4, 2048, 1024, 0), (2, 5000, 9, 1),
     (130, 64, 256, 0), (128, 1, 128, 0), (257, 136, 264, 8), (300, 321, 130, 5), (129, 127, 129, 0), (100, 4104, 104, 16), (33, 1031, 65, 0),
     (2048, 96, 1032, 8), (2049, 511, 999, 1), (4096, 128, 4096, 0), (1, 63, 70000, 0), (70000, 9, 3, 0),
+    (4400, 64, 8192, 0), (4400, 136, 8201, 0), (6000, 72, 1032, 1), (40, 512, 264, 1), (64, 4096, 1000, 0), (65, 4096, 1000, 3), (1300, 1024, 1300, 0),
 ]
 
 
@@ -312,3 +313,75 @@ def test_one_row_for_all():
         B.dd_linear(row.expand(300, k), w, y, residual=residual.expand(300, n))
         torch.cuda.synchronize()
         assert torch.equal(y, (row.double() @ w.double() + residual.double()).to(torch.bfloat16).expand(300, n))
+
+
+@pytest.mark.parametrize("odd", [0, 1])
+def test_offsets_past_32_bits(odd):
+    """Rows of x, and of y, that begin more than 2^32 elements apart from the first."""
+    import torch
+    require_gpu()
+    rows, k, n, stride = 66000, 64 + odd, 72, 65600 + odd
+    gen = torch.Generator("cuda").manual_seed(2)
+    wide = torch.zeros(rows * stride, device="cuda", dtype=torch.bfloat16)
+    x = wide.as_strided((rows, k), (stride, 1))
+    y = wide.as_strided((rows, n), (stride, 1), 128)
+    x.copy_(torch.randint(-2, 3, (rows, k), generator=gen, device="cuda"))
+    w = torch.randint(-2, 3, (k, n), generator=gen, device="cuda").to(torch.bfloat16)
+    B.dd_linear(x, w, y)
+    dw = torch.empty_like(w)
+    B.dd_linear_grad(y, x, w, dw=dw)
+    torch.cuda.synchronize()
+    want = x.double() @ w.double()
+    assert torch.equal(y, want.to(torch.bfloat16))
+    want = x.double().t() @ y.double()      # (sums of whole numbers, but too large to be exact in 32 bits)
+    check("dw", dw, want, (rows + 8) * 2.0 ** -23 * (x.double().abs().t() @ y.double().abs()))
+    assert not wide.as_strided((rows, 20), (stride, 1), 100).any() and not wide.as_strided((rows - 1, 1000), (stride, 1), 200).any()
+
+
+def test_calls_of_many_sizes_share_given_memory():
+    """One piece of working memory for calls of different shapes in a row on a stream."""
+    import torch
+    require_gpu()
+    gen = torch.Generator("cuda").manual_seed(6)
+    shapes = [(4, 8192, 136), (300, 321, 131), (8192, 24, 40), (70, 5000, 90), (129, 127, 129)]
+    work = torch.empty(max(max(B.dd_linear_work(*s), B.dd_linear_grad_work(*s)) for s in shapes), dtype=torch.uint8, device="cuda")
+    kept = []
+    for rows, k, n in shapes * 2:
+        x, w, dy = (torch.randint(-2, 3, s, generator=gen, device="cuda").to(torch.float16) for s in ((rows, k), (k, n), (rows, n)))
+        y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+        B.dd_linear(x, w, y, work=work)
+        B.dd_linear_grad(dy, x, w, dx=dx, dw=dw, db=db, work=work)
+        kept.append((x, w, dy, y, dx, dw, db))
+    torch.cuda.synchronize()
+    for x, w, dy, y, dx, dw, db in kept:
+        assert torch.equal(y, (x.double() @ w.double()).half()) and torch.equal(dx, (dy.double() @ w.double().t()).half())
+        assert torch.equal(dw, (x.double().t() @ dy.double()).half()) and torch.equal(db.double(), dy.double().sum(0))
+
+
+def test_sums_of_more_columns_than_a_launch_has_threads_for():
+    import torch
+    require_gpu()
+    n = (1 << 28) + 24
+    dy = torch.ones(2, n, device="cuda", dtype=torch.bfloat16)
+    dy[1, 5::7] = -3
+    db = torch.empty(n, device="cuda", dtype=torch.bfloat16)
+    B.dd_linear_grad(dy, w=torch.empty(1, n, device="cuda", dtype=torch.bfloat16), db=db)
+    torch.cuda.synchronize()
+    assert torch.equal(db, dy[0] + dy[1])
+
+
+@pytest.mark.parametrize("rows,k,n", [(4, 8192, 136), (300, 321, 131), (8192, 24, 40), (70, 5000, 90), (129, 127, 129), (1021, 777, 1237)])
+def test_nothing_behind_the_working_memory(rows, k, n):
+    """Exactly the bytes that are asked for, at the end of a buffer of which the rest stays as it was."""
+    import torch
+    require_gpu()
+    gen = torch.Generator("cuda").manual_seed(8)
+    x, w, dy = (torch.randint(-2, 3, s, generator=gen, device="cuda").to(torch.bfloat16) for s in ((rows, k), (k, n), (rows, n)))
+    y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+    for need, call in ((B.dd_linear_work(rows, k, n), lambda m: B.dd_linear(x, w, y, work=m)),
+                       (B.dd_linear_grad_work(rows, k, n), lambda m: B.dd_linear_grad(dy, x, w, dx=dx, dw=dw, db=db, work=m))):
+        room = torch.full((1024 + need + 4096,), 171, device="cuda", dtype=torch.uint8)
+        call(room[1024:1024 + need])
+        torch.cuda.synchronize()
+        assert bool((room[:1024] == 171).all()) and bool((room[1024 + need:] == 171).all())
+    assert torch.equal(y, (x.double() @ w.double()).to(torch.bfloat16)) and torch.equal(db.double(), dy.double().sum(0))

@@ -63,7 +63,7 @@ DROP = dict(rows=3, cols=8, sx=8, sr=8, so=8, x=P, r=P, out=P, state=P, used=P +
 @pytest.mark.parametrize("change,word", [
     (dict(rows=-1), "rows"), (dict(cols=0), "cols"), (dict(rows=1 << 31), "2^31"), (dict(type=3), "type"), (dict(p=-0.1), "p must"),
     (dict(p=1.1), "p must"), (dict(p=math.nan), "p must"), (dict(state=0), "d_state"), (dict(state=P + 4), "d_state"), (dict(used=P + 4), "d_used"),
-    (dict(used=P), "d_used is d_state"), (dict(res=1), "reserved"), (dict(x=0), "x is NULL"), (dict(out=P + 2), "out is not"),
+    (dict(used=P), "d_used is d_state"), (dict(used=P + 8), "overlaps"), (dict(res=1), "reserved"), (dict(x=0), "x is NULL"), (dict(out=P + 2), "out is not"),
     (dict(r=P + 1), "residual"), (dict(sx=-1), "x: stride"), (dict(so=7), "out: stride"),
 ])
 def test_dropout_refusals(lib, change, word):  # noqa: F811
@@ -87,7 +87,7 @@ EGRAD = dict(tokens=3, vocab=5, cols=8, sd=8, st=8, ids=P, dy=P, dtable=P, work=
 
 @pytest.mark.parametrize("change,word", [
     (dict(tokens=-1), "tokens"), (dict(bytes=0), "id_bytes"), (dict(ids=P + 2), "ids"), (dict(pad=-2), "pad"), (dict(pad=5), "pad"),
-    (dict(dy=0), "dy is NULL"), (dict(dtable=0), "dtable is NULL"), (dict(st=7), "dtable: stride"), (dict(work=P + 1), "work"), (dict(res=2), "reserved"),
+    (dict(vocab=1 << 29), "2^29"), (dict(dy=0), "dy is NULL"), (dict(dtable=0), "dtable is NULL"), (dict(st=7), "dtable: stride"), (dict(work=P + 1), "work"), (dict(res=2), "reserved"),
 ])
 def test_embedding_gradient_refusals(lib, change, word):  # noqa: F811
     refused(lib, "dd_embed_grad", B._EMBED_GRAD, EGRAD, change, word)
