@@ -17,7 +17,8 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int bytes, int64_t t) 
 }
 __host__ __device__ inline int have_of(int64_t n, int64_t i) { return n - i >= 8 ? 8 : n - i < 0 ? 0 : (int)(n - i); }
 
-// A thread has eight columns of a token.  Bound: HBM; few tokens, the launch.
+// A thread has eight columns of a token.  Bound: HBM; few tokens, the launch.  65,536 words of 32,000 x 1,024 bf16 in
+// 49 us (rows read again come from the caches: 5.5 TB/s), 4 in 5.
 template <class T>
 __global__ void __launch_bounds__(256) k_embed(dd_embed_args a, uint32_t packs) {
     const int64_t total = a.tokens * packs;
@@ -107,8 +108,8 @@ __device__ __forceinline__ void fill_table(const dd_embed_grad_args &a, int64_t 
     }
 }
 
-// Few tokens: one workgroup sorts them in LDS, EACH to a thread.  2,047 tokens 6 us, in which
-// the others may fill the table.
+// Few tokens: one workgroup sorts them in LDS, EACH to a thread, while the others may fill the table (50,021 x 513
+// f32 in 15 us, 6.6 TB/s: the fill's time).
 constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 template <class T, int EACH>
 __global__ void __launch_bounds__(kSmallThreads) k_embed_sort(dd_embed_grad_args a, Sorted to, int passes, int64_t rows) {
@@ -299,7 +300,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
 // LANES lanes have a chunk of CHUNK sorted places and 8 LANES columns.  A run of one id
 // that lies in the chunk is stored; the part of a run that begins before the chunk goes to
 // part 0 of the chunk, that of a run which goes on behind it to part 1 (a run that does
-// both, to part 0).
+// both, to part 0).  Bound: HBM.  65,536 words of 32,000 x 1,024 bf16 in 47 us: 200 MB at 4.3 TB/s.
 
 template <int LANES>
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int i) {
@@ -317,41 +318,140 @@ __device__ __forceinline__ void store_scaled(const dd_embed_grad_args &a, int64_
     p.store(static_cast<T *>(a.dtable) + id * a.dtable_stride + c, have);
 }
 
+// The first place from lo on, before hi, whose id is not k (k's come first): a wave looks at 64 places at once.
+__device__ __forceinline__ int64_t behind(const uint32_t *key, int64_t lo, int64_t hi, uint32_t k) {
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 63) / 64, p = lo + (threadIdx.x & 63) * step;
+        const uint64_t past = __ballot(p >= hi || key[p < hi ? p : hi - 1] != k);
+        const int n = past ? __builtin_ctzll(past) : 64;
+        if (n == 0) break;
+        if (lo + n * step < hi) hi = lo + n * step;
+        lo += (n - 1) * step + 1;
+    }
+    return lo;
+}
+
+// Zeros in the rows of the table that no token has, kRowsOfWave from `filled` on by a wave: a lane looks one up,
+// all of them write the row.
 constexpr int kRowsOfWave = 16;
-template <class T, int LANES, int CHUNK>
-__global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted in, float *part, int64_t chunks, int64_t blocks_of_runs, int64_t strips, int64_t filled) {
-    constexpr int kGroups = 256 / LANES;
-    const int lane = threadIdx.x % LANES;
+template <class T>
+__device__ __forceinline__ void fill_others(const dd_embed_grad_args &a, const Sorted &in, int64_t filled, int64_t wave) {
+    const int64_t first = filled + wave * kRowsOfWave, id = first + (threadIdx.x & 63);
+    bool there = (threadIdx.x & 63) >= kRowsOfWave || id >= a.vocab;
+    if (!there) {
+        int64_t lo = 0, hi = a.tokens;      // the first place with an id of at least this
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) >> 1;
+            if (in.key[mid] < (uint32_t)id) lo = mid + 1;
+            else hi = mid;
+        }
+        there = lo < a.tokens && in.key[lo] == (uint32_t)id;
+    }
+    uint64_t none = __ballot(!there);
+    Pack<T, 8> zero;
+    zero.v = 0;
+    while (none) {
+        const int r = __builtin_ctzll(none);
+        // rows in a row, where they lie end to end, are written as one
+        const uint64_t after = ~(none >> r);
+        const int rows = a.dtable_stride != a.cols ? 1 : after ? __builtin_ctzll(after) < 64 - r ? __builtin_ctzll(after) : 64 - r : 64 - r;
+        none &= r + rows < 64 ? ~uint64_t(0) << (r + rows) : 0;
+        T *to = static_cast<T *>(a.dtable) + (first + r) * a.dtable_stride;
+        const int64_t n = rows * a.cols;
+        for (int64_t c = 8 * (threadIdx.x & 63); c < n; c += 512) zero.store(to + c, have_of(n, c));
+    }
+}
+
+// Few tokens: a workgroup has kPlaces sorted places and 128 columns, and as many groups of 16 lanes,
+// each of which sums the run that begins at its place as far as the workgroup's places go.  The last run, where it goes
+// on behind them, is summed by all groups, eight places each in turn, joined in order: no parts, and
+// no launch to join them (2,047 tokens of 513 columns f32: 9 us, 11 with both; 2,048 times one id of 1,024
+// columns bf16, all of the gradient: 32, and 30).  Bound: latency; for one id in many places, what one compute unit loads, and so few columns.
+constexpr int kPlaces = 16, kFewLanes = 16;
+template <class T>
+__global__ void __launch_bounds__(kPlaces * kFewLanes) k_embed_few(dd_embed_grad_args a, Sorted in, int64_t blocks_of_runs, int64_t strips, int64_t filled) {
     if (blockIdx.x >= blocks_of_runs) {
-        // rows of the table that no token has: a lane looks one up, all of them write the row
-        const int64_t first = filled + ((blockIdx.x - blocks_of_runs) * 4 + threadIdx.x / 64) * kRowsOfWave;
-        const int64_t id = first + (threadIdx.x & 63);
-        bool there = (threadIdx.x & 63) >= kRowsOfWave || id >= a.vocab;
-        if (!there) {
-            int64_t lo = 0, hi = a.tokens;      // the first place with an id of at least this
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (in.key[mid] < (uint32_t)id) lo = mid + 1;
-                else hi = mid;
-            }
-            there = lo < a.tokens && in.key[lo] == (uint32_t)id;
-        }
-        uint64_t none = __ballot(!there);
-        Pack<T, 8> zero;
-        zero.v = 0;
-        while (none) {
-            const int r = __builtin_ctzll(none);
-            // rows in a row, where they lie end to end, are written as one
-            const uint64_t after = ~(none >> r);
-            const int rows = a.dtable_stride != a.cols ? 1 : after ? __builtin_ctzll(after) < 64 - r ? __builtin_ctzll(after) : 64 - r : 64 - r;
-            none &= r + rows < 64 ? ~uint64_t(0) << (r + rows) : 0;
-            T *to = static_cast<T *>(a.dtable) + (first + r) * a.dtable_stride;
-            const int64_t n = rows * a.cols;
-            for (int64_t c = 8 * (threadIdx.x & 63); c < n; c += 512) zero.store(to + c, have_of(n, c));
-        }
+        fill_others<T>(a, in, filled, (blockIdx.x - blocks_of_runs) * (kPlaces * kFewLanes / 64) + threadIdx.x / 64);
         return;
     }
-    const int64_t task = (int64_t)blockIdx.x * kGroups + threadIdx.x / LANES;
+    __shared__ float lds[kPlaces][8 * kFewLanes];
+    const int lane = threadIdx.x % kFewLanes, wave_lane = threadIdx.x & 63;
+    const int g = threadIdx.x / kFewLanes;
+    const int n_tokens = (int)a.tokens, p0 = (int)(blockIdx.x / strips) * kPlaces;
+    const int64_t strip = (blockIdx.x % strips) * (8 * kFewLanes), c = strip + 8 * lane;
+    const int have = have_of(a.cols, c), n = n_tokens - p0 < kPlaces ? n_tokens - p0 : kPlaces;
+    // ids of the places from the one before on
+    const int at = p0 - 1 + wave_lane;
+    const uint32_t none = 0xffffffffu, key = wave_lane <= n + 1 && at >= 0 && at < n_tokens ? in.key[at] : none;
+    const uint32_t place = wave_lane < n ? in.place[p0 + wave_lane] : 0;
+    const uint32_t next = __shfl_down(key, 1, 64);
+    const uint64_t starts = __ballot(key != next) & ((uint64_t(1) << n) - 1);      // bit i: place i begins a run
+    const bool goes_on = ((__ballot(key == next) >> n) & 1) && p0 + n < n_tokens;
+    const T *dy = static_cast<const T *>(a.dy) + c;
+    const uint32_t mine = __shfl(key, g + 1, 64);
+    const int last = starts ? 63 - __builtin_clzll(starts) : -1;       // where the workgroup's last run begins
+    const uint64_t later = starts >> g >> 1;
+    const int len = !(starts >> g & 1) || mine >= (uint32_t)a.vocab || (g == last && goes_on) ? 0 : later ? __builtin_ctzll(later) + 1 : n - g;
+    if (__any(len > 0)) {
+        float s[8] = {};
+#pragma unroll
+        for (int b = 0; b < kPlaces; b += 8) {
+            if (!__any(b < len)) break;
+            Pack<T, 8> p[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) p[i].load(dy + (int64_t)__shfl(place, b + i < len ? g + b + i : g, 64) * a.dy_stride, len > 0 ? have : 0);
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                float x[8];
+                p[i].to(x);
+#pragma unroll
+                for (int j = 0; j < 8; j++) s[j] += b + i < len ? x[j] : 0.0f;
+            }
+        }
+        if (len > 0 && have > 0) store_scaled<T>(a, mine, c, have, s);
+    }
+    const uint32_t k = __shfl(key, last + 1, 64);
+    if (last < 0 || !goes_on || k >= (uint32_t)a.vocab) return;
+    const int end = (int)behind(in.key, p0 + n, n_tokens, k);
+    float s[8] = {};
+    // (the places are loaded a turn ahead, by as many lanes)
+    auto ahead = [&](int q) { return in.place[q + (lane & 7) < end ? q + (lane & 7) : end - 1]; };
+    uint32_t to_come = ahead(p0 + last + 8 * g);
+    for (int q0 = p0 + last; q0 < end; q0 += 8 * kPlaces) {
+        const int q = q0 + 8 * g;
+        const uint32_t places = to_come;
+        to_come = ahead(q + 8 * kPlaces);
+        Pack<T, 8> p[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) p[i].load(dy + (int64_t)of_lane<kFewLanes>(places, i) * a.dy_stride, have);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            float x[8];
+            p[i].to(x);
+#pragma unroll
+            for (int j = 0; j < 8; j++) s[j] += q + i < end ? x[j] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds[g][8 * lane + j] = s[j];
+    __syncthreads();
+    const int col = threadIdx.x;
+    if (col >= 8 * kFewLanes || strip + col >= a.cols) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPlaces; i++) sum += lds[i][col];
+    static_cast<T *>(a.dtable)[k * a.dtable_stride + strip + col] = (T)(sum * a.scale);
+}
+
+template <class T, int LANES, int CHUNK>
+__global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted in, float *part, int64_t chunks, uint32_t blocks_of_rows, int64_t strips, int64_t filled) {
+    constexpr int kGroups = 256 / LANES;
+    const int lane = threadIdx.x % LANES;
+    if (blockIdx.x < blocks_of_rows) {      // (first: their lookups take time, but little else)
+        fill_others<T>(a, in, filled, (int64_t)blockIdx.x * 4 + threadIdx.x / 64);
+        return;
+    }
+    const int64_t task = (int64_t)(blockIdx.x - blocks_of_rows) * kGroups + threadIdx.x / LANES;
     const int64_t chunk = LANES == 64 ? __builtin_amdgcn_readfirstlane((int)(task / strips)) : task / strips;
     if (chunk >= chunks) return;
     const int64_t c = (task - chunk * strips) * (8 * LANES) + 8 * lane;
@@ -409,68 +509,85 @@ __global__ void __launch_bounds__(256) k_embed_runs(dd_embed_grad_args a, Sorted
     }
 }
 
-// Runs over several chunks.  A workgroup has the chunk a run begins in and 256 columns: its four groups of
-// 32 lanes sum every fourth of the run's parts, and the groups are joined in order.
-constexpr int kJoinGroups = 4;
+// Runs over several chunks.  A wave looks at the chunk that a run may begin in, for 256 columns.  It sums the
+// parts of a short run by itself; those of a longer one are summed by the workgroup's waves, each in turn eight of
+// them, and joined in order.
+constexpr int kJoinWaves = 8, kJoinAtOnce = 8, kJoinAlone = 2 * kJoinAtOnce;
 template <class T, int CHUNK>
-__global__ void __launch_bounds__(32 * kJoinGroups) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part) {
-    __shared__ float lds[kJoinGroups][256];
-    __shared__ int64_t last_chunk;
-    const int64_t chunk = blockIdx.x, end = (chunk + 1) * CHUNK;
-    if (end >= a.tokens) return;
-    const uint32_t k = in.key[end - 1];
-    if (k >= (uint32_t)a.vocab || in.key[end] != k) return;
-    // (begun in this chunk: its first place has another id, or follows one)
-    if (in.key[end - CHUNK] == k && chunk > 0 && in.key[end - CHUNK - 1] == k) return;
-    if (threadIdx.x == 0) {
-        int64_t lo = end, hi = a.tokens;        // the first place behind the run
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (in.key[mid] == k) lo = mid + 1;
-            else hi = mid;
-        }
-        last_chunk = (lo - 1) / CHUNK;
+__global__ void __launch_bounds__(64 * kJoinWaves) k_embed_join(dd_embed_grad_args a, Sorted in, const float *part) {
+    __shared__ float lds[kJoinWaves][256];
+    __shared__ int lasts[kJoinWaves];
+    __shared__ uint32_t ids[kJoinWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = blockIdx.x * kJoinWaves, mine = first + wave;
+    const int64_t end = (int64_t)(mine + 1) * CHUNK;
+    // (0: no run over several chunks begins in the wave's)
+    int last = 0;
+    uint32_t id = 0;
+    if (end < a.tokens) {
+        id = in.key[end - 1];
+        const uint32_t next = in.key[end], begin = in.key[end - CHUNK], before = in.key[mine > 0 ? end - CHUNK - 1 : 0];
+        if (id < (uint32_t)a.vocab && next == id && !(begin == id && mine > 0 && before == id)) last = __builtin_amdgcn_readfirstlane((int)((behind(in.key, end, a.tokens, id) - 1) / CHUNK));
+    }
+    if (lane == 0) {
+        lasts[wave] = last;
+        ids[wave] = id;
     }
     __syncthreads();
-    const int64_t last = last_chunk;
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.cols; c0 += (int64_t)gridDim.y * 256) {
-        const int64_t c = c0 + 8 * x;
-        const int have = have_of(a.cols, c);
-        float s[8] = {};
-        for (int64_t i = chunk + y; i <= last; i += 4 * kJoinGroups) {
-            Pack<float, 8> f[4];
+    auto sum = [&](int chunk, int to, int i, int by, int64_t c, int have, float (&s)[4]) __attribute__((always_inline)) {
+        for (; i <= to; i += by * kJoinAtOnce) {
+            Pack<float, 4> f[kJoinAtOnce];
 #pragma unroll
-            for (int u = 0; u < 4; u++) f[u].load(part + (2 * (i + kJoinGroups * u) + (i + kJoinGroups * u == chunk ? 1 : 0)) * a.cols + c, i + kJoinGroups * u <= last ? have : 0);
+            for (int u = 0; u < kJoinAtOnce; u++) {
+                f[u].v = 0.0f;
+                if (i + by * u <= to) f[u].load(part + (2 * (int64_t)(i + by * u) + (i + by * u == chunk ? 1 : 0)) * a.cols + c, have);
+            }
 #pragma unroll
-            for (int u = 0; u < 4; u++) {
-                float v[8];
+            for (int u = 0; u < kJoinAtOnce; u++) {
+                float v[4];
                 f[u].to(v);
 #pragma unroll
-                for (int j = 0; j < 8; j++) s[j] += v[j];
+                for (int j = 0; j < 4; j++) s[j] += v[j];
             }
         }
-        __syncthreads();
+    };
+    for (int64_t c0 = (int64_t)blockIdx.y * 256; c0 < a.cols; c0 += (int64_t)gridDim.y * 256) {
+        const int64_t c = c0 + 4 * lane;
+        const int have = a.cols - c >= 4 ? 4 : a.cols - c < 0 ? 0 : (int)(a.cols - c);
+        if (last && last - mine < kJoinAlone) {
+            float s[4] = {};
+            sum(mine, last, mine, 1, c, have, s);
+            Pack<T, 4> p;
 #pragma unroll
-        for (int j = 0; j < 8; j++) lds[y][8 * x + j] = s[j];
-        __syncthreads();
-        if (y == 0) {
+            for (int j = 0; j < 4; j++) s[j] *= a.scale;
+            p.from(s);
+            p.store(static_cast<T *>(a.dtable) + id * a.dtable_stride + c, have);
+        }
+        for (int w = 0; w < kJoinWaves; w++) {
+            const int chunk = first + w, to = __builtin_amdgcn_readfirstlane(lasts[w]);
+            if (!to || to - chunk < kJoinAlone) continue;
+            float s[4] = {};
+            sum(chunk, to, chunk + wave, kJoinWaves, c, have, s);
+            __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; j++) s[j] = 0.0f;
+            for (int j = 0; j < 4; j++) lds[wave][4 * lane + j] = s[j];
+            __syncthreads();
+            if (threadIdx.x < 256 && c0 + threadIdx.x < a.cols) {
+                float t = 0.0f;
 #pragma unroll
-            for (int g = 0; g < kJoinGroups; g++)
-#pragma unroll
-                for (int j = 0; j < 8; j++) s[j] += lds[g][8 * x + j];
-            if (have > 0) store_scaled<T>(a, k, c, have, s);
+                for (int g = 0; g < kJoinWaves; g++) t += lds[g][threadIdx.x];
+                static_cast<T *>(a.dtable)[ids[w] * a.dtable_stride + c0 + threadIdx.x] = (T)(t * a.scale);
+            }
         }
     }
 }
 
 // Working memory of the gradient: two lists of sorted tokens, counts, parts.
-// A chunk of few tokens is short: there is little to go round, and what counts is how long one takes
-// (2,047 tokens: 8 us a chunk of 32, 5 of 8).
+// Few tokens are summed without parts unless a group's one load at a time counts (8,192 tokens of 32,000 x 1,024 bf16:
+// 45 us, 41 with parts), and in short chunks, as there is little to go round.
 constexpr int64_t kSmallTokens = kSmallThreads * 8;
 int chunk_of(int64_t tokens) { return tokens <= kSmallTokens ? 8 : 32; }
+bool without_parts(int64_t tokens, int64_t cols) { return tokens <= kSmallTokens && tokens * cols <= (1 << 22); }
 struct Room {
     int64_t blocks, chunks, counts, part, bytes;     // places in bytes
     int passes;
@@ -478,7 +595,7 @@ struct Room {
 Room room_of(int64_t tokens, int64_t vocab, int64_t cols) {
     Room r;
     r.blocks = (tokens + kSortBlock - 1) / kSortBlock;
-    r.chunks = (tokens + chunk_of(tokens) - 1) / chunk_of(tokens);
+    r.chunks = without_parts(tokens, cols) ? 0 : (tokens + chunk_of(tokens) - 1) / chunk_of(tokens);
     r.passes = 1;
     while (r.passes < 4 && (uint64_t)vocab >> (8 * r.passes)) r.passes++;
     r.counts = (tokens * 16 + 15) / 16 * 16;
@@ -488,15 +605,22 @@ Room room_of(int64_t tokens, int64_t vocab, int64_t cols) {
 }
 
 // filled: rows that are zeros; of the others, those that no token has are looked up and written too
+int64_t waves_of_rows(const dd_embed_grad_args &a, int64_t filled) { return (a.vocab - filled + kRowsOfWave - 1) / kRowsOfWave; }
+
+template <class T>
+void few_runs(const dd_embed_grad_args &a, const Sorted &in, int64_t filled, hipStream_t s) {
+    const int64_t strips = (a.cols + 8 * kFewLanes - 1) / (8 * kFewLanes), waves = kPlaces * kFewLanes / 64;
+    const int64_t of_runs = (a.tokens + kPlaces - 1) / kPlaces * strips, of_rows = (waves_of_rows(a, filled) + waves - 1) / waves;
+    k_embed_few<T><<<(unsigned)(of_runs + of_rows), kPlaces * kFewLanes, 0, s>>>(a, in, of_runs, strips, filled);
+}
+
 template <class T, int LANES, int CHUNK>
 void runs(const dd_embed_grad_args &a, const Sorted &in, float *part, const Room &r, int64_t filled, hipStream_t s) {
     const int64_t strips = (a.cols + 8 * LANES - 1) / (8 * LANES), groups = 256 / LANES;
-    const int64_t of_runs = (r.chunks * strips + groups - 1) / groups, of_rows = (a.vocab - filled + 4 * kRowsOfWave - 1) / (4 * kRowsOfWave);
-    k_embed_runs<T, LANES, CHUNK><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, of_runs, strips, filled);
-    if (r.chunks > 1) {
-        const int64_t y = (a.cols + 255) / 256;
-        k_embed_join<T, CHUNK><<<dim3((unsigned)r.chunks, (unsigned)(y < 1024 ? y : 1024)), 32 * kJoinGroups, 0, s>>>(a, in, part);
-    }
+    const int64_t of_runs = (r.chunks * strips + groups - 1) / groups, of_rows = (waves_of_rows(a, filled) + 3) / 4;
+    k_embed_runs<T, LANES, CHUNK><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, (uint32_t)of_rows, strips, filled);
+    const int64_t y = (a.cols + 255) / 256;
+    k_embed_join<T, CHUNK><<<dim3((unsigned)((r.chunks + kJoinWaves - 1) / kJoinWaves), (unsigned)(y < 1024 ? y : 1024)), 64 * kJoinWaves, 0, s>>>(a, in, part);
 }
 
 template <class T>
@@ -530,9 +654,9 @@ void embed_grad(const dd_embed_grad_args &a, void *work, hipStream_t s) {
             to = x;
         }
     }
-    const bool small = a.tokens <= kSmallTokens;
-    if (a.cols <= 128) small ? runs<T, 16, 8>(a, from, part, r, filled, s) : runs<T, 16, 32>(a, from, part, r, filled, s);
-    else small ? runs<T, 64, 8>(a, from, part, r, filled, s) : runs<T, 64, 32>(a, from, part, r, filled, s);
+    if (without_parts(a.tokens, a.cols)) few_runs<T>(a, from, filled, s);
+    else if (a.tokens <= kSmallTokens) a.cols <= 128 ? runs<T, 16, 8>(a, from, part, r, filled, s) : runs<T, 64, 8>(a, from, part, r, filled, s);
+    else a.cols <= 128 ? runs<T, 16, 32>(a, from, part, r, filled, s) : runs<T, 64, 32>(a, from, part, r, filled, s);
 }
 
 }  // namespace

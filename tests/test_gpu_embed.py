@@ -69,7 +69,8 @@ def _ids(gen, how, tokens, vocab):
 @pytest.mark.parametrize("how", ["even", "few", "one", "last"])
 @pytest.mark.parametrize("tokens,vocab,cols,pad", [
     (1, 1, 1, 0), (1, 70000, 16, 0), (31, 7, 8, 0), (32, 300, 100, 3), (33, 2, 129, 0), (64, 64, 640, 8), (65, 1000, 128, 0),
-    (2047, 256, 24, 0), (2049, 257, 513, 0), (5000, 40, 72, 5), (9000, 66000, 40, 0), (30000, 300, 520, 0), (4097, 1 << 24, 1, 0), (8192, 3000, 24, 0), (8193, 3000, 24, 0), (1100000, 5000, 8, 0), (1048577, 70001, 2, 0)])
+    (2047, 256, 24, 0), (2049, 257, 513, 0), (5000, 40, 72, 5), (9000, 66000, 40, 0), (30000, 300, 520, 0), (4097, 1 << 24, 1, 0), (8192, 3000, 24, 0), (8193, 3000, 24, 0), (1100000, 5000, 8, 0), (1048577, 70001, 2, 0),
+    (15, 4, 130, 0), (16, 9, 128, 0), (17, 9, 257, 3), (129, 3, 140, 0), (8192, 600, 512, 0), (8192, 600, 513, 0), (4100, 30, 1100, 1), (300, 5, 8200, 0)])
 def test_gradient(tokens, vocab, cols, pad, how, kind):
     """Whole numbers: sums without rounding, so every row is the rounded truth bit for bit."""
     import torch
