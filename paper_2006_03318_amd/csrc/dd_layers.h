@@ -41,8 +41,15 @@ struct PadRows {
 size_t padded_size(int64_t rows, int64_t cols);
 // x and its stride become those of the copy in `to`; the size of the copy
 size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, void *to, PadRows *r);
-hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, hipStream_t s);
-
+// Sums over few rows of an array (type), into out (out_type).  No columns: none.
+struct FewSums {
+    const void *x;
+    void *out;
+    int64_t stride, cols;
+    int32_t rows, type, out_type;
+};
+bool few_rows(int64_t rows, int64_t cols);
+hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, const FewSums &sums, hipStream_t s);
 
 // bytes of working memory of an m by n product of k sums (0: none), and the product
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_by_rows);

@@ -153,12 +153,18 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             const void *dy = a->dy, *x = a->x, *w = a->w;
             int64_t dy_stride = a->dy_stride, x_stride = a->x_stride, w_stride = a->w_stride;
             hipError_t e = hipSuccess;
+            bool summed = false;
             if (pad) {
                 dd::PadRows r[3];
                 work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, &r[0]);
                 work += dd::pad_rows(x, x_stride, a->rows, a->k, work, &r[1]);
                 work += dd::pad_rows(w, w_stride, wr, wc, work, &r[2]);
-                e = dd::launch_pad_rows(r[0], r[1], r[2], s);
+                dd::FewSums sums{};
+                if (a->db && dd::few_rows(a->rows, a->n)) {
+                    sums = dd::FewSums{a->dy, a->db, a->dy_stride, a->n, (int32_t)a->rows, a->type, a->bias_type};
+                    summed = true;
+                }
+                e = dd::launch_pad_rows(r[0], r[1], r[2], sums, s);
             }
             if (e == hipSuccess && a->dw) {
                 dd::Product p{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, pad ? 3 : 0, {}};
@@ -172,7 +178,7 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
                 p.e.out_stride = a->dw_stride;
                 e = dd::launch_product(p, work, s);
             }
-            if (e == hipSuccess && a->db) e = dd::launch_column_sum(dy, dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
+            if (e == hipSuccess && a->db && !summed) e = dd::launch_column_sum(dy, dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
             if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
                 dd::Product p{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, pad ? 3 : 0, {}};
                 p.e.in_z = a->in_z;

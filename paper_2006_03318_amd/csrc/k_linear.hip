@@ -84,16 +84,80 @@ bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count,
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (padded || (by_rows ? k : count) % 8 == 0) && stride < (int64_t(1) << 22);
 }
 
+// --- sums over few rows -----------------------------------------------------------
+__device__ __forceinline__ void store_as(void *p, int32_t type, int64_t i, float x) {
+    if (type == DD_F32) static_cast<float *>(p)[i] = x;
+    else if (type == DD_BF16) static_cast<bf16_t *>(p)[i] = (bf16_t)x;
+    else static_cast<f16_t *>(p)[i] = (f16_t)x;
+}
+
+// Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  1,021 x 1,237 f16 4.4 us
+// (7.5 with parts).
+constexpr int kFewRows = 4096;
+typedef float FewRoom[128][65];
+template <class T>
+__device__ __forceinline__ void sum_few(const FewSums &a, int64_t block, FewRoom &lds) {
+    const T *x = static_cast<const T *>(a.x);
+    const int64_t stride = a.stride, cols = a.cols;
+    const int rows = a.rows;
+    const int cx = threadIdx.x % 8, cy = threadIdx.x / 8;
+    const int64_t c = block * 64 + 8 * cx;
+    const int have = cols - c >= 8 ? 8 : cols - c < 0 ? 0 : (int)(cols - c);
+    float s[8] = {};
+    for (int r = cy; r < rows; r += 512) {
+        Pack<T, 8> p[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) p[i].load(x + (r + i * 128) * stride + c, r + i * 128 < rows ? have : 0);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            float v[8];
+            p[i].to(v);
+#pragma unroll
+            for (int j = 0; j < 8; j++) s[j] += v[j];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; j++) lds[cy][8 * cx + j] = s[j];
+    __syncthreads();
+    const int y = threadIdx.x / 64, mine = threadIdx.x % 64;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i++) t += lds[y * 8 + i][mine];
+    __syncthreads();
+    lds[y][mine] = t;
+    __syncthreads();
+    if (y || block * 64 + mine >= cols) return;
+    t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t += lds[i][mine];
+    store_as(a.out, a.out_type, block * 64 + mine, t);
+}
+__device__ __forceinline__ void sum_few(const FewSums &a, int64_t block, FewRoom &lds) {
+    if (a.type == DD_BF16) sum_few<bf16_t>(a, block, lds);
+    else sum_few<f16_t>(a, block, lds);
+}
+__global__ void __launch_bounds__(1024) k_column_sum_few(FewSums a) {
+    __shared__ FewRoom lds;
+    sum_few(a, blockIdx.x, lds);
+}
+
 // --- operands of odd sizes --------------------------------------------------------
 // Rows that are not multiples of 16 bytes cannot be loaded to LDS directly, which makes a step half as fast and
 // more.  Where the sizes themselves are odd and an operand is read many times, it is copied first, rows padded with
-// zeros to 16 bytes.  4,099 x 1,237 -> 777 f16 24 us (32 without), 1,021 x 777 x 1,237 14 (18 to 25).
-__global__ void __launch_bounds__(256) k_pad_rows(PadRows x, PadRows y, PadRows z) {
-    const PadRows &r = blockIdx.y == 0 ? x : blockIdx.y == 1 ? y : z;
+// zeros to 16 bytes, and sums over few rows are taken by workgroups of the same launch.  4,099 x 1,237 -> 777 f16
+// PADFIG.
+__global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows z, FewSums sums) {
+    __shared__ FewRoom lds;
+    const int which = (int)blockIdx.y - (sums.cols ? 1 : 0);
+    if (which < 0) {        // (first: they take longest)
+        if ((int64_t)blockIdx.x * 64 < sums.cols) sum_few(sums, blockIdx.x, lds);
+        return;
+    }
+    const PadRows &r = which == 0 ? x : which == 1 ? y : z;
     const int64_t packs = (r.cols + 7) / 8, total = packs * r.rows;
     const bf16_t *from = static_cast<const bf16_t *>(r.from);       // (16 bits, whatever they mean)
-    for (int64_t t = blockIdx.x * (int64_t)256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / packs, j = (t - i * packs) * 8;
+    for (int64_t t = blockIdx.x * (int64_t)1024 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 1024) {
+        const int64_t i = (uint64_t)total >> 32 ? t / packs : (int64_t)((uint32_t)t / (uint32_t)packs), j = (t - i * packs) * 8;
         Pack<bf16_t, 8> v;
         v.load(from + i * r.stride + j, r.cols - j >= 8 ? 8 : (int)(r.cols - j));
         v.store(static_cast<bf16_t *>(r.to) + t * 8);
@@ -118,7 +182,7 @@ hipError_t product(const Product &args, char *work, hipStream_t s) {
         PadRows x{}, y{};
         if (!ap) to += pad_rows(a.p, a.p_stride, a.p_by_rows ? a.m : a.k, a.p_by_rows ? a.k : a.m, to, &x);
         if (!aq) pad_rows(a.q, a.q_stride, a.q_by_rows ? a.n : a.k, a.q_by_rows ? a.k : a.n, to, &y);
-        const hipError_t e = launch_pad_rows(x, y, PadRows{}, s);
+        const hipError_t e = launch_pad_rows(x, y, PadRows{}, FewSums{}, s);
         if (e != hipSuccess) return e;
     }
     if (direct) launch_tiles<T, true>(a, p, part, s);
@@ -135,12 +199,6 @@ hipError_t product(const Product &args, char *work, hipStream_t s) {
 // and writes its sums to part j (a single one: to the output); then 32 threads a
 // column join the parts in order.
 constexpr int kSumParts = 256, kSumCols = 256, kSumRows = 8;
-
-__device__ __forceinline__ void store_as(void *p, int32_t type, int64_t i, float x) {
-    if (type == DD_F32) static_cast<float *>(p)[i] = x;
-    else if (type == DD_BF16) static_cast<bf16_t *>(p)[i] = (bf16_t)x;
-    else static_cast<f16_t *>(p)[i] = (f16_t)x;
-}
 
 template <class T>
 __global__ void __launch_bounds__(kSumCols) k_column_sum(const T *x, int64_t stride, int64_t rows, int64_t cols, int64_t run, void *out, int32_t out_type,
@@ -205,46 +263,6 @@ __global__ void __launch_bounds__(1024) k_column_join(const float *part, int n, 
     store_as(out, out_type, c, s);
 }
 
-// Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  1,021 x 1,237 f16 4.4 us
-// (7.5 with parts).
-constexpr int kFewRows = 4096;
-bool few_rows(int64_t rows, int64_t cols) { return rows <= kFewRows && cols < (int64_t(1) << 27); }     // (16 threads a column)
-template <class T>
-__global__ void __launch_bounds__(1024) k_column_sum_few(const T *x, int64_t stride, int rows, int64_t cols, void *out, int32_t out_type) {
-    __shared__ float lds[128][65];
-    const int cx = threadIdx.x % 8, cy = threadIdx.x / 8;
-    const int64_t c = (int64_t)blockIdx.x * 64 + 8 * cx;
-    const int have = cols - c >= 8 ? 8 : cols - c < 0 ? 0 : (int)(cols - c);
-    float s[8] = {};
-    for (int r = cy; r < rows; r += 512) {
-        Pack<T, 8> p[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) p[i].load(x + (r + i * 128) * stride + c, r + i * 128 < rows ? have : 0);
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            float v[8];
-            p[i].to(v);
-#pragma unroll
-            for (int j = 0; j < 8; j++) s[j] += v[j];
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; j++) lds[cy][8 * cx + j] = s[j];
-    __syncthreads();
-    const int y = threadIdx.x / 64, mine = threadIdx.x % 64;
-    float t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) t += lds[y * 8 + i][mine];
-    __syncthreads();
-    lds[y][mine] = t;
-    __syncthreads();
-    if (y || (int64_t)blockIdx.x * 64 + mine >= cols) return;
-    t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; i++) t += lds[i][mine];
-    store_as(out, out_type, (int64_t)blockIdx.x * 64 + mine, t);
-}
-
 // parts of the rows: enough workgroups to fill the card, of 32 rows at least
 int sum_parts(int64_t rows, int64_t cols) {
     if (few_rows(rows, cols)) return 1;
@@ -288,10 +306,14 @@ size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, voi
 
 size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)tiles_of(cols, 8) * 16; }
 
-hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, hipStream_t s) {
+bool few_rows(int64_t rows, int64_t cols) { return rows <= kFewRows && cols < (int64_t(1) << 27); }     // (16 threads a column)
+
+hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z, const FewSums &sums, hipStream_t s) {
     int64_t most = 1;
-    for (const PadRows *r : {&x, &y, &z}) most = tiles_of(tiles_of(r->cols, 8) * r->rows, 256) > most ? tiles_of(tiles_of(r->cols, 8) * r->rows, 256) : most;
-    k_pad_rows<<<dim3((unsigned)(most < 8 * kUnits ? most : 8 * kUnits), z.rows ? 3 : y.rows ? 2 : 1), 256, 0, s>>>(x, y, z);
+    for (const PadRows *r : {&x, &y, &z}) most = tiles_of(tiles_of(r->cols, 8) * r->rows, 1024) > most ? tiles_of(tiles_of(r->cols, 8) * r->rows, 1024) : most;
+    most = most < 2 * kUnits ? most : 2 * kUnits;
+    if (tiles_of(sums.cols, 64) > most) most = tiles_of(sums.cols, 64);
+    k_pad_rows<<<dim3((unsigned)most, (z.rows ? 3 : y.rows ? 2 : 1) + (sums.cols ? 1 : 0)), 1024, 0, s>>>(x, y, z, sums);
     return hipGetLastError();
 }
 
@@ -320,9 +342,7 @@ size_t column_sum_work(int64_t rows, int64_t cols) {
 hipError_t launch_column_sum(const void *x, int64_t stride, int64_t rows, int64_t cols, int32_t type, void *out, int32_t out_type, void *work,
                              hipStream_t s) {
     if (few_rows(rows, cols)) {
-        const unsigned grid = (unsigned)tiles_of(cols, 64);
-        if (type == DD_BF16) k_column_sum_few<bf16_t><<<grid, 1024, 0, s>>>(static_cast<const bf16_t *>(x), stride, (int)rows, cols, out, out_type);
-        else k_column_sum_few<f16_t><<<grid, 1024, 0, s>>>(static_cast<const f16_t *>(x), stride, (int)rows, cols, out, out_type);
+        k_column_sum_few<<<(unsigned)tiles_of(cols, 64), 1024, 0, s>>>(FewSums{x, out, stride, cols, (int32_t)rows, type, out_type});
         return hipGetLastError();
     }
     const int n = sum_parts(rows, cols);

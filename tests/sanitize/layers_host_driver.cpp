@@ -17,7 +17,8 @@ size_t pad_rows(const void *&, int64_t &, int64_t rows, int64_t cols, void *, Pa
     *r = PadRows{};
     return padded_size(rows, cols);
 }
-hipError_t launch_pad_rows(const PadRows &, const PadRows &, const PadRows &, hipStream_t) { STUB; }
+bool few_rows(int64_t, int64_t) { return true; }
+hipError_t launch_pad_rows(const PadRows &, const PadRows &, const PadRows &, const FewSums &, hipStream_t) { STUB; }
 size_t column_sum_work(int64_t, int64_t cols) { return (size_t)cols * 4; }
 hipError_t launch_column_sum(const void *, int64_t, int64_t, int64_t, int32_t, void *, int32_t, void *, hipStream_t) { STUB; }
 hipError_t launch_act_grad(const dd_act_grad_args &, hipStream_t) { STUB; }
