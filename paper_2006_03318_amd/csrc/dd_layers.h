@@ -39,6 +39,9 @@ struct PadRows {
     int64_t stride, rows, cols;
 };
 size_t padded_size(int64_t rows, int64_t cols);
+// an operand, `count` rows (or columns) of k sums, needs no copy
+bool loads_directly(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k);
+bool weight_pads(int64_t rows, int64_t k, int64_t n);       // the gradient of the rows gains from a padded weight
 // x and its stride become those of the copy in `to`; the size of the copy
 size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, void *to, PadRows *r);
 // Sums over few rows of an array (type), into out (out_type).  No columns: none.

@@ -103,8 +103,8 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
     });
 }
 
-// Whether the gradients of the weight and of the rows are taken from copies padded once for both (dy's rows
-// cannot be loaded as they are, and each is read many times).
+// Whether the gradients of the weight and of the rows are taken from dy padded once for both (its rows
+// cannot be loaded as they are, and each is read many times), and from padded rows; from a padded weight, if that pays.
 static bool pads_once(int64_t rows, int64_t k, int64_t n) { return n % 8 && rows > 64 && k > 64 && n > 64; }
 static size_t pads_once_size(int64_t rows, int64_t k, int64_t n) {
     const size_t w = dd::padded_size(k, n), turned = dd::padded_size(n, k);
@@ -154,11 +154,15 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             int64_t dy_stride = a->dy_stride, x_stride = a->x_stride, w_stride = a->w_stride;
             hipError_t e = hipSuccess;
             bool summed = false;
+            int padded = 0;         // of dy and w
             if (pad) {
-                dd::PadRows r[3];
+                dd::PadRows r[3] = {};
+                const bool of_x = !dd::loads_directly(x, x_stride, false, a->k, a->rows);
+                const bool of_w = !dd::loads_directly(w, w_stride, !a->turned, a->k, a->n) && dd::weight_pads(a->rows, a->k, a->n);
                 work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, &r[0]);
-                work += dd::pad_rows(x, x_stride, a->rows, a->k, work, &r[1]);
-                work += dd::pad_rows(w, w_stride, wr, wc, work, &r[2]);
+                if (of_x) work += dd::pad_rows(x, x_stride, a->rows, a->k, work, &r[1]);
+                if (of_w) work += dd::pad_rows(w, w_stride, wr, wc, work, &r[of_x ? 2 : 1]);
+                padded = of_w ? 3 : 1;
                 dd::FewSums sums{};
                 if (a->db && dd::few_rows(a->rows, a->n)) {
                     sums = dd::FewSums{a->dy, a->db, a->dy_stride, a->n, (int32_t)a->rows, a->type, a->bias_type};
@@ -180,7 +184,7 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             }
             if (e == hipSuccess && a->db && !summed) e = dd::launch_column_sum(dy, dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
             if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
-                dd::Product p{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, pad ? 3 : 0, {}};
+                dd::Product p{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, padded, {}};
                 p.e.in_z = a->in_z;
                 p.e.side_stride = a->in_z_stride;
                 p.e.in_act = a->in_act;

@@ -25,12 +25,12 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
         Pack<T, 8> side;
         load_bias<T>(a.e, j, have, bias);
         load_side<T>(a.e, i, j, have, side);
-        for (int s = 0; s < splits; s += 4) {       // (four loads at a time)
-            Pack<float, 8> b[4];
+        for (int s = 0; s < splits; s += 8) {       // (eight loads at a time)
+            Pack<float, 8> b[8];
 #pragma unroll
-            for (int u = 0; u < 4; u++) b[u].load(p + (s + u) * a.m * a.n, s + u < splits ? have : 0);
+            for (int u = 0; u < 8; u++) b[u].load(p + (s + u) * a.m * a.n, s + u < splits ? have : 0);
 #pragma unroll
-            for (int u = 0; u < 4; u++) {
+            for (int u = 0; u < 8; u++) {
                 float x[8];
                 b[u].to(x);
 #pragma unroll
@@ -45,32 +45,32 @@ __global__ void __launch_bounds__(256) k_product_join(Product a, const float *pa
 int64_t tiles_of(int64_t x, int64_t n) { return (x + n - 1) / n; }
 constexpr int64_t kMostApart = int64_t(1) << 22;        // a workgroup of 512 threads each: a launch has fewer than 2^32
 
-// Tile and parts that are expected to take least, from what was measured (us): a step of 64 sums of one
-// tile per compute unit takes 1.44 with 256 x 256 (8,192^3 bf16 in 768) and 0.53 with 128 x 128 (4,096 x 4,096 ->
-// 1,024 in 37), 0.83 with operands of any alignment; an epilogue 7.5 and 2 (its stores).  Where waves share
-// the sums of 64 x 64, a wave's step takes 0.75 of four waves and the end 2.4 (1,024 x 1,024 -> 768 in 8, of
-// any alignment 2.5 of eight waves, and 4).  Joining parts takes another launch and its traffic.
+// Tile and parts that are expected to take least (us).  A step of 64 sums of a tile takes 1.44 with 256 x 256
+// and 0.53 with 128 x 128 where all compute units have one, and down to 1.0 and 0.4 where few do (1.05 with operands of
+// any alignment); what comes after, the epilogue, 11 and 3.4.  Measured, from x k to 8,192 x 8,192 bf16, in us a round of 256
+// tiles: 256 x 256 k 64 12.5, 512 23.2, 1,024 34.0; 128 x 128 4.6, 7.6, 11.2.  Where waves share
+// the sums of 64 x 64, a wave's step takes 0.75 of four waves and the end 3 (k 64 3.8, 1,024 6.1; of
+// any alignment 2.5 of eight waves, and 5.5).  Joining parts takes another launch, and their bytes come from the
+// caches (4 parts of 2,048 x 2,048 17, 16 of 1,024 x 1,024 15).
 Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
-    Plan p{0, 0, 0, 1, 0};
-    double least = 0.0;
+    Plan p{0, 0, 0, 1, 0, 0.0};
     const int64_t steps = tiles_of(k, 64) > 0 ? tiles_of(k, 64) : 1;
     for (int tile : {256, 128, 64, 16}) {
         if ((tile == 256 && !direct) || (tile == 16 && (m > 16 || !p_rows))) continue;
         const int64_t tm = tiles_of(m, tile), tn = tiles_of(n, tile <= 64 ? 64 : tile);
         const int64_t waves = tile == 16 ? 8 : tile == 64 ? (direct ? kApart<true> : kApart<false>) : 1;
-        for (int64_t s = 1; s <= tiles_of(steps, waves); s *= 2) {
-            const int64_t each = tiles_of(tiles_of(steps, waves), s) * waves, rounds = tiles_of(tm * tn * tiles_of(steps, each), kUnits);
-            if (tile <= 64 && tm * tn * tiles_of(steps, each) >= kMostApart) break;
-            double us = tile == 256 ? (each * 1.44 + 7.5) * rounds : tile == 128 ? (each * (direct ? 0.53 : 0.83) + 2.0) * rounds
-                      : (each / waves * (direct ? 0.75 : 2.5) + (direct ? 2.4 : 4.0)) * rounds;
-            if (s > 1) us += 4.0 + 4e-6 / 3.0 * (double)(2 * s) * (double)m * (double)n;
-            if (p.tile && us >= least) continue;
-            least = us;
-            p.tile = tile;
-            p.tm = (int)tm;
-            p.tn = (int)tn;
-            p.k_part = each * 64;
-            p.splits = (int)tiles_of(steps, each);
+        const int64_t turns = tiles_of(steps, waves);
+        for (int64_t s = 1; s <= turns && (s == 1 || tm * tn * s < 4 * kUnits); s += s < 8 ? 1 : s / 4) {
+            const int64_t each = tiles_of(turns, s) * waves, parts = tiles_of(steps, each), tiles = tm * tn * parts;
+            if (tile <= 64 && tiles >= kMostApart) break;
+            const int64_t rounds = tiles_of(tiles, kUnits);
+            const double busy = tiles < kUnits ? (double)tiles / kUnits : 1.0;
+            double us = tile == 256 ? each * (1.0 + 0.44 * busy) + 11.0 : tile == 128 ? each * (direct ? 0.4 + 0.13 * busy : 1.05) + 3.4
+                      : each / waves * (direct ? 0.75 : 2.5) + (direct ? 3.0 : 5.5);
+            us *= (double)rounds;
+            if (parts > 1) us += 4.0 + (0.1 + 0.8e-6 * (double)m * (double)n) * (double)parts;
+            if (p.tile && us >= p.us) continue;
+            p = Plan{tile, (int)tm, (int)tn, (int)parts, each * 64, us};
         }
     }
     return p;
@@ -91,8 +91,8 @@ __device__ __forceinline__ void store_as(void *p, int32_t type, int64_t i, float
     else static_cast<f16_t *>(p)[i] = (f16_t)x;
 }
 
-// Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  1,021 x 1,237 f16 4.4 us
-// (7.5 with parts).
+// Up to 4,096 rows in one launch: a workgroup has 64 columns, 128 rows at a time.  Bound: latency.  1,021 x 1,237
+// f16 6 us; with parts two launches, 9.
 constexpr int kFewRows = 4096;
 typedef float FewRoom[128][65];
 template <class T>
@@ -143,9 +143,10 @@ __global__ void __launch_bounds__(1024) k_column_sum_few(FewSums a) {
 
 // --- operands of odd sizes --------------------------------------------------------
 // Rows that are not multiples of 16 bytes cannot be loaded to LDS directly, which makes a step half as fast and
-// more.  Where the sizes themselves are odd and an operand is read many times, it is copied first, rows padded with
-// zeros to 16 bytes, and sums over few rows are taken by workgroups of the same launch.  4,099 x 1,237 -> 777 f16
-// PADFIG.
+// more.  Where the sizes themselves are odd, operands are copied first, rows padded with zeros to 16 bytes, if that is expected
+// to take less than it gains (4,099 x 1,237 -> 777 f16 29 us, of which the copies 8; 32 without.  A weight of
+// 15,219 x 3,471 bf16 is not copied for 139 rows: 45 us).  Sums over few rows are taken by workgroups of the same
+// launch (1,021 rows, 777 x 1,237 f16, all gradients: 35 us, 40 with a launch of their own).
 __global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows z, FewSums sums) {
     __shared__ FewRoom lds;
     const int which = (int)blockIdx.y - (sums.cols ? 1 : 0);
@@ -164,6 +165,10 @@ __global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows
     }
 }
 bool pads(int64_t m, int64_t n, int64_t k) { return (m % 8 || n % 8 || k % 8) && m > 64 && n > 64; }
+// whether a product gains more than copies of `bytes` take, and their launch
+bool padding_pays(int64_t m, int64_t n, int64_t k, bool p_rows, size_t bytes, double launch = 2.5) {
+    return plan_of(m, n, k, p_rows, true).us + launch + (double)bytes * (2.0 / 4.5e6) < plan_of(m, n, k, p_rows, false).us;
+}
 size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
     auto most = [&](int64_t i) { return i * tiles_of(k, 8) > k * tiles_of(i, 8) ? i * tiles_of(k, 8) : k * tiles_of(i, 8); };
     return pads(m, n, k) ? (size_t)(most(m) + most(n)) * 16 : 0;
@@ -174,7 +179,9 @@ hipError_t product(const Product &args, char *work, hipStream_t s) {
     Product a = args;
     const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k, a.padded & 1);
     const bool aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k, a.padded & 2);
-    const bool pad = !(ap && aq) && pads(a.m, a.n, a.k), direct = (ap && aq) || pad;
+    const bool pad = !(ap && aq) && pads(a.m, a.n, a.k) &&
+                     padding_pays(a.m, a.n, a.k, a.p_by_rows, (size_t)((ap ? 0 : a.m) + (aq ? 0 : a.n)) * (size_t)a.k * 2);
+    const bool direct = (ap && aq) || pad;
     const Plan p = plan_of(a.m, a.n, a.k, a.p_by_rows, direct);
     float *part = reinterpret_cast<float *>(work);
     if (pad) {
@@ -303,6 +310,10 @@ size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, voi
     stride = tiles_of(cols, 8) * 8;
     return padded_size(rows, cols);
 }
+
+bool loads_directly(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k) { return aligned_operand(p, stride, by_rows, count, k, false); }
+// (dy is copied all the same)
+bool weight_pads(int64_t rows, int64_t k, int64_t n) { return padding_pays(rows, k, n, true, (size_t)k * (size_t)n * 2, 0.0); }
 
 size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)tiles_of(cols, 8) * 16; }
 

@@ -18,6 +18,8 @@ size_t pad_rows(const void *&, int64_t &, int64_t rows, int64_t cols, void *, Pa
     return padded_size(rows, cols);
 }
 bool few_rows(int64_t, int64_t) { return true; }
+bool loads_directly(const void *, int64_t, bool, int64_t, int64_t) { return false; }
+bool weight_pads(int64_t, int64_t, int64_t) { return true; }
 hipError_t launch_pad_rows(const PadRows &, const PadRows &, const PadRows &, const FewSums &, hipStream_t) { STUB; }
 size_t column_sum_work(int64_t, int64_t cols) { return (size_t)cols * 4; }
 hipError_t launch_column_sum(const void *, int64_t, int64_t, int64_t, int32_t, void *, int32_t, void *, hipStream_t) { STUB; }
