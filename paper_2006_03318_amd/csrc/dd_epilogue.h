@@ -9,15 +9,15 @@
 namespace dd {
 
 // --- activations --------------------------------------------------------------
-// Phi(x) and exp(-x^2 / 2), from Abramowitz and Stegun 7.1.26 (off by 1.5e-7
-// at most).
-__device__ __forceinline__ void normal(float x, float &phi, float &e) {
-    const float a = fabsf(x) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.0f));
-    e = __builtin_amdgcn_exp2f(a * a * -1.44269504f);
-    const float s = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
-                                     0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
-    phi = x < 0.0f ? s : 1.0f - s;
+// Phi(-|x|) and exp(-x^2 / 2), from Abramowitz and Stegun 7.1.26 (off by 1.5e-7
+// at most).  Few instructions count: each takes 3.4 us of 16,384 x 2,048 -> 8,192, where
+// the matrix units wait: GELU 513 us, SiLU 485, none 475.
+__device__ __forceinline__ void normal(float x, float &below, float &e) {
+    const float u = x * 0.84932180f;        // sqrt(log2(e) / 2)
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.27273748f, fabsf(u), 1.0f));       // 0.3275911 |x| / sqrt(2)
+    e = __builtin_amdgcn_exp2f(-(u * u));
+    below = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f),
+                             0.5f * -0.284496736f), 0.5f * 0.254829592f) * e;
 }
 __device__ __forceinline__ float sigmoid(float x) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504f));
@@ -26,9 +26,9 @@ template <int ACT>
 __device__ __forceinline__ float act_of(float z) {
     if (ACT == DD_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;
     if (ACT == DD_ACT_GELU) {
-        float phi, e;
-        normal(z, phi, e);
-        return z * phi;
+        float below, e;
+        normal(z, below, e);
+        return fmaf(-fminf(fabsf(z), 1e30f), below, fmaxf(z, 0.0f));      // z Phi(z), also of infinities
     }
     if (ACT == DD_ACT_GELU_TANH) return z * sigmoid(z * fmaf(2.0f * 0.7978845608f * 0.044715f, z * z, 2.0f * 0.7978845608f));
     if (ACT == DD_ACT_SILU) return z * sigmoid(z);
@@ -38,9 +38,9 @@ template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
     if (ACT == DD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (ACT == DD_ACT_GELU) {
-        float phi, e;
-        normal(z, phi, e);
-        return fmaf(z * e, 0.3989422804f, phi);
+        float below, e;
+        normal(z, below, e);
+        return fmaf(z * e, 0.3989422804f, z < 0.0f ? below : 1.0f - below);
     }
     if (ACT == DD_ACT_GELU_TANH) {
         const float x = z > 20.0f ? 20.0f : z < -20.0f ? -20.0f : z;     // (x^2 in range; the slope is 0 or 1 there)

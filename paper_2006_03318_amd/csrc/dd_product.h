@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
 // Small products, whose bound are the weight's bytes or the latency of a step's loads.  A workgroup has one
 // tile of 16 MT rows by 64 columns, and each of its waves a run of the sums with tiles of its own in LDS, so that
 // no wave waits for another until the waves' sums are joined in order at the end.  4 x 2,048 -> 8,192 bf16 with GELU 9.4 us (33.6 MB
-// of weight at 3.6 TB/s, launch included; 14 with 128 x 128); 1,021 x 1,237 -> 777 f16 11, 25 with 128 x 128.
+// of weight at 3.6 TB/s, launch included); 1,021 x 1,237 -> 777 f16 with its copies 16.5, 24 with 128 x 128.
 template <class T, bool PROWS, bool QROWS, int MT, int WAVES, bool DIRECT>
 __global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *part, int tm, int tn, int splits, int64_t k_part) {
     constexpr int BK = 64, BN = 64, NT = BN / 32, STAGES = DIRECT ? 2 : 1;
