@@ -23,6 +23,8 @@ paper's rule, which keeps the summed time of the update), 98.2 measured fused.
 Tracing lengthens every host call, so an iteration whose host is the slower side
 has to be longer on the GPU for the trace to show it as it is: 16,384 rows take
 37.2 ms plain, 46.4 while traced, and 25.9 fused where 29.4 are predicted.
+With the products too, 65,536 rows take 92.4 ms where 93.3 are predicted (96.3
+with norms and update fused alone, in the same run), 16,384 rows 24.6.
 """
 from __future__ import annotations
 
