@@ -619,6 +619,7 @@ void runs(const dd_embed_grad_args &a, const Sorted &in, float *part, const Room
     const int64_t strips = (a.cols + 8 * LANES - 1) / (8 * LANES), groups = 256 / LANES;
     const int64_t of_runs = (r.chunks * strips + groups - 1) / groups, of_rows = (waves_of_rows(a, filled) + 3) / 4;
     k_embed_runs<T, LANES, CHUNK><<<(unsigned)(of_runs + of_rows), 256, 0, s>>>(a, in, part, r.chunks, (uint32_t)of_rows, strips, filled);
+    if (r.chunks < 2) return;
     const int64_t y = (a.cols + 255) / 256;
     k_embed_join<T, CHUNK><<<dim3((unsigned)((r.chunks + kJoinWaves - 1) / kJoinWaves), (unsigned)(y < 1024 ? y : 1024)), 64 * kJoinWaves, 0, s>>>(a, in, part);
 }

@@ -220,7 +220,8 @@ class Dropout:
     again; p counts in 65,536ths.  The generator's key and counter are on the GPU
     (`state`): `step()`, once an iteration, moves the counter behind the calls made
     so far, and is captured with them where an iteration is captured, so that every replay has
-    other masks."""
+    other masks.  A forward pass that is run again for its gradient (checkpointed) gets
+    other masks than the first time: keep dropouts out of it."""
 
     def __init__(self, seed: int = 0, device="cuda"):
         key = seed & (1 << 64) - 1
