@@ -530,8 +530,8 @@ size_t dd_linear_work(int64_t rows, int64_t k, int64_t n);
  * dw and db of no rows are zeros.  dx may be in_z or x, element for element.
  * Sums over many rows are cut into parts whose sums are joined in order: the same
  * bits on every call.
- *   work holds these parts and, where rows, k or n is no multiple of 8, copies of
- * operands with rows padded to 16 bytes (in dd_linear too).
+ *   work holds these parts and copies of operands whose rows 16 bytes do not divide
+ * (in dd_linear too).
  */
 typedef struct {
     int64_t rows, k, n;

@@ -41,7 +41,13 @@ struct PadRows {
 size_t padded_size(int64_t rows, int64_t cols);
 // an operand, `count` rows (or columns) of k sums, needs no copy
 bool loads_directly(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k);
-bool weight_pads(int64_t rows, int64_t k, int64_t n);       // the gradient of the rows gains from a padded weight
+// Operands of a layer's gradients that are copied once for both products.  needed: those that do not load directly
+// as they are; grad_copies_work bytes hold all (0: none is copied).
+struct GradCopies {
+    bool dy, x, w;
+};
+GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool turned, const GradCopies &needed);
+size_t grad_copies_work(int64_t rows, int64_t k, int64_t n);
 // x and its stride become those of the copy in `to`; the size of the copy
 size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, void *to, PadRows *r);
 // Sums over few rows of an array (type), into out (out_type).  No columns: none.
@@ -56,6 +62,7 @@ hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z,
 
 // bytes of working memory of an m by n product of k sums (0: none), and the product
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_by_rows);
+size_t product_need(const Product &p);      // of these operands: at most that
 bool product_fits(int64_t m, int64_t n, int64_t k, bool p_by_rows);      // one launch takes it
 hipError_t launch_product(const Product &p, void *work, hipStream_t s);
 

@@ -99,23 +99,15 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         p.e.out = a->y;
         p.e.out_stride = a->y_stride;
         hipStream_t s = (hipStream_t)stream;
-        return with_work(a->work, dd::product_work(a->rows, a->n, a->k, true), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
+        return with_work(a->work, dd::product_need(p), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
     });
-}
-
-// Whether the gradients of the weight and of the rows are taken from dy padded once for both (its rows
-// cannot be loaded as they are, and each is read many times), and from padded rows; from a padded weight, if that pays.
-static bool pads_once(int64_t rows, int64_t k, int64_t n) { return n % 8 && rows > 64 && k > 64 && n > 64; }
-static size_t pads_once_size(int64_t rows, int64_t k, int64_t n) {
-    const size_t w = dd::padded_size(k, n), turned = dd::padded_size(n, k);
-    return dd::padded_size(rows, n) + dd::padded_size(rows, k) + (w > turned ? w : turned);
 }
 
 size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
     if (!sizes_known(rows, k, n)) return 0;
     size_t most = dd::column_sum_work(rows, n);
     for (size_t x : {rows > 0 ? dd::product_work(rows, k, n, true) : 0, dd::product_work(k, n, rows, false), dd::product_work(n, k, rows, false)}) most = x > most ? x : most;
-    return most + (pads_once(rows, k, n) ? pads_once_size(rows, k, n) : 0);
+    return most + (rows > 0 ? dd::grad_copies_work(rows, k, n) : 0);
 }
 
 dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
@@ -141,57 +133,58 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
         }
         if (!aligned(a->db, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "db is not aligned to its elements");
         hipStream_t s = (hipStream_t)stream;
-        size_t need = 0;
-        auto needs = [&](size_t x) { need = x > need ? x : need; };
-        if (a->dw) needs(dd::product_work(wr, wc, a->rows, false));
-        if (a->db) needs(dd::column_sum_work(a->rows, a->n));
-        if (a->dx && a->rows > 0) needs(dd::product_work(a->rows, a->k, a->n, true));
-        const bool pad = a->dw && a->dx && pads_once(a->rows, a->k, a->n);
-        if (pad) need += pads_once_size(a->rows, a->k, a->n);
-        return with_work(a->work, need, s, "linear gradient", [&](void *given) {
-            char *work = static_cast<char *>(given);
+        dd::GradCopies copies{};
+        if (a->dw && a->dx && a->rows > 0) {
+            const bool of_dy = !dd::loads_directly(a->dy, a->dy_stride, true, a->rows, a->n) || !dd::loads_directly(a->dy, a->dy_stride, false, a->n, a->rows);
+            copies = dd::grad_copies(a->rows, a->k, a->n, a->turned, dd::GradCopies{of_dy, !dd::loads_directly(a->x, a->x_stride, false, a->k, a->rows),
+                                                                                     !dd::loads_directly(a->w, a->w_stride, !a->turned, a->k, a->n)});
+        }
+        // the two products, with copies in `work` (of which the size is returned)
+        dd::Product dw{}, dx{};
+        dd::PadRows pads[3];
+        auto lay_out = [&](char *work) {
+            const char *begin = work;
             const void *dy = a->dy, *x = a->x, *w = a->w;
             int64_t dy_stride = a->dy_stride, x_stride = a->x_stride, w_stride = a->w_stride;
+            for (dd::PadRows &r : pads) r = dd::PadRows{};
+            dd::PadRows *r = pads;
+            if (copies.dy) work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, r++);
+            if (copies.x) work += dd::pad_rows(x, x_stride, a->rows, a->k, work, r++);
+            if (copies.w) work += dd::pad_rows(w, w_stride, wr, wc, work, r++);
+            dw = dd::Product{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, copies.x | copies.dy << 1, {}};
+            if (a->turned) dw = dd::Product{dy, x, wr, wc, a->rows, dy_stride, x_stride, 0, 0, a->type, copies.dy | copies.x << 1, {}};
+            dw.e.out = a->dw;
+            dw.e.out_stride = a->dw_stride;
+            dx = dd::Product{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, copies.dy | copies.w << 1, {}};
+            dx.e.in_z = a->in_z;
+            dx.e.side_stride = a->in_z_stride;
+            dx.e.in_act = a->in_act;
+            dx.e.out = a->dx;
+            dx.e.out_stride = a->dx_stride;
+            return (size_t)(work - begin);
+        };
+        const size_t copied = lay_out(reinterpret_cast<char *>(uintptr_t(16)));      // (an address as aligned as the memory's)
+        size_t need = 0;
+        auto needs = [&](size_t x) { need = x > need ? x : need; };
+        if (a->dw) needs(dd::product_need(dw));
+        if (a->db) needs(dd::column_sum_work(a->rows, a->n));
+        if (a->dx && a->rows > 0) needs(dd::product_need(dx));
+        return with_work(a->work, copied + need, s, "linear gradient", [&](void *given) {
+            char *work = static_cast<char *>(given);
             hipError_t e = hipSuccess;
             bool summed = false;
-            int padded = 0;         // of dy and w
-            if (pad) {
-                dd::PadRows r[3] = {};
-                const bool of_x = !dd::loads_directly(x, x_stride, false, a->k, a->rows);
-                const bool of_w = !dd::loads_directly(w, w_stride, !a->turned, a->k, a->n) && dd::weight_pads(a->rows, a->k, a->n);
-                work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, &r[0]);
-                if (of_x) work += dd::pad_rows(x, x_stride, a->rows, a->k, work, &r[1]);
-                if (of_w) work += dd::pad_rows(w, w_stride, wr, wc, work, &r[of_x ? 2 : 1]);
-                padded = of_w ? 3 : 1;
+            if (copied) {
+                work += lay_out(work);
                 dd::FewSums sums{};
                 if (a->db && dd::few_rows(a->rows, a->n)) {
                     sums = dd::FewSums{a->dy, a->db, a->dy_stride, a->n, (int32_t)a->rows, a->type, a->bias_type};
                     summed = true;
                 }
-                e = dd::launch_pad_rows(r[0], r[1], r[2], sums, s);
+                e = dd::launch_pad_rows(pads[0], pads[1], pads[2], sums, s);
             }
-            if (e == hipSuccess && a->dw) {
-                dd::Product p{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, pad ? 3 : 0, {}};
-                if (a->turned) {
-                    p.p = dy;
-                    p.p_stride = dy_stride;
-                    p.q = x;
-                    p.q_stride = x_stride;
-                }
-                p.e.out = a->dw;
-                p.e.out_stride = a->dw_stride;
-                e = dd::launch_product(p, work, s);
-            }
-            if (e == hipSuccess && a->db && !summed) e = dd::launch_column_sum(dy, dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
-            if (e == hipSuccess && a->dx && a->rows > 0) {      // (last: it may be x)
-                dd::Product p{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, padded, {}};
-                p.e.in_z = a->in_z;
-                p.e.side_stride = a->in_z_stride;
-                p.e.in_act = a->in_act;
-                p.e.out = a->dx;
-                p.e.out_stride = a->dx_stride;
-                e = dd::launch_product(p, work, s);
-            }
+            if (e == hipSuccess && a->dw) e = dd::launch_product(dw, work, s);
+            if (e == hipSuccess && a->db && !summed) e = dd::launch_column_sum(a->dy, a->dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
+            if (e == hipSuccess && a->dx && a->rows > 0) e = dd::launch_product(dx, work, s);      // (last: it may be x)
             return e;
         });
     });

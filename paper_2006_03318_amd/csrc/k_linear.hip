@@ -143,8 +143,8 @@ __global__ void __launch_bounds__(1024) k_column_sum_few(FewSums a) {
 
 // --- operands of odd sizes --------------------------------------------------------
 // Rows that are not multiples of 16 bytes cannot be loaded to LDS directly, which makes a step half as fast and
-// more.  Where the sizes themselves are odd, operands are copied first, rows padded with zeros to 16 bytes, if that is expected
-// to take less than it gains (4,099 x 1,237 -> 777 f16 29 us, of which the copies 8; 32 without.  A weight of
+// more.  So operands are copied first, rows padded with zeros to 16 bytes, if that is expected to take less than it
+// gains (4,099 x 1,237 -> 777 f16 29 us, of which the copies 8; 32 without.  A weight of
 // 15,219 x 3,471 bf16 is not copied for 139 rows: 45 us).  Sums over few rows are taken by workgroups of the same
 // launch (1,021 rows, 777 x 1,237 f16, all gradients: 35 us, 40 with a launch of their own).
 __global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows z, FewSums sums) {
@@ -164,35 +164,53 @@ __global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows
         v.store(static_cast<bf16_t *>(r.to) + t * 8);
     }
 }
-bool pads(int64_t m, int64_t n, int64_t k) { return (m % 8 || n % 8 || k % 8) && m > 64 && n > 64; }
-// whether a product gains more than copies of `bytes` take, and their launch
-bool padding_pays(int64_t m, int64_t n, int64_t k, bool p_rows, size_t bytes, double launch = 2.5) {
-    return plan_of(m, n, k, p_rows, true).us + launch + (double)bytes * (2.0 / 4.5e6) < plan_of(m, n, k, p_rows, false).us;
+// Whether operands may be copied: always for odd sizes; where only strides or addresses are in the way, which the size of
+// the working memory does not know, up to kMostCopied bytes (249 rows of 14,400 x 1,136 bf16 at odd strides, all
+// gradients: 56 us, 62 through registers).
+constexpr int64_t kMostCopied = int64_t(64) << 20;
+bool pads(int64_t m, int64_t n, int64_t k) {
+    if (m <= 64 || n <= 64) return false;
+    return m % 8 || n % 8 || k % 8 || (double)(m + n) * (double)k * 2.0 <= (double)kMostCopied;
 }
+double copy_us(size_t bytes) { return (double)bytes * (2.0 / 4.5e6); }
+constexpr double kCopyLaunch = 2.5;
 size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
     auto most = [&](int64_t i) { return i * tiles_of(k, 8) > k * tiles_of(i, 8) ? i * tiles_of(k, 8) : k * tiles_of(i, 8); };
     return pads(m, n, k) ? (size_t)(most(m) + most(n)) * 16 : 0;
 }
 
+// How a product runs: which operands are copied, and the plan.
+struct Way {
+    bool copy_p, copy_q, direct;
+    Plan plan;
+};
+Way way_of(const Product &a) {
+    const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k, a.padded & 1);
+    const bool aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k, a.padded & 2);
+    const Plan direct = plan_of(a.m, a.n, a.k, a.p_by_rows, true);
+    if ((ap && aq) || a.k == 0) return Way{false, false, true, direct};     // (no sums: nothing is loaded)
+    const Plan any = plan_of(a.m, a.n, a.k, a.p_by_rows, false);
+    const size_t bytes = (size_t)((ap ? 0 : a.m) + (aq ? 0 : a.n)) * (size_t)a.k * 2;
+    if (pads(a.m, a.n, a.k) && direct.us + kCopyLaunch + copy_us(bytes) < any.us) return Way{!ap, !aq, true, direct};
+    return Way{false, false, false, any};
+}
+size_t up16(size_t x) { return (x + 15) / 16 * 16; }
+
 template <class T>
 hipError_t product(const Product &args, char *work, hipStream_t s) {
     Product a = args;
-    const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k, a.padded & 1);
-    const bool aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k, a.padded & 2);
-    const bool pad = !(ap && aq) && pads(a.m, a.n, a.k) &&
-                     padding_pays(a.m, a.n, a.k, a.p_by_rows, (size_t)((ap ? 0 : a.m) + (aq ? 0 : a.n)) * (size_t)a.k * 2);
-    const bool direct = (ap && aq) || pad;
-    const Plan p = plan_of(a.m, a.n, a.k, a.p_by_rows, direct);
+    const Way way = way_of(a);
+    const Plan &p = way.plan;
     float *part = reinterpret_cast<float *>(work);
-    if (pad) {
-        char *to = work + (plan_work(p, a.m, a.n) + 15) / 16 * 16;
+    if (way.copy_p || way.copy_q) {
+        char *to = work + up16(plan_work(p, a.m, a.n));
         PadRows x{}, y{};
-        if (!ap) to += pad_rows(a.p, a.p_stride, a.p_by_rows ? a.m : a.k, a.p_by_rows ? a.k : a.m, to, &x);
-        if (!aq) pad_rows(a.q, a.q_stride, a.q_by_rows ? a.n : a.k, a.q_by_rows ? a.k : a.n, to, &y);
+        if (way.copy_p) to += pad_rows(a.p, a.p_stride, a.p_by_rows ? a.m : a.k, a.p_by_rows ? a.k : a.m, to, &x);
+        if (way.copy_q) pad_rows(a.q, a.q_stride, a.q_by_rows ? a.n : a.k, a.q_by_rows ? a.k : a.n, to, way.copy_p ? &y : &x);
         const hipError_t e = launch_pad_rows(x, y, PadRows{}, FewSums{}, s);
         if (e != hipSuccess) return e;
     }
-    if (direct) launch_tiles<T, true>(a, p, part, s);
+    if (way.direct) launch_tiles<T, true>(a, p, part, s);
     else launch_tiles<T, false>(a, p, part, s);
     if (p.splits > 1) {
         const int64_t need = tiles_of(a.m * tiles_of(a.n, 8), 256);
@@ -312,8 +330,28 @@ size_t pad_rows(const void *&x, int64_t &stride, int64_t rows, int64_t cols, voi
 }
 
 bool loads_directly(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k) { return aligned_operand(p, stride, by_rows, count, k, false); }
-// (dy is copied all the same)
-bool weight_pads(int64_t rows, int64_t k, int64_t n) { return padding_pays(rows, k, n, true, (size_t)k * (size_t)n * 2, 0.0); }
+
+GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool turned, const GradCopies &needed) {
+    if (!needed.dy || !grad_copies_work(rows, k, n)) return GradCopies{};
+    auto us = [&](bool of_dw, bool direct) {
+        return of_dw ? plan_of(turned ? n : k, turned ? k : n, rows, false, direct).us : plan_of(rows, k, n, true, direct).us;
+    };
+    const size_t dy = (size_t)rows * (size_t)n * 2, x = needed.x ? (size_t)rows * (size_t)k * 2 : 0, w = needed.w ? (size_t)k * (size_t)n * 2 : 0;
+    auto alone = [&](bool of_dw, size_t bytes) {
+        const double any = us(of_dw, false), copied = us(of_dw, true) + kCopyLaunch + copy_us(bytes);
+        return any < copied ? any : copied;
+    };
+    const double apart = alone(true, dy + x) + alone(false, dy + w), both = us(true, true) + kCopyLaunch + copy_us(dy + x);
+    const double with_w = both + copy_us(w) + us(false, true), without = both + us(false, !needed.w);
+    if (apart <= with_w && apart <= without) return GradCopies{};
+    return GradCopies{true, needed.x, needed.w && with_w < without};
+}
+
+size_t grad_copies_work(int64_t rows, int64_t k, int64_t n) {
+    if (rows <= 64 || k <= 64 || n <= 64) return 0;
+    const size_t w = padded_size(k, n), turned = padded_size(n, k), all = padded_size(rows, n) + padded_size(rows, k) + (w > turned ? w : turned);
+    return n % 8 || all <= (size_t)kMostCopied ? all : 0;
+}
 
 size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)tiles_of(cols, 8) * 16; }
 
@@ -329,8 +367,16 @@ hipError_t launch_pad_rows(const PadRows &x, const PadRows &y, const PadRows &z,
 }
 
 size_t product_work(int64_t m, int64_t n, int64_t k, bool p_rows) {
-    const size_t a = (plan_work(plan_of(m, n, k, p_rows, true), m, n) + 15) / 16 * 16 + pad_work(m, n, k), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
+    const size_t a = up16(plan_work(plan_of(m, n, k, p_rows, true), m, n)) + pad_work(m, n, k), b = plan_work(plan_of(m, n, k, p_rows, false), m, n);
     return a > b ? a : b;
+}
+
+size_t product_need(const Product &a) {
+    const Way way = way_of(a);
+    const size_t parts = plan_work(way.plan, a.m, a.n);
+    if (!way.copy_p && !way.copy_q) return parts;
+    return up16(parts) + (way.copy_p ? padded_size(a.p_by_rows ? a.m : a.k, a.p_by_rows ? a.k : a.m) : 0) +
+           (way.copy_q ? padded_size(a.q_by_rows ? a.n : a.k, a.q_by_rows ? a.k : a.n) : 0);
 }
 
 bool product_fits(int64_t m, int64_t n, int64_t k, bool p_rows) {

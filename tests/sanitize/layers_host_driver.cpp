@@ -19,7 +19,9 @@ size_t pad_rows(const void *&, int64_t &, int64_t rows, int64_t cols, void *, Pa
 }
 bool few_rows(int64_t, int64_t) { return true; }
 bool loads_directly(const void *, int64_t, bool, int64_t, int64_t) { return false; }
-bool weight_pads(int64_t, int64_t, int64_t) { return true; }
+size_t product_need(const Product &p) { return product_work(p.m, p.n, p.k, true); }
+size_t grad_copies_work(int64_t rows, int64_t k, int64_t n) { return n % 8 && rows > 64 ? (size_t)(rows * (n + k) + k * n) * 2 : 0; }
+GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool, const GradCopies &needed) { return grad_copies_work(rows, k, n) ? needed : GradCopies{}; }
 hipError_t launch_pad_rows(const PadRows &, const PadRows &, const PadRows &, const FewSums &, hipStream_t) { STUB; }
 size_t column_sum_work(int64_t, int64_t cols) { return (size_t)cols * 4; }
 hipError_t launch_column_sum(const void *, int64_t, int64_t, int64_t, int32_t, void *, int32_t, void *, hipStream_t) { STUB; }
@@ -102,6 +104,14 @@ int main() {
     EXPECT(failed_on_device(dd_linear_grad(&g, nullptr)), "dw of no rows");
     g.in_act = DD_ACT_GELU;
     EXPECT(dd_linear_grad(&g, nullptr) == DD_EINVAL, "in_act without in_z");
+    g.in_act = DD_ACT_NONE;
+    g.rows = 100;
+    g.n = 81;
+    g.dy_stride = g.w_stride = g.dw_stride = 81;
+    g.work = nullptr;
+    EXPECT(failed_on_device(dd_linear_grad(&g, nullptr)), "copies without a device");
+    g.work = room;
+    EXPECT(failed_on_device(dd_linear_grad(&g, nullptr)), "copies in given memory without a device");
 
     dd_act_grad_args a;
     memset(&a, 0, sizeof(a));

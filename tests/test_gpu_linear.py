@@ -370,14 +370,16 @@ def test_sums_of_more_columns_than_a_launch_has_threads_for():
     assert torch.equal(db, dy[0] + dy[1])
 
 
-@pytest.mark.parametrize("rows,k,n", [(4, 8192, 136), (300, 321, 131), (8192, 24, 40), (70, 5000, 90), (129, 127, 129), (1021, 777, 1237)])
-def test_nothing_behind_the_working_memory(rows, k, n):
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("rows,k,n", [(4, 8192, 136), (300, 321, 131), (8192, 24, 40), (70, 5000, 90), (129, 127, 129), (1021, 777, 1237),
+                                      (256, 1440, 1136), (2048, 136, 2048), (72, 3471, 1219)])
+def test_nothing_behind_the_working_memory(rows, k, n, pad):
     """Exactly the bytes that are asked for, at the end of a buffer of which the rest stays as it was."""
     import torch
     require_gpu()
     gen = torch.Generator("cuda").manual_seed(8)
-    x, w, dy = (torch.randint(-2, 3, s, generator=gen, device="cuda").to(torch.bfloat16) for s in ((rows, k), (k, n), (rows, n)))
-    y, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+    x, w, dy = (torch.randint(-2, 3, (a, b + pad), generator=gen, device="cuda").to(torch.bfloat16)[:, :b] for a, b in ((rows, k), (k, n), (rows, n)))
+    y, dx, dw, db = torch.empty(rows, n, device="cuda", dtype=x.dtype), torch.empty(rows, k, device="cuda", dtype=x.dtype), torch.empty_like(w), torch.empty(n, device="cuda")
     for need, call in ((B.dd_linear_work(rows, k, n), lambda m: B.dd_linear(x, w, y, work=m)),
                        (B.dd_linear_grad_work(rows, k, n), lambda m: B.dd_linear_grad(dy, x, w, dx=dx, dw=dw, db=db, work=m))):
         room = torch.full((1024 + need + 4096,), 171, device="cuda", dtype=torch.uint8)
@@ -385,3 +387,4 @@ def test_nothing_behind_the_working_memory(rows, k, n):
         torch.cuda.synchronize()
         assert bool((room[:1024] == 171).all()) and bool((room[1024 + need:] == 171).all())
     assert torch.equal(y, (x.double() @ w.double()).to(torch.bfloat16)) and torch.equal(db.double(), dy.double().sum(0))
+    assert torch.equal(dx, (dy.double() @ w.double().t()).to(torch.bfloat16)) and torch.equal(dw, (x.double().t() @ dy.double()).to(torch.bfloat16))
