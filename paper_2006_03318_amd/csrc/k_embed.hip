@@ -17,29 +17,37 @@ __device__ __forceinline__ int64_t id_at(const void *ids, int bytes, int64_t t) 
 }
 __host__ __device__ inline int have_of(int64_t n, int64_t i) { return n - i >= 8 ? 8 : n - i < 0 ? 0 : (int)(n - i); }
 
-// A thread has eight columns of a token.  Bound: HBM; few tokens, the launch.  65,536 words of 32,000 x 1,024 bf16 in
-// 49 us (rows read again come from the caches: 5.5 TB/s), 4 in 5.
-template <class T>
+// A thread has eight columns of a token, or of EACH tokens whose rows are loaded at once.  Bound: HBM; few
+// tokens, the launch.
+template <class T, int EACH>
 __global__ void __launch_bounds__(256) k_embed(dd_embed_args a, uint32_t packs) {
     const int64_t total = a.tokens * packs;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t t = (uint64_t)i >> 32 ? i / packs : (int64_t)((uint32_t)i / packs);
-        const int64_t c = (i - t * packs) * 8;
-        const int have = have_of(a.cols, c);
-        const int64_t id = id_at(a.ids, a.id_bytes, t);
-        Pack<T, 8> p;
-        float x[8];
-        if (id >= 0 && id < a.vocab) {
-            p.load(static_cast<const T *>(a.table) + id * a.table_stride + c, have);
-            p.to(x);
+    for (int64_t i0 = blockIdx.x * (int64_t)(256 * EACH) + threadIdx.x; i0 < total; i0 += (int64_t)gridDim.x * (256 * EACH)) {
+        int64_t t[EACH], c[EACH], id[EACH];
+        Pack<T, 8> p[EACH];
 #pragma unroll
-            for (int j = 0; j < 8; j++) x[j] *= a.scale;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = __builtin_nanf("");
+        for (int u = 0; u < EACH; u++) {
+            const int64_t i = i0 + 256 * u < total ? i0 + 256 * u : i0;
+            t[u] = (uint64_t)i >> 32 ? i / packs : (int64_t)((uint32_t)i / packs);
+            c[u] = (i - t[u] * packs) * 8;
+            id[u] = id_at(a.ids, a.id_bytes, t[u]);
         }
-        p.from(x);
-        p.store(static_cast<T *>(a.out) + t * a.out_stride + c, have);
+#pragma unroll
+        for (int u = 0; u < EACH; u++) {
+            const bool there = id[u] >= 0 && id[u] < a.vocab;
+            p[u].load(static_cast<const T *>(a.table) + (there ? id[u] : 0) * a.table_stride + c[u], there ? have_of(a.cols, c[u]) : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < EACH; u++) {
+            if (i0 + 256 * u >= total) continue;
+            const bool there = id[u] >= 0 && id[u] < a.vocab;
+            float x[8];
+            p[u].to(x);
+#pragma unroll
+            for (int j = 0; j < 8; j++) x[j] = there ? x[j] * a.scale : __builtin_nanf("");
+            p[u].from(x);
+            p[u].store(static_cast<T *>(a.out) + t[u] * a.out_stride + c[u], have_of(a.cols, c[u]));
+        }
     }
 }
 
@@ -662,12 +670,20 @@ void embed_grad(const dd_embed_grad_args &a, void *work, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_embed(const dd_embed_args &a, hipStream_t s) {
+template <class T>
+static void embed(const dd_embed_args &a, hipStream_t s) {
+    // (two of 16 bits fill the compute units' queues: 65,536 words of 32,000 x 1,024 bf16 43 us, 49 with one, 42 with
+    // eight; 32 bits have two loads as it is: x 1,000 87, 88 with two)
+    constexpr int kEach = sizeof(T) == 2 ? 2 : 1;
     const int64_t packs = (a.cols + 7) / 8, need = (a.tokens * packs + 255) / 256;
-    const unsigned grid = (unsigned)(need < (1 << 20) ? need : (1 << 20));
-    if (a.type == DD_F32) k_embed<float><<<grid, 256, 0, s>>>(a, (uint32_t)packs);
-    else if (a.type == DD_BF16) k_embed<bf16_t><<<grid, 256, 0, s>>>(a, (uint32_t)packs);
-    else k_embed<f16_t><<<grid, 256, 0, s>>>(a, (uint32_t)packs);
+    if (need < 4096) k_embed<T, 1><<<(unsigned)need, 256, 0, s>>>(a, (uint32_t)packs);
+    else k_embed<T, kEach><<<(unsigned)(need / kEach < (1 << 20) ? (need + kEach - 1) / kEach : (1 << 20)), 256, 0, s>>>(a, (uint32_t)packs);
+}
+
+hipError_t launch_embed(const dd_embed_args &a, hipStream_t s) {
+    if (a.type == DD_F32) embed<float>(a, s);
+    else if (a.type == DD_BF16) embed<bf16_t>(a, s);
+    else embed<f16_t>(a, s);
     return hipGetLastError();
 }
 

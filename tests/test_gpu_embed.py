@@ -20,7 +20,7 @@ def _bound(got, want, slack):
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("id_kind", ["int64", "int32"])
-@pytest.mark.parametrize("tokens,vocab,cols,pad", [(1, 1, 1, 0), (4, 100, 2048, 0), (77, 5, 7, 3), (300, 1000, 129, 7), (2000, 50, 16, 0)])
+@pytest.mark.parametrize("tokens,vocab,cols,pad", [(1, 1, 1, 0), (4, 100, 2048, 0), (77, 5, 7, 3), (300, 1000, 129, 7), (2000, 50, 16, 0), (40001, 50, 250, 0), (5001, 70, 1700, 3)])
 def test_lookup(tokens, vocab, cols, pad, kind, id_kind):
     import torch
     require_gpu()
@@ -182,3 +182,18 @@ def test_nothing_behind_the_working_memory(tokens, vocab, cols):
     torch.cuda.synchronize()
     assert bool((room[:1024] == 171).all()) and bool((room[1024 + need:] == 171).all())
     assert torch.equal(out, torch.bincount(ids, minlength=vocab).float()[:, None].expand(vocab, cols))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_many_ids_that_the_table_does_not_have(kind):
+    import torch
+    require_gpu()
+    t = getattr(torch, kind)
+    gen = torch.Generator("cuda").manual_seed(9)
+    table = torch.randint(-3, 4, (1000, 520), generator=gen, device="cuda").to(t)
+    ids = torch.randint(-200, 1200, (20003,), generator=gen, device="cuda")
+    out = torch.empty(20003, 520, device="cuda", dtype=t)
+    B.dd_embed(ids, table, out, scale=2.0)
+    torch.cuda.synchronize()
+    bad = (ids < 0) | (ids >= 1000)
+    assert bool(out[bad].isnan().all()) and torch.equal(out[~bad], 2 * table[ids[~bad]])
