@@ -29,6 +29,7 @@ struct Product {
     int32_t p_by_rows, q_by_rows;
     int32_t type;
     int32_t padded;             // 1: p's, 2: q's rows are padded with zeros to 16 bytes, whatever their length
+    int32_t small;              // 1: aligned operands go in tiles of 64 x 64, uncut
     Epilogue e;
 };
 
@@ -65,6 +66,11 @@ size_t product_work(int64_t m, int64_t n, int64_t k, bool p_by_rows);
 size_t product_need(const Product &p);      // of these operands: at most that
 bool product_fits(int64_t m, int64_t n, int64_t k, bool p_by_rows);      // one launch takes it
 hipError_t launch_product(const Product &p, void *work, hipStream_t s);
+// Whether the products of a layer's gradients take less in one launch, by their sizes (both are `small` then, which one
+// alone is too, for the same bits), and by their operands; that launch, without working memory.
+bool small_gradients(int64_t rows, int64_t k, int64_t n, bool turned);
+bool goes_together(const Product &dw, const Product &dx);
+hipError_t launch_together(const Product &dw, const Product &dx, hipStream_t s);
 
 // sums over the rows of an array (type, rows) into out (out_type), with
 // column_sum_work bytes

@@ -55,6 +55,13 @@ dd_status check_product(int64_t m, int64_t n, int64_t k, bool p_by_rows) {
     return dd::product_fits(m, n, k, p_by_rows) ? DD_OK : fail(DD_EINVAL, "a product of %lld by %lld is too large for one launch", (long long)m, (long long)n);
 }
 
+// Whether two arrays of rows of 16-bit elements have bytes in common (or rows that lie between each other's).
+bool overlap(const void *x, int64_t x_stride, const void *y, int64_t y_stride, int64_t rows, int64_t cols) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+    auto bytes = [&](int64_t stride) { return (uintptr_t)((rows > 1 ? (rows - 1) * stride : 0) + cols) * 2; };
+    return a < b + bytes(y_stride) && b < a + bytes(x_stride);
+}
+
 bool sizes_known(int64_t rows, int64_t k, int64_t n) { return rows >= 0 && k >= 1 && n >= 1 && rows < kMost && k < kMost && n < kMost; }
 
 dd_status check_table(int64_t tokens, int64_t vocab, int64_t cols, int32_t type, const void *ids, int32_t id_bytes, float scale, int32_t reserved) {
@@ -88,7 +95,7 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
         CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
         if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
         CHECK(check_product(a->rows, a->n, a->k, true));
-        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, 0, {}};
+        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, 0, 0, {}};
         p.e.bias = a->bias;
         p.e.bias_type = a->bias_type;
         p.e.act = a->act;
@@ -139,6 +146,7 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             copies = dd::grad_copies(a->rows, a->k, a->n, a->turned, dd::GradCopies{of_dy, !dd::loads_directly(a->x, a->x_stride, false, a->k, a->rows),
                                                                                      !dd::loads_directly(a->w, a->w_stride, !a->turned, a->k, a->n)});
         }
+        const int32_t small = a->rows > 0 && dd::small_gradients(a->rows, a->k, a->n, a->turned);
         // the two products, with copies in `work` (of which the size is returned)
         dd::Product dw{}, dx{};
         dd::PadRows pads[3];
@@ -151,11 +159,11 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
             if (copies.dy) work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, r++);
             if (copies.x) work += dd::pad_rows(x, x_stride, a->rows, a->k, work, r++);
             if (copies.w) work += dd::pad_rows(w, w_stride, wr, wc, work, r++);
-            dw = dd::Product{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, copies.x | copies.dy << 1, {}};
-            if (a->turned) dw = dd::Product{dy, x, wr, wc, a->rows, dy_stride, x_stride, 0, 0, a->type, copies.dy | copies.x << 1, {}};
+            dw = dd::Product{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, copies.x | copies.dy << 1, small, {}};
+            if (a->turned) dw = dd::Product{dy, x, wr, wc, a->rows, dy_stride, x_stride, 0, 0, a->type, copies.dy | copies.x << 1, small, {}};
             dw.e.out = a->dw;
             dw.e.out_stride = a->dw_stride;
-            dx = dd::Product{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, copies.dy | copies.w << 1, {}};
+            dx = dd::Product{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, copies.dy | copies.w << 1, small, {}};
             dx.e.in_z = a->in_z;
             dx.e.side_stride = a->in_z_stride;
             dx.e.in_act = a->in_act;
@@ -182,9 +190,13 @@ dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
                 }
                 e = dd::launch_pad_rows(pads[0], pads[1], pads[2], sums, s);
             }
-            if (e == hipSuccess && a->dw) e = dd::launch_product(dw, work, s);
+            const void *x = a->turned ? dw.q : dw.p;
+            const int64_t x_stride = a->turned ? dw.q_stride : dw.p_stride;
+            const bool both = a->dw && a->dx && a->rows > 0 && dd::goes_together(dw, dx) && !overlap(a->dx, a->dx_stride, x, x_stride, a->rows, a->k);
+            if (e == hipSuccess && both) e = dd::launch_together(dw, dx, s);
+            if (e == hipSuccess && a->dw && !both) e = dd::launch_product(dw, work, s);
             if (e == hipSuccess && a->db && !summed) e = dd::launch_column_sum(a->dy, a->dy_stride, a->rows, a->n, a->type, a->db, a->bias_type, work, s);
-            if (e == hipSuccess && a->dx && a->rows > 0) e = dd::launch_product(dx, work, s);      // (last: it may be x)
+            if (e == hipSuccess && a->dx && a->rows > 0 && !both) e = dd::launch_product(dx, work, s);      // (last: it may be x)
             return e;
         });
     });

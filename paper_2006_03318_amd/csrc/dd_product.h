@@ -22,6 +22,9 @@ constexpr int kApart = DIRECT ? 4 : 8;      // waves that share the sums of a ti
 // the tiles' passes; of a plan for aligned operands (DIRECT) or any
 template <class T, bool DIRECT>
 void launch_tiles(const Product &a, const Plan &p, float *part, hipStream_t s);
+// both products of a layer's gradients in tiles of 64 x 64, uncut, with aligned operands
+template <class T>
+void launch_two(const Product &a, const Product &b, hipStream_t s);
 
 }  // namespace dd
 
@@ -449,20 +452,21 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
 // tile of 16 MT rows by 64 columns, and each of its waves a run of the sums with tiles of its own in LDS, so that
 // no wave waits for another until the waves' sums are joined in order at the end.  4 x 2,048 -> 8,192 bf16 with GELU 9.4 us (33.6 MB
 // of weight at 3.6 TB/s, launch included); 1,021 x 1,237 -> 777 f16 with its copies 16.5, 24 with 128 x 128.
+template <int MT, int WAVES, bool DIRECT>
+constexpr int kApartBytes = WAVES * (DIRECT ? 2 : 1) * (16 * MT + 64) * 64 * 2;
 template <class T, bool PROWS, bool QROWS, int MT, int WAVES, bool DIRECT>
-__global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *part, int tm, int tn, int splits, int64_t k_part) {
+__device__ __forceinline__ void apart(const Product &a, float *part, int tm, int tn, int splits, int64_t k_part, int block, char *lds) {
     constexpr int BK = 64, BN = 64, NT = BN / 32, STAGES = DIRECT ? 2 : 1;
     typedef Tile<PROWS, false, 16 * MT, BK> PTile;
     typedef Tile<QROWS, true, BN, BK> QTile;
     typedef Loads<T, PTile, PROWS, 1, DIRECT> PLoads;
     typedef Loads<T, QTile, QROWS, 1, DIRECT> QLoads;
     constexpr int kStage = PTile::kBytes + QTile::kBytes, kLoads = PLoads::kCount + QLoads::kCount, kSums = 16 * MT * BN * 4;
-    static_assert(kSums <= STAGES * kStage, "room for the sums");
-    __shared__ __attribute__((aligned(1024))) char lds[WAVES * STAGES * kStage];
+    static_assert(kSums <= STAGES * kStage && WAVES * STAGES * kStage == kApartBytes<MT, WAVES, DIRECT>, "room");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lptr<char>)(lds), mine = lds0 + wave * (STAGES * kStage);
     // (few rows: what is read is the weight, a part of it by each workgroup alone)
-    const Place at = MT == 1 ? Place{0, (int)(blockIdx.x % tn), (int)(blockIdx.x / tn)} : place_of(blockIdx.x, tm, tn, splits);
+    const Place at = MT == 1 ? Place{0, block % tn, block / tn} : place_of(block, tm, tn, splits);
     const int64_t m0 = (int64_t)at.m * (16 * MT), n0 = (int64_t)at.n * BN, s0 = at.split * k_part, s1 = s0 + k_part < a.k ? s0 + k_part : a.k;
     const int64_t each = ((s1 - s0 + WAVES * BK - 1) / (WAVES * BK)) * BK;
     const int64_t k0 = s0 + wave * each, k1 = k0 + each < s1 ? k0 + each : s1;
@@ -559,6 +563,22 @@ __global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *
     }
 }
 
+template <class T, bool PROWS, bool QROWS, int MT, int WAVES, bool DIRECT>
+__global__ void __launch_bounds__(64 * WAVES) k_product_apart(Product a, float *part, int tm, int tn, int splits, int64_t k_part) {
+    __shared__ __attribute__((aligned(1024))) char lds[kApartBytes<MT, WAVES, DIRECT>];
+    apart<T, PROWS, QROWS, MT, WAVES, DIRECT>(a, part, tm, tn, splits, k_part, blockIdx.x, lds);
+}
+
+// Both products of a layer's gradients, where neither fills the compute units: the gradient of the weight (a) by the first
+// workgroups, that of the rows (b) by those from `second` on, a multiple of eight (the XCDs).  256 rows of 256 x 256 bf16, with
+// db, 10 us, 14.5 in launches of their own; 1,021 of 777 x 1,237 30, 35.
+template <class T, bool QROWS>
+__global__ void __launch_bounds__(64 * kApart<true>) k_product_two(Product a, Product b, int atm, int atn, int btm, int btn, int second) {
+    __shared__ __attribute__((aligned(1024))) char lds[kApartBytes<4, kApart<true>, true>];
+    if ((int)blockIdx.x < atm * atn) apart<T, false, false, 4, kApart<true>, true>(a, nullptr, atm, atn, 1, (a.k + 63) / 64 * 64, blockIdx.x, lds);
+    else if ((int)blockIdx.x >= second) apart<T, true, QROWS, 4, kApart<true>, true>(b, nullptr, btm, btn, 1, (b.k + 63) / 64 * 64, blockIdx.x - second, lds);
+}
+
 template <class T, bool PROWS, bool QROWS, int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
 void run_product(const Product &a, const Plan &p, float *part, hipStream_t s) {
     const int tiles = p.tm * p.tn * p.splits, grid = tiles < PER_CU * kUnits ? tiles : PER_CU * kUnits;
@@ -574,6 +594,14 @@ void run_plan(const Product &a, const Plan &p, float *part, hipStream_t s) {
 }
 
 }  // namespace
+
+template <class T>
+void launch_two(const Product &a, const Product &b, hipStream_t s) {
+    const int atm = (int)((a.m + 63) / 64), atn = (int)((a.n + 63) / 64), btm = (int)((b.m + 63) / 64), btn = (int)((b.n + 63) / 64);
+    const int second = (atm * atn + 7) / 8 * 8;
+    if (b.q_by_rows) k_product_two<T, true><<<second + btm * btn, 64 * kApart<true>, 0, s>>>(a, b, atm, atn, btm, btn, second);
+    else k_product_two<T, false><<<second + btm * btn, 64 * kApart<true>, 0, s>>>(a, b, atm, atn, btm, btn, second);
+}
 
 template <class T, bool DIRECT>
 void launch_tiles(const Product &a, const Plan &p, float *part, hipStream_t s) {

@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(1024) k_column_sum_few(FewSums a) {
 // more.  So operands are copied first, rows padded with zeros to 16 bytes, if that is expected to take less than it
 // gains (4,099 x 1,237 -> 777 f16 29 us, of which the copies 8; 32 without.  A weight of
 // 15,219 x 3,471 bf16 is not copied for 139 rows: 45 us).  Sums over few rows are taken by workgroups of the same
-// launch (1,021 rows, 777 x 1,237 f16, all gradients: 35 us, 40 with a launch of their own).
+// launch (1,021 rows of 777 x 1,237 f16, all gradients: 5 us less than with a launch of their own).
 __global__ void __launch_bounds__(1024) k_pad_rows(PadRows x, PadRows y, PadRows z, FewSums sums) {
     __shared__ FewRoom lds;
     const int which = (int)blockIdx.y - (sums.cols ? 1 : 0);
@@ -173,7 +173,7 @@ bool pads(int64_t m, int64_t n, int64_t k) {
     return m % 8 || n % 8 || k % 8 || (double)(m + n) * (double)k * 2.0 <= (double)kMostCopied;
 }
 double copy_us(size_t bytes) { return (double)bytes * (2.0 / 4.5e6); }
-constexpr double kCopyLaunch = 2.5;
+constexpr double kLaunch = 2.5;
 size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
     auto most = [&](int64_t i) { return i * tiles_of(k, 8) > k * tiles_of(i, 8) ? i * tiles_of(k, 8) : k * tiles_of(i, 8); };
     return pads(m, n, k) ? (size_t)(most(m) + most(n)) * 16 : 0;
@@ -184,14 +184,19 @@ struct Way {
     bool copy_p, copy_q, direct;
     Plan plan;
 };
+double apart_us(int64_t k) { return (double)tiles_of(tiles_of(k, 64), kApart<true>) * 0.75 + 3.0; }
 Way way_of(const Product &a) {
     const bool ap = aligned_operand(a.p, a.p_stride, a.p_by_rows, a.m, a.k, a.padded & 1);
     const bool aq = aligned_operand(a.q, a.q_stride, a.q_by_rows, a.n, a.k, a.padded & 2);
-    const Plan direct = plan_of(a.m, a.n, a.k, a.p_by_rows, true);
+    Plan direct = plan_of(a.m, a.n, a.k, a.p_by_rows, true);
+    if (a.small) {
+        const int64_t tm = tiles_of(a.m, 64), tn = tiles_of(a.n, 64);
+        direct = Plan{64, (int)tm, (int)tn, 1, tiles_of(a.k, 64) * 64, (double)tiles_of(tm * tn, kUnits) * apart_us(a.k)};
+    }
     if ((ap && aq) || a.k == 0) return Way{false, false, true, direct};     // (no sums: nothing is loaded)
     const Plan any = plan_of(a.m, a.n, a.k, a.p_by_rows, false);
     const size_t bytes = (size_t)((ap ? 0 : a.m) + (aq ? 0 : a.n)) * (size_t)a.k * 2;
-    if (pads(a.m, a.n, a.k) && direct.us + kCopyLaunch + copy_us(bytes) < any.us) return Way{!ap, !aq, true, direct};
+    if (pads(a.m, a.n, a.k) && direct.us + kLaunch + copy_us(bytes) < any.us) return Way{!ap, !aq, true, direct};
     return Way{false, false, false, any};
 }
 size_t up16(size_t x) { return (x + 15) / 16 * 16; }
@@ -338,10 +343,10 @@ GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool turned, const Gr
     };
     const size_t dy = (size_t)rows * (size_t)n * 2, x = needed.x ? (size_t)rows * (size_t)k * 2 : 0, w = needed.w ? (size_t)k * (size_t)n * 2 : 0;
     auto alone = [&](bool of_dw, size_t bytes) {
-        const double any = us(of_dw, false), copied = us(of_dw, true) + kCopyLaunch + copy_us(bytes);
+        const double any = us(of_dw, false), copied = us(of_dw, true) + kLaunch + copy_us(bytes);
         return any < copied ? any : copied;
     };
-    const double apart = alone(true, dy + x) + alone(false, dy + w), both = us(true, true) + kCopyLaunch + copy_us(dy + x);
+    const double apart = alone(true, dy + x) + alone(false, dy + w), both = us(true, true) + kLaunch + copy_us(dy + x);
     const double with_w = both + copy_us(w) + us(false, true), without = both + us(false, !needed.w);
     if (apart <= with_w && apart <= without) return GradCopies{};
     return GradCopies{true, needed.x, needed.w && with_w < without};
@@ -385,6 +390,23 @@ bool product_fits(int64_t m, int64_t n, int64_t k, bool p_rows) {
         if ((int64_t)p.tm * p.tn * p.splits >= (int64_t(1) << 30)) return false;
     }
     return true;
+}
+
+// (the longer of the two decides how long a round of workgroups takes, and a launch is saved)
+bool small_gradients(int64_t rows, int64_t k, int64_t n, bool turned) {
+    const int64_t wr = turned ? n : k, wc = turned ? k : n, tiles = tiles_of(wr, 64) * tiles_of(wc, 64) + tiles_of(rows, 64) * tiles_of(k, 64);
+    return tiles < 4 * kUnits && (double)tiles_of(tiles, kUnits) * apart_us(rows > n ? rows : n) < plan_of(wr, wc, rows, false, true).us + plan_of(rows, k, n, true, true).us + kLaunch;
+}
+
+bool goes_together(const Product &dw, const Product &dx) {
+    const Way w = way_of(dw), x = way_of(dx);
+    return dw.small && dx.small && w.direct && x.direct && !w.copy_p && !w.copy_q && !x.copy_p && !x.copy_q;
+}
+
+hipError_t launch_together(const Product &dw, const Product &dx, hipStream_t s) {
+    if (dw.type == DD_BF16) launch_two<bf16_t>(dw, dx, s);
+    else launch_two<f16_t>(dw, dx, s);
+    return hipGetLastError();
 }
 
 hipError_t launch_product(const Product &p, void *work, hipStream_t s) {

@@ -12,6 +12,9 @@ namespace dd {
 size_t product_work(int64_t m, int64_t n, int64_t k, bool) { return k > 1000 ? (size_t)m * (size_t)n * 8 : 0; }
 bool product_fits(int64_t m, int64_t n, int64_t, bool) { return m < (1 << 30) && n < (1 << 30); }
 hipError_t launch_product(const Product &, void *, hipStream_t) { STUB; }
+bool goes_together(const Product &dw, const Product &) { return dw.m < 64; }
+hipError_t launch_together(const Product &, const Product &, hipStream_t) { STUB; }
+bool small_gradients(int64_t rows, int64_t, int64_t, bool) { return rows < 64; }
 size_t padded_size(int64_t rows, int64_t cols) { return (size_t)rows * (size_t)cols * 2; }
 size_t pad_rows(const void *&, int64_t &, int64_t rows, int64_t cols, void *, PadRows *r) {
     *r = PadRows{};
