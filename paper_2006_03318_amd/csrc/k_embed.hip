@@ -185,9 +185,10 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_sort(dd_embed_grad_args
 }
 
 // More: a workgroup has kSortBlock places in a row and a wave a run of them, so ranks count waves, then lanes.
-// Bound: latency; 65,536 tokens take 5 to 6 us to count and 7 to 9 to place, a pass.
-constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64, kSortEach = 8, kSortBlock = kSortThreads * kSortEach;
-static_assert(kSortThreads == kDigits, "a thread has a digit");
+// Bound: latency; 65,536 tokens take 5 us to count and 7 to place, a pass (16 waves with two keys a lane; four with
+// eight 6 and 8, and with one key and twice the workgroups 200,000 tokens take 15 us longer).
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortEach = 2, kSortBlock = kSortThreads * kSortEach;
+static_assert(kSortThreads >= kDigits, "a thread has a digit");
 
 // A workgroup's places with each digit lie digit by digit (those to be summed by a scan) or workgroup by
 // workgroup (which threads of a digit each read side by side).
@@ -204,7 +205,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args
         return;
     }
     __shared__ uint32_t n[kDigits];
-    n[threadIdx.x] = 0;
+    if (threadIdx.x < kDigits) n[threadIdx.x] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * kSortBlock;
     uint32_t key[kSortEach];
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_count(dd_embed_grad_args
     for (int i = 0; i < kSortEach; i++)
         if (first + i * kSortThreads + threadIdx.x < a.tokens) atomicAdd(&n[key[i] >> shift & (kDigits - 1)], 1u);
     __syncthreads();
-    counts[count_at(threadIdx.x, blockIdx.x, blocks)] = n[threadIdx.x];
+    if (threadIdx.x < kDigits) counts[count_at(threadIdx.x, blockIdx.x, blocks)] = n[threadIdx.x];
 }
 
 // Where there are too many workgroups for each to sum the others' counts: a workgroup has a digit, makes running sums of its
@@ -259,23 +260,25 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
         place[i] = !in ? 0 : FIRST ? (uint32_t)t : from.place[t];
     }
     // this thread's digit: places of earlier digits, and of earlier workgroups
-    uint32_t at = 0;
-    if (blocks > kManyBlocks) {
-        at = digits_before(counts[(int64_t)kDigits * blocks + threadIdx.x], room) + counts[count_at(threadIdx.x, blockIdx.x, blocks)];
-    } else {
-        uint32_t all = 0, mine = 0;
-        for (int b = 0; b < blocks; b += 8) {
-            uint32_t x[8];
+    uint32_t all = 0, mine = 0;
+    if (threadIdx.x < kDigits) {
+        if (blocks > kManyBlocks) {
+            all = counts[(int64_t)kDigits * blocks + threadIdx.x];
+            mine = counts[count_at(threadIdx.x, blockIdx.x, blocks)];
+        } else {
+            for (int b = 0; b < blocks; b += 16) {
+                uint32_t x[16];
 #pragma unroll
-            for (int u = 0; u < 8; u++) x[u] = b + u < blocks ? counts[count_at(threadIdx.x, b + u, blocks)] : 0;
+                for (int u = 0; u < 16; u++) x[u] = b + u < blocks ? counts[count_at(threadIdx.x, b + u, blocks)] : 0;
 #pragma unroll
-            for (int u = 0; u < 8; u++) {
-                all += x[u];
-                mine += b + u < (int)blockIdx.x ? x[u] : 0;
+                for (int u = 0; u < 16; u++) {
+                    all += x[u];
+                    mine += b + u < (int)blockIdx.x ? x[u] : 0;
+                }
             }
         }
-        at = digits_before(all, room) + mine;
     }
+    uint32_t at = digits_before(all, room) + mine;
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < kSortEach; i++) {
@@ -289,12 +292,13 @@ __global__ void __launch_bounds__(kSortThreads) k_embed_scatter(dd_embed_grad_ar
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
+    if (threadIdx.x < kDigits)
 #pragma unroll
-    for (int w = 0; w < kSortWaves; w++) {
-        const uint32_t x = next[w][threadIdx.x];
-        next[w][threadIdx.x] = at;
-        at += x;
-    }
+        for (int w = 0; w < kSortWaves; w++) {
+            const uint32_t x = next[w][threadIdx.x];
+            next[w][threadIdx.x] = at;
+            at += x;
+        }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSortEach; i++) {
