@@ -80,10 +80,13 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, bool p_rows, bool direct) {
 size_t plan_work(const Plan &p, int64_t m, int64_t n) { return p.splits > 1 ? (size_t)p.splits * (size_t)m * (size_t)n * sizeof(float) : 0; }
 
 // An operand that loads go to LDS directly from: 16 bytes in a row lie aligned, all of
-// one row (or one l), and a tile spans less than 2 GiB.
+// one row (or one l), and a tile spans less than 2 GiB, the reach of a load's offset.
+constexpr int64_t kReach = int64_t(1) << 22;        // of strides, in elements
 bool aligned_operand(const void *p, int64_t stride, bool by_rows, int64_t count, int64_t k, bool padded) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (padded || (by_rows ? k : count) % 8 == 0) && stride < (int64_t(1) << 22);
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && (padded || (by_rows ? k : count) % 8 == 0) && stride < kReach;
 }
+// so is a copy, of rows of that length
+bool copy_reaches(int64_t cols) { return tiles_of(cols, 8) * 8 < kReach; }
 
 // --- sums over few rows -----------------------------------------------------------
 __device__ __forceinline__ void store_as(void *p, int32_t type, int64_t i, float x) {
@@ -176,7 +179,10 @@ bool pads(int64_t m, int64_t n, int64_t k) {
 double copy_us(size_t bytes) { return (double)bytes * (2.0 / 4.5e6); }
 constexpr double kLaunch = 2.5;
 size_t pad_work(int64_t m, int64_t n, int64_t k) {       // (of either layout)
-    auto most = [&](int64_t i) { return i * tiles_of(k, 8) > k * tiles_of(i, 8) ? i * tiles_of(k, 8) : k * tiles_of(i, 8); };
+    auto most = [&](int64_t i) {
+        const int64_t by_rows = copy_reaches(k) ? i * tiles_of(k, 8) : 0, by_sums = copy_reaches(i) ? k * tiles_of(i, 8) : 0;
+        return by_rows > by_sums ? by_rows : by_sums;
+    };
     return pads(m, n, k) ? (size_t)(most(m) + most(n)) * 16 : 0;
 }
 
@@ -197,7 +203,8 @@ Way way_of(const Product &a) {
     if ((ap && aq) || a.k == 0) return Way{false, false, true, direct};     // (no sums: nothing is loaded)
     const Plan any = plan_of(a.m, a.n, a.k, a.p_by_rows, false);
     const size_t bytes = (size_t)((ap ? 0 : a.m) + (aq ? 0 : a.n)) * (size_t)a.k * 2;
-    if (pads(a.m, a.n, a.k) && direct.us + kLaunch + copy_us(bytes) < any.us) return Way{!ap, !aq, true, direct};
+    const bool reach = (ap || copy_reaches(a.p_by_rows ? a.k : a.m)) && (aq || copy_reaches(a.q_by_rows ? a.k : a.n));
+    if (reach && pads(a.m, a.n, a.k) && direct.us + kLaunch + copy_us(bytes) < any.us) return Way{!ap, !aq, true, direct};
     return Way{false, false, false, any};
 }
 size_t up16(size_t x) { return (x + 15) / 16 * 16; }
@@ -339,6 +346,7 @@ bool loads_directly(const void *p, int64_t stride, bool by_rows, int64_t count, 
 
 GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool turned, const GradCopies &needed) {
     if (!needed.dy || !grad_copies_work(rows, k, n)) return GradCopies{};
+    if ((needed.x && !copy_reaches(k)) || (needed.w && !copy_reaches(turned ? k : n))) return GradCopies{};
     auto us = [&](bool of_dw, bool direct) {
         return of_dw ? plan_of(turned ? n : k, turned ? k : n, rows, false, direct).us : plan_of(rows, k, n, true, direct).us;
     };
@@ -354,7 +362,7 @@ GradCopies grad_copies(int64_t rows, int64_t k, int64_t n, bool turned, const Gr
 }
 
 size_t grad_copies_work(int64_t rows, int64_t k, int64_t n) {
-    if (rows <= 64 || k <= 64 || n <= 64) return 0;
+    if (rows <= 64 || k <= 64 || n <= 64 || !copy_reaches(n)) return 0;
     const size_t w = padded_size(k, n), turned = padded_size(n, k), all = padded_size(rows, n) + padded_size(rows, k) + (w > turned ? w : turned);
     return n % 8 || all <= (size_t)kMostCopied ? all : 0;
 }
