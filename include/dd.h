@@ -497,6 +497,9 @@ size_t dd_rms_norm_grad_work(int64_t rows, int64_t cols);
 #define DD_ACT_GELU 2        /* z Phi(z) */
 #define DD_ACT_GELU_TANH 3   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
 #define DD_ACT_SILU 4        /* z / (1 + exp(-z)) */
+/* At infinities the derivatives are their limits, 0 or 1: a z of 16 bits is infinite where the
+ * sum lies beyond its range.  DD_ACT_GELU of -infinity (of a sum in 32 bits) is 0 too, DD_ACT_GELU_TANH
+ * and DD_ACT_SILU of it are NaN. */
 
 /*
  * dd_linear -- for rows x [rows][k] and a weight w of k by n, summed in 32 bits:

@@ -34,13 +34,16 @@ __device__ __forceinline__ float act_of(float z) {
     if (ACT == DD_ACT_SILU) return z * sigmoid(z);
     return z;
 }
+// z where its factor is 0 from far below 200 on: that of an infinity stays 0 (a NaN's factor is one itself)
+__device__ __forceinline__ float reined(float z) { return __builtin_amdgcn_fmed3f(z, -200.0f, 200.0f); }
+// The derivative; at infinities, which a z of 16 bits holds for sums beyond its range, its limit.
 template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
     if (ACT == DD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     if (ACT == DD_ACT_GELU) {
         float below, e;
         normal(z, below, e);
-        return fmaf(z * e, 0.3989422804f, z < 0.0f ? below : 1.0f - below);
+        return fmaf(reined(z) * e, 0.3989422804f, z < 0.0f ? below : 1.0f - below);
     }
     if (ACT == DD_ACT_GELU_TANH) {
         const float x = z > 20.0f ? 20.0f : z < -20.0f ? -20.0f : z;     // (x^2 in range; the slope is 0 or 1 there)
@@ -49,7 +52,7 @@ __device__ __forceinline__ float slope_of(float z) {
     }
     if (ACT == DD_ACT_SILU) {
         const float s = sigmoid(z);
-        return s * fmaf(z, 1.0f - s, 1.0f);
+        return s * fmaf(reined(z), 1.0f - s, 1.0f);
     }
     return 1.0f;
 }
