@@ -120,13 +120,15 @@ def _linear_grad(dy, x, weight, bias, wanted, in_act="none", in_z=None):
     return dx, dw, db
 
 
+# (What an activation takes is kept for the gradient alone.  Inside forward gradients are always off, and
+# needs_input_grad tells of the inputs, so whether they are on is an argument.)
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, act):
+    def forward(ctx, x, weight, bias, residual, act, grad):
         x = _rows(x)
         ctx.act = act
         y, z = _linear(x, weight, bias, None if residual is None else _rows(residual), act,
-                       act != "none" and any(ctx.needs_input_grad[:3]))
+                       grad and act != "none" and any(ctx.needs_input_grad[:3]))
         ctx.save_for_backward(x, weight, bias, z)
         return y
 
@@ -139,7 +141,7 @@ class _Linear(torch.autograd.Function):
             dz = torch.empty_like(z)
             with _on(dy, z):
                 B.dd_act_grad(dy, z, dz, ctx.act, stream=_stream())
-        return (*_linear_grad(dz, x, weight, bias, ctx.needs_input_grad[:3]), dy if ctx.needs_input_grad[3] else None, None)
+        return (*_linear_grad(dz, x, weight, bias, ctx.needs_input_grad[:3]), dy if ctx.needs_input_grad[3] else None, None, None)
 
 
 def linear(x, weight, bias=None, act="none", residual=None):
@@ -151,15 +153,16 @@ def linear(x, weight, bias=None, act="none", residual=None):
     weight = _matrix(weight)
     if residual is not None:
         residual = residual.expand(x.shape[:-1] + weight.shape[1:])
-    return _Linear.apply(x, weight, bias, residual, act)
+    return _Linear.apply(x, weight, bias, residual, act, torch.is_grad_enabled())
 
 
 class _Mlp(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, up, down, bias_up, bias_down, residual, act):
+    def forward(ctx, x, up, down, bias_up, bias_down, residual, act, grad):
         x = _rows(x)
         ctx.act = act
-        a, z = _linear(x, up, bias_up, None, act, act != "none" and any(ctx.needs_input_grad[:5]))
+        need = ctx.needs_input_grad
+        a, z = _linear(x, up, bias_up, None, act, grad and act != "none" and (need[0] or need[1] or need[3]))
         y, _ = _linear(a, down, bias_down, None if residual is None else _rows(residual), "none", False)
         ctx.save_for_backward(x, up, down, bias_up, bias_down, z, a)
         return y
@@ -175,7 +178,7 @@ class _Mlp(torch.autograd.Function):
         dx = dup = dbias_up = None
         if first:
             dx, dup, dbias_up = _linear_grad(dz, x, up, bias_up, (need[0], need[1], need[3]))
-        return dx, dup, ddown, dbias_up, dbias_down, dy if need[5] else None, None
+        return dx, dup, ddown, dbias_up, dbias_down, dy if need[5] else None, None, None
 
 
 def mlp(x, up, down, bias_up=None, bias_down=None, act="gelu", residual=None):
@@ -186,7 +189,7 @@ def mlp(x, up, down, bias_up=None, bias_down=None, act="gelu", residual=None):
     up, down = _matrix(up), _matrix(down)
     if residual is not None:
         residual = residual.expand(x.shape[:-1] + down.shape[1:])
-    return _Mlp.apply(x, up, down, bias_up, bias_down, residual, act)
+    return _Mlp.apply(x, up, down, bias_up, bias_down, residual, act, torch.is_grad_enabled())
 
 
 class _Dropout(torch.autograd.Function):
