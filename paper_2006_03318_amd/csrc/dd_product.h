@@ -157,13 +157,24 @@ struct Loads {
         }
     }
     __device__ __forceinline__ uint64_t from(int64_t l0) const { return (uint64_t)(uintptr_t)(base + (ROWS ? l0 : l0 * stride)); }
-    // load j of the tile that begins at `from`, to LDS at `to`
+    __device__ __forceinline__ i4 buffer_at(uint64_t from) const {
+        return {__builtin_amdgcn_readfirstlane((int)(uint32_t)from), __builtin_amdgcn_readfirstlane((int)(uint32_t)(from >> 32)), (int)0x80000000u, 0x00020000};
+    }
+    // load j of the tile that begins at `from`, to LDS at `to`.  m0 is the place in LDS.  The text waits by itself, as the compiler does
+    // not look into it: one state between m0 and the load, and five between a vector instruction that wrote a scalar
+    // operand and the load.
     __device__ __forceinline__ void direct(uint64_t from, uint32_t to, int j) const {
-        const i4 buffer = {__builtin_amdgcn_readfirstlane((int)(uint32_t)from), __builtin_amdgcn_readfirstlane((int)(uint32_t)(from >> 32)),
-                           (int)0x80000000u, 0x00020000};
-        // (m0 is the place in LDS, which nothing else here uses; one wait state before the load that does)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
-                     "v"(off[j]), "s"(buffer));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
+                     "v"(off[j]), "s"(buffer_at(from)) : "m0");
+    }
+    // all of them, by a wave alone; two in turn share the longer wait
+    __device__ __forceinline__ void direct(uint64_t from, uint32_t to) const {
+        static_assert(WAVES == 1 && kCount % 2 == 0, "pairs");
+#pragma unroll
+        for (int j = 0; j < kCount; j += 2)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds" ::"s"(to + j * 1024), "s"(to + (j + 1) * 1024),
+                         "v"(off[j]), "v"(off[j + 1]), "s"(buffer_at(from)) : "m0");
     }
     // whether a step of `full` sums, of those `left`, is loaded without a look at what is there
     __device__ __forceinline__ bool quick(int64_t left, int full) const {
@@ -486,10 +497,8 @@ __device__ __forceinline__ void apart(const Product &a, float *part, int tm, int
             }
             const uint32_t to = mine + (t & 1) * kStage;
             const uint64_t fp = lp.from(l0), fq = lq.from(l0);
-#pragma unroll
-            for (int j = 0; j < QLoads::kCount; j++) lq.direct(fq, to + PTile::kBytes, j);
-#pragma unroll
-            for (int j = 0; j < PLoads::kCount; j++) lp.direct(fp, to, j);
+            lq.direct(fq, to + PTile::kBytes);
+            lp.direct(fp, to);
         } else {
             load_step(lp, lq, l0, left, BK);
         }
