@@ -64,6 +64,25 @@ bool overlap(const void *x, int64_t x_stride, const void *y, int64_t y_stride, i
 
 bool sizes_known(int64_t rows, int64_t k, int64_t n) { return rows >= 0 && k >= 1 && n >= 1 && rows < kMost && k < kMost && n < kMost; }
 
+// Bytes of a gradient whose products share the copies of their operands: those copies, and behind them what the
+// products and the sums over rows need then, whose operands load directly but for w, which dx may read as it is.
+// (Tiles and parts of dw are those of its transpose.)
+size_t shared_work(int64_t rows, int64_t k, int64_t n) {
+    if (!dd::grad_copies_work(rows, k, n)) return 0;
+    auto longer = [](size_t x, size_t y) { return x > y ? x : y; };
+    auto padded = [](int64_t x) { return (x + 7) / 8 * 8; };
+    const char *at = reinterpret_cast<const char *>(uintptr_t(16));
+    const int32_t small = dd::small_gradients(rows, k, n, false);
+    const dd::Product dw{at, at, k, n, rows, padded(k), padded(n), 0, 0, DD_BF16, 3, small, {}};
+    dd::Product dx{at, at, rows, k, n, padded(n), padded(n), 1, 1, DD_BF16, 3, small, {}};
+    const size_t behind = longer(longer(dd::product_need(dw), dd::product_need(dx)), dd::column_sum_work(rows, n));
+    dx.q = at + 2;
+    const size_t by_rows = dd::product_need(dx);
+    dx.q_by_rows = 0;
+    const size_t by_sums = dd::product_need(dx), with_w = longer(dd::padded_size(k, n), dd::padded_size(n, k)) + behind;
+    return dd::padded_size(rows, n) + dd::padded_size(rows, k) + longer(with_w, longer(by_rows, by_sums));
+}
+
 dd_status check_table(int64_t tokens, int64_t vocab, int64_t cols, int32_t type, const void *ids, int32_t id_bytes, float scale, int32_t reserved) {
     if (tokens < 0 || vocab < 1 || cols < 1) return fail(DD_EINVAL, "tokens must be at least 0, vocab and cols at least 1");
     if (tokens >= (int64_t(1) << 28) || vocab >= kMost || cols >= kMost)
@@ -112,9 +131,11 @@ dd_status dd_linear(const dd_linear_args *a, void *stream) {
 
 size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
     if (!sizes_known(rows, k, n)) return 0;
+    // each product by itself, or both with copies that they share: never the copies of either
     size_t most = dd::column_sum_work(rows, n);
     for (size_t x : {rows > 0 ? dd::product_work(rows, k, n, true) : 0, dd::product_work(k, n, rows, false), dd::product_work(n, k, rows, false)}) most = x > most ? x : most;
-    return most + (rows > 0 ? dd::grad_copies_work(rows, k, n) : 0);
+    const size_t shared = rows > 0 ? shared_work(rows, k, n) : 0;
+    return shared > most ? shared : most;
 }
 
 dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {

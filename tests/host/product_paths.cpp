@@ -124,8 +124,9 @@ struct Call {
     int turned, type, wanted;
 };
 
-static dd_status run(const Call &c) {
-    auto at = [](int i) { return reinterpret_cast<char *>((uintptr_t(1) << 52) + ((uintptr_t)i << 48)); };
+// odd: operand i lies 2 bytes further than 16 bytes divide, if its bit is set
+static dd_status run(const Call &c, unsigned odd = 0) {
+    auto at = [odd](int i) { return reinterpret_cast<char *>((uintptr_t(1) << 52) + ((uintptr_t)i << 48) + (odd >> i & 1 ? 2 : 0)); };
     const int64_t wr = c.turned ? c.n : c.k, wc = c.turned ? c.k : c.n;
     char line[200];
     snprintf(line, sizeof(line), "%s %lld %lld %lld pad %lld turned %d wanted %d:", c.grad ? "grad" : "fwd", c.rows, c.k, c.n, c.pad, c.turned, c.wanted);
@@ -190,7 +191,7 @@ int main(int argc, char **argv) {
             c.n = size(wide == 2 ? 30 : 14);
             c.pad = gen() % 3 == 0 ? (long long)(gen() % 20) : gen() % 5 == 0 ? 8 : 0;
             if (gen() % 3 == 0) c.rows = (c.rows + 7) / 8 * 8, c.k = (c.k + 7) / 8 * 8, c.n = (c.n + 7) / 8 * 8;
-            const dd_status st = run(c);
+            const dd_status st = run(c, gen() % 3 ? 0 : gen() % 8);
             EXPECT(st == DD_OK || st == DD_EINVAL);
             EXPECT(used <= room);
         }

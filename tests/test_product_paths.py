@@ -27,3 +27,22 @@ def test_reach_of_loads_and_room(program):
     memory is written within the bytes that the sizes ask for."""
     r = subprocess.run([program, "draw", "300000"], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "ALL OK" in r.stdout, r.stderr[:4000]
+
+
+def ask(program, calls):
+    """(status, bytes used, bytes asked for, what was launched) of each call."""
+    r = subprocess.run([program], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[:4000]
+    lines = [line.split(" ", 3) for line in r.stdout.splitlines()]
+    assert len(lines) == len(calls)
+    return [(int(a), int(b), int(c), d.split(": ", 1)[1] if ": " in d else "") for a, b, c, d in lines]
+
+
+@pytest.mark.parametrize("rows,k,n", [(65536, 4096, 50257), (16384, 2048, 50257), (8192, 1024, 1024), (4096, 1000, 1003)])
+def test_gradients_ask_for_no_more_than_they_use(program, rows, k, n):
+    """Copies that the two products share take the place of their own: of all strides and layouts one uses what the
+    sizes ask for, and that is little more than the operands."""
+    got = ask(program, [("grad", rows, k, n, pad, turned, 0, 7) for pad in (0, 1, 3, 8) for turned in (0, 1)])
+    asked = {g[2] for g in got}
+    assert len(asked) == 1 and max(g[1] for g in got) >= 0.95 * asked.pop()
+    assert got[0][2] <= 1.1 * 2 * (rows * n + rows * k + k * n)
