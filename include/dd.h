@@ -532,7 +532,8 @@ size_t dd_linear_work(int64_t rows, int64_t k, int64_t n);
  *   db = sum over rows of dy     in bias_type
  * dw and db of no rows are zeros.  dx may be in_z or x, element for element.
  * Sums over many rows are cut into parts whose sums are joined in order: the same
- * bits on every call.
+ * bits on every call that has these sizes, strides and alignments and wants the same.  (Copies
+ * of operands are shared where dx and dw are both wanted, and may change how sums are cut.)
  *   work holds these parts and copies of operands whose rows 16 bytes do not divide
  * (in dd_linear too).
  */

@@ -67,7 +67,8 @@ size_t product_need(const Product &p);      // of these operands: at most that
 bool product_fits(int64_t m, int64_t n, int64_t k, bool p_by_rows);      // one launch takes it
 hipError_t launch_product(const Product &p, void *work, hipStream_t s);
 // Whether the products of a layer's gradients take less in one launch, by their sizes (both are `small` then, which one
-// alone is too, for the same bits), and by their operands; that launch, without working memory.
+// alone is too: where operands load directly, its bits do not depend on whether the other is wanted), and by their
+// operands; that launch, without working memory.
 bool small_gradients(int64_t rows, int64_t k, int64_t n, bool turned);
 bool goes_together(const Product &dw, const Product &dx);
 hipError_t launch_together(const Product &dw, const Product &dx, hipStream_t s);

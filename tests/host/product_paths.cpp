@@ -4,7 +4,8 @@
 //   product_paths          reads calls, "fwd" or "grad", rows, k, n, pad (elements between rows), turned, type
 //                          (0: bf16, 1: f16), wanted (1 dx, 2 dw, 4 db), a line each; writes a line for each
 //   product_paths draw N   N drawn calls: what is loaded to LDS directly lies within the reach of a load's
-//                          offset, and all that is written to working memory within the bytes that are asked for
+//                          offset, all that is written to working memory within the bytes that are asked for, and a
+//                          gradient alone is cut as it is beside the others where operands load directly
 #include "k_linear.hip"
 
 #include <stdio.h>
@@ -42,6 +43,12 @@ static void uses(const void *p, size_t bytes) {
 static void check_reach(int64_t stride, bool by_rows, int64_t lines, int64_t width) {
     EXPECT(((lines - 1) * stride + (by_rows ? 64 : width)) * 2 <= int64_t(1) << 31);
 }
+// tile and parts of dx and dw, as launched last
+struct Cut {
+    int tile, splits;
+    bool operator==(const Cut &o) const { return tile == o.tile && splits == o.splits; }
+};
+static Cut cut_dx, cut_dw;
 static char operand(const void *p) {
     for (const void *g : given)
         if (p == g) return 'g';
@@ -51,6 +58,7 @@ static void say(const Product &a, const Plan &p, bool direct, const char *how) {
     char line[200];
     const char *what = a.e.out == y_at ? "y" : a.e.out == dx_at ? "dx" : "dw";
     const int64_t tiles = (int64_t)p.tm * p.tn * p.splits;
+    (a.e.out == dx_at ? cut_dx : cut_dw) = Cut{p.tile, p.splits};
     snprintf(line, sizeof(line), " %s:%d%s%s%s%c%c%s", what, p.tile, how, p.splits > 1 ? "/cut" : "", direct ? "/direct" : "/any", operand(a.p), operand(a.q),
              tiles > dd::kUnits ? "/rounds" : "");
     said += line;
@@ -182,6 +190,7 @@ static dd_status run(const Call &c, unsigned odd = 0) {
 int main(int argc, char **argv) {
     if (argc == 3 && !strcmp(argv[1], "draw")) {
         std::mt19937_64 gen(7);
+        int alike = 0;
         auto size = [&](double most) { return (long long)exp2(std::uniform_real_distribution<double>(0.0, most)(gen)); };
         for (int i = 0; i < atoi(argv[2]); i++) {
             Call c{gen() % 2 == 0, 0, 0, 0, 0, (int)(gen() % 2), (int)(gen() % 2), (int)(gen() % 8)};
@@ -194,7 +203,20 @@ int main(int argc, char **argv) {
             const dd_status st = run(c, gen() % 3 ? 0 : gen() % 8);
             EXPECT(st == DD_OK || st == DD_EINVAL);
             EXPECT(used <= room);
+            // operands that load directly: what is wanted alone has the tiles and parts that it has beside the other
+            if (!c.grad || st != DD_OK || c.k % 8 || c.n % 8 || c.pad % 8) continue;
+            c.wanted = 7;
+            run(c);
+            const Cut dx = cut_dx, dw = cut_dw;
+            c.wanted = 1;
+            run(c);
+            EXPECT(cut_dx == dx);
+            c.wanted = 2;
+            run(c);
+            EXPECT(cut_dw == dw);
+            alike++;
         }
+        EXPECT(alike > atoi(argv[2]) / 100);
         if (!bad) printf("ALL OK\n");
         return bad ? 1 : 0;
     }

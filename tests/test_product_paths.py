@@ -24,7 +24,8 @@ def program(tmp_path_factory):
 
 def test_reach_of_loads_and_room(program):
     """Whatever is loaded to LDS directly, copies among it, lies below 2 GiB from where its tile begins, and working
-    memory is written within the bytes that the sizes ask for."""
+    memory is written within the bytes that the sizes ask for.  A gradient wanted alone has the tiles and parts that it
+    has beside the other where operands load directly."""
     r = subprocess.run([program, "draw", "300000"], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "ALL OK" in r.stdout, r.stderr[:4000]
 
