@@ -1,10 +1,12 @@
 """Which kernels products and their gradients go to, on the CPU: the library's own checks, plan and working memory,
 with the launches written down."""
 import os
+import random
 import subprocess
 
 import pytest
 
+from tests.product_cases import CASES
 from tests.test_host_code import CLANGXX, CSRC, INC, ROOT
 
 HIPCC = "/opt/rocm/bin/hipcc"
@@ -47,3 +49,20 @@ def test_gradients_ask_for_no_more_than_they_use(program, rows, k, n):
     asked = {g[2] for g in got}
     assert len(asked) == 1 and max(g[1] for g in got) >= 0.95 * asked.pop()
     assert got[0][2] <= 1.1 * 2 * (rows * n + rows * k + k * n)
+
+
+def test_every_path_has_a_case(program):
+    """The cases that a GPU runs go where their list says, and no drawn call finds a path that none of them takes."""
+    got = ask(program, [(*c[:6], 0, 7) for c in CASES])
+    assert [g[0] for g in got] == [0] * len(CASES)
+    assert [(c[:6], g[3]) for c, g in zip(CASES, got)] == [(c[:6], c[6]) for c in CASES]
+    taken = {(part, c[5]) for c in CASES for part in c[6].split()}
+    rng = random.Random(5)
+
+    def size(most):
+        n = int(2 ** rng.uniform(0, most))
+        return n if rng.random() < 0.5 else (n + 7) // 8 * 8
+    calls = [(rng.choice(("fwd", "grad")), size(16), size(14), size(14), rng.choice((0, 0, 0, 8, 1, 3)), rng.randint(0, 1), rng.randint(0, 1), 7)
+             for _ in range(100000)]
+    new = {(part, c[5]): c for c, g in zip(calls, ask(program, calls)) if g[0] == 0 for part in g[3].split() if (part, c[5]) not in taken}
+    assert not new, new
