@@ -160,21 +160,14 @@ struct Loads {
     __device__ __forceinline__ i4 buffer_at(uint64_t from) const {
         return {__builtin_amdgcn_readfirstlane((int)(uint32_t)from), __builtin_amdgcn_readfirstlane((int)(uint32_t)(from >> 32)), (int)0x80000000u, 0x00020000};
     }
-    // load j of the tile that begins at `from`, to LDS at `to`.  m0 is the place in LDS.  The text waits by itself, as the compiler does
-    // not look into it: one state between m0 and the load, and five between a vector instruction that wrote a scalar
-    // operand and the load.
+    // loads j and j + 1 of the tile that begins at `from`, to LDS at `to`.  m0 is the place in LDS.  The text waits by itself, as
+    // the compiler does not look into it: one state between m0 and a load, and five between a vector instruction that
+    // wrote a scalar operand and the load.
     __device__ __forceinline__ void direct(uint64_t from, uint32_t to, int j) const {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
-                     "v"(off[j]), "s"(buffer_at(from)) : "m0");
-    }
-    // all of them, by a wave alone; two in turn share the longer wait
-    __device__ __forceinline__ void direct(uint64_t from, uint32_t to) const {
-        static_assert(WAVES == 1 && kCount % 2 == 0, "pairs");
-#pragma unroll
-        for (int j = 0; j < kCount; j += 2)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
-                         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds" ::"s"(to + j * 1024), "s"(to + (j + 1) * 1024),
-                         "v"(off[j]), "v"(off[j + 1]), "s"(buffer_at(from)) : "m0");
+        static_assert(kCount % 2 == 0, "pairs");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+                     "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %4, 0 offen lds" ::"s"(to + number(wave, j) * 1024),
+                     "s"(to + number(wave, j + 1) * 1024), "v"(off[j]), "v"(off[j + 1]), "s"(buffer_at(from)) : "m0");
     }
     // whether a step of `full` sums, of those `left`, is loaded without a look at what is there
     __device__ __forceinline__ bool quick(int64_t left, int full) const {
@@ -322,7 +315,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PER_CU * WM * WN / 4)
     // the loads that go with chunk i of n
     auto issue = [&](uint32_t to, int i, int n) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kLoads; j++)
+        for (int j = 0; j < kLoads; j += 2)
             if (j * n / kLoads == i) {
                 if (j < PLoads::kCount) lp.direct(from_p, lds0 + to, j);
                 else lq.direct(from_q, lds0 + to + PTile::kBytes, j - PLoads::kCount);
@@ -497,8 +490,10 @@ __device__ __forceinline__ void apart(const Product &a, float *part, int tm, int
             }
             const uint32_t to = mine + (t & 1) * kStage;
             const uint64_t fp = lp.from(l0), fq = lq.from(l0);
-            lq.direct(fq, to + PTile::kBytes);
-            lp.direct(fp, to);
+#pragma unroll
+            for (int j = 0; j < QLoads::kCount; j += 2) lq.direct(fq, to + PTile::kBytes, j);
+#pragma unroll
+            for (int j = 0; j < PLoads::kCount; j += 2) lp.direct(fp, to, j);
         } else {
             load_step(lp, lq, l0, left, BK);
         }
