@@ -11,7 +11,7 @@ namespace dd {
 // --- activations --------------------------------------------------------------
 // Phi(-|x|) and exp(-x^2 / 2), from Abramowitz and Stegun 7.1.26 (off by 1.5e-7
 // at most).  Few instructions count: each takes 3.4 us of 16,384 x 2,048 -> 8,192, where
-// the matrix units wait: GELU 513 us, SiLU 485, none 475.
+// the matrix units wait: GELU 510 us, SiLU 479, none 477.
 __device__ __forceinline__ void normal(float x, float &below, float &e) {
     const float u = x * 0.84932180f;        // sqrt(log2(e) / 2)
     const float t = __builtin_amdgcn_rcpf(fmaf(0.27273748f, fabsf(u), 1.0f));       // 0.3275911 |x| / sqrt(2)
@@ -36,7 +36,8 @@ __device__ __forceinline__ float act_of(float z) {
 }
 // z where its factor is 0 from far below 200 on: that of an infinity stays 0 (a NaN's factor is one itself)
 __device__ __forceinline__ float reined(float z) { return __builtin_amdgcn_fmed3f(z, -200.0f, 200.0f); }
-// The derivative; at infinities, which a z of 16 bits holds for sums beyond its range, its limit.
+// The derivative; at infinities, which a z of 16 bits holds for sums beyond its range, its limit.  dx of 16,384 x 2,048 ->
+// 8,192 bf16 through GELU 529 us, SiLU 512, none 458.
 template <int ACT>
 __device__ __forceinline__ float slope_of(float z) {
     if (ACT == DD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;

@@ -230,7 +230,7 @@ __device__ __forceinline__ Place place_of(int b, int tm, int tn, int splits) {
 // next one's loads are under way and the stores of the last go out.
 //   Bound: the matrix instructions, fed by a barrier a step.  256 x 256 tiles (two stages of 64 KB) use each element
 // from L2 256 times: 8,192^3 bf16 in 770 to 790 us (1.4 PFLOP/s);
-// 65,536 x 8,192 -> 2,048 into a residual 1,700; 16,384 x 2,048 -> 8,192 475, 530 to 550 with bias, GELU and both
+// 65,536 x 8,192 -> 2,048 into a residual 1,700 to 1,725; 16,384 x 2,048 -> 8,192 477, 530 to 555 with bias, GELU and both
 // outputs.  128 x 128 (four stages of 32 KB) where 256 x 256 would leave compute units without a tile: 4,096 x 1,280 ->
 // 768 in 17.  Fewer or more stages, deeper prefetch in the epilogue, and tiles by 32 sums were slower.
 template <class T, bool PROWS, bool QROWS, int BM, int BN, int WM, int WN, int STAGES, int PER_CU, bool DIRECT>
