@@ -490,7 +490,10 @@ size_t dd_rms_norm_grad_work(int64_t rows, int64_t cols);
  *            aligned to 16, which the call overwrites, or NULL: the library
  *            takes it from its cache for the time of the call.  A call that
  *            needs some and is captured into a graph has to bring it
- *            (DD_EINVAL): the replays write there too.
+ *            (DD_EINVAL): the replays write there too.  That size goes by the sizes
+ *            alone; where there is a function that ends in _need, it gives what a call
+ *            with these strides and addresses uses (work itself is not looked at; 0 if the
+ *            call would be refused), which for aligned operands is less.
  */
 #define DD_ACT_NONE 0
 #define DD_ACT_RELU 1
@@ -522,6 +525,7 @@ typedef struct {
 } dd_linear_args;
 dd_status dd_linear(const dd_linear_args *a, void *stream);
 size_t dd_linear_work(int64_t rows, int64_t k, int64_t n);
+size_t dd_linear_need(const dd_linear_args *a);
 
 /*
  * dd_linear_grad -- from the gradient dy [rows][n] of x w + bias (with an
@@ -550,6 +554,7 @@ typedef struct {
 } dd_linear_grad_args;
 dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream);
 size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n);
+size_t dd_linear_grad_need(const dd_linear_grad_args *a);
 
 /*
  * dd_act_grad -- dz = dy * act'(z), element by element.  dz may be dy or z.

@@ -89,6 +89,7 @@ def lib():
             "dd_linear", "dd_linear_grad", "dd_act_grad", "dd_dropout", "dd_embed", "dd_embed_grad")},
         **{name: (ctypes.c_size_t, [_i64, _i64, _i64]) for name in (
             "dd_linear_work", "dd_linear_grad_work", "dd_embed_grad_work")},
+        **{name: (ctypes.c_size_t, [ctypes.c_char_p]) for name in ("dd_linear_need", "dd_linear_grad_need")},
         "dd_graph_free": (None, [_vp]),
         "dd_sched_free": (None, [_vp]),
         "dd_variants_free": (None, [_vp]),
@@ -517,10 +518,23 @@ def _bias(name, t, n, kind):
     return _gpu(name, t, n, bk), bk
 
 
+def _given(work, need, record, head, tail, size):
+    """(address, tensor) of a caller's working memory: a tensor of size bytes, or a function that gives
+    one of the bytes that `need` tells of the call (head and tail: its arguments before and behind the address)."""
+    if not callable(work):
+        return _work(work, size(*head[:3])), work
+    bytes_ = need(record.pack(*head, 0, *tail))
+    if not bytes_:
+        return 0, None
+    work = work(bytes_)
+    return _work(work, bytes_), work
+
+
 def dd_linear(x, w, y, bias=None, residual=None, act="none", z=None, work=None, stream=None):
     """y = act(x w + bias) + residual, for x [..., k] and w [k, n] in bfloat16 or float16;
     w by rows, or by columns (the transpose of an [n, k] weight).  z receives x w + bias.
-    work: uint8 of dd_linear_work(rows, k, n), or None (from the library's cache; not
+    work: uint8 of dd_linear_work(rows, k, n), a function that is called with the bytes that
+    this call uses, if any, and gives them, or None (from the library's cache; not
     under graph capture if it is not 0)."""
     kind, shape, dt = _half("x", x), x.shape, x.dtype
     k = shape[-1]
@@ -534,9 +548,10 @@ def dd_linear(x, w, y, bias=None, residual=None, act="none", z=None, work=None, 
     pr, sr = _rows("residual", residual, out, n, dt)
     py, sy = _rows("y", y, out, n, dt)
     pz, sz = _rows("z", z, out, n, dt)
-    args = _LINEAR.pack(rows, k, n, sx, sw, sr, sy, sz, px, pw, pb, pr, py, pz,
-                        0 if work is None else _work(work, dd_linear_work(rows, k, n)), kind, bk, _act(act), turned)
-    rc = (_lib or lib()).dd_linear(args, None if stream is None else _stream(stream))
+    head, tail, at = (rows, k, n, sx, sw, sr, sy, sz, px, pw, pb, pr, py, pz), (kind, bk, _act(act), turned), 0
+    if work is not None:
+        at, work = _given(work, lib().dd_linear_need, _LINEAR, head, tail, dd_linear_work)
+    rc = (_lib or lib()).dd_linear(_LINEAR.pack(*head, at, *tail), None if stream is None else _stream(stream))
     if rc:
         _check(rc)
 
@@ -548,7 +563,7 @@ def dd_linear_work(rows: int, k: int, n: int) -> int:
 def dd_linear_grad(dy, x=None, w=None, dx=None, dw=None, db=None, in_act="none", in_z=None, work=None, stream=None):
     """dx = (dy w^T) * in_act'(in_z), dw = x^T dy (by rows or by columns) and db = the sum of
     dy's rows, each if it is given; dx needs w, dw needs x.  work: uint8 of
-    dd_linear_grad_work(rows, k, n), or None (as in dd_linear)."""
+    dd_linear_grad_work(rows, k, n), a function, or None (as in dd_linear)."""
     kind, shape, dt = _half("dy", dy), dy.shape, dy.dtype
     n = shape[-1]
     rows = dy.numel() // n
@@ -569,17 +584,21 @@ def dd_linear_grad(dy, x=None, w=None, dx=None, dw=None, db=None, in_act="none",
     pw, sw, turned = _matrix("w", w, wide, dt) if dx is not None else (0, 0, 0)
     pdw, sdw, dturned = _matrix("dw", dw, wide, dt) if dw is not None else (0, 0, 0)
     pdb, bk = _bias("db", db, n, kind)
-    pwork = 0 if work is None else _work(work, dd_linear_grad_work(rows, k, n))
     act = _act(in_act) if dx is not None and not (rows == 0 and in_z is not None) else 0      # (tensors without rows have no address)
-    call, s = (_lib or lib()).dd_linear_grad, None if stream is None else _stream(stream)
+
     if dx is not None and dw is not None and turned != dturned:
         # (each by its own layout; dw first, as dx may be x)
-        rc = call(_LINEAR_GRAD.pack(rows, k, n, sd, sx, 0, 0, 0, sdw, pd, px, 0, 0, 0, pdw, pdb, pwork, kind, bk, 0, dturned), s)
-        if rc:
-            _check(rc)
+        _linear_grad((rows, k, n, sd, sx, 0, 0, 0, sdw, pd, px, 0, 0, 0, pdw, pdb), (kind, bk, 0, dturned), work, stream)
         pdw = pdb = 0
-    rc = call(_LINEAR_GRAD.pack(rows, k, n, sd, sx, sw, si, sdx, sdw, pd, px, pw, pi, pdx, pdw, pdb, pwork, kind, bk, act,
-                                turned if dx is not None else dturned), s)
+    _linear_grad((rows, k, n, sd, sx, sw, si, sdx, sdw, pd, px, pw, pi, pdx, pdw, pdb), (kind, bk, act, turned if dx is not None else dturned),
+                 work, stream)
+
+
+def _linear_grad(head, tail, work, stream):
+    at = 0
+    if work is not None:
+        at, work = _given(work, lib().dd_linear_grad_need, _LINEAR_GRAD, head, tail, dd_linear_grad_work)
+    rc = (_lib or lib()).dd_linear_grad(_LINEAR_GRAD.pack(*head, at, *tail), None if stream is None else _stream(stream))
     if rc:
         _check(rc)
 

@@ -83,6 +83,109 @@ size_t shared_work(int64_t rows, int64_t k, int64_t n) {
     return dd::padded_size(rows, n) + dd::padded_size(rows, k) + longer(with_w, longer(by_rows, by_sums));
 }
 
+dd_status check_linear(const dd_linear_args *a) {
+    if (!a) return fail(DD_EINVAL, "args is NULL");
+    CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
+    if (!act_type(a->act)) return fail(DD_EINVAL, "unknown act %d", a->act);
+    if (!aligned(a->bias, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "bias is not aligned to its elements");
+    if (a->rows == 0) return DD_OK;
+    CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
+    CHECK(check_rows("w", a->w, a->turned ? a->n : a->k, a->turned ? a->k : a->n, a->w_stride, a->type, false));
+    if (a->residual) CHECK(check_rows("residual", a->residual, a->rows, a->n, a->residual_stride, a->type, false));
+    CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
+    if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
+    return check_product(a->rows, a->n, a->k, true);
+}
+
+dd::Product product_of(const dd_linear_args &a) {
+    dd::Product p{a.x, a.w, a.rows, a.n, a.k, a.x_stride, a.w_stride, 1, a.turned, a.type, 0, 0, {}};
+    p.e.bias = a.bias;
+    p.e.bias_type = a.bias_type;
+    p.e.act = a.act;
+    p.e.residual = a.residual;
+    p.e.side_stride = a.residual_stride;
+    p.e.z = a.z;
+    p.e.z_stride = a.z_stride;
+    p.e.out = a.y;
+    p.e.out_stride = a.y_stride;
+    return p;
+}
+
+dd_status check_linear_grad(const dd_linear_grad_args *a) {
+    if (!a) return fail(DD_EINVAL, "args is NULL");
+    CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
+    if (!act_type(a->in_act)) return fail(DD_EINVAL, "unknown in_act %d", a->in_act);
+    if (!a->in_z && a->in_act != DD_ACT_NONE) return fail(DD_EINVAL, "in_act needs in_z");
+    const int64_t wr = a->turned ? a->n : a->k, wc = a->turned ? a->k : a->n;
+    if (a->rows > 0) {
+        if (a->dx || a->dw || a->db) CHECK(check_rows("dy", a->dy, a->rows, a->n, a->dy_stride, a->type, false));
+        if (a->dw) CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
+        if (a->dx) {
+            CHECK(check_rows("w", a->w, wr, wc, a->w_stride, a->type, false));
+            if (a->in_z) CHECK(check_rows("in_z", a->in_z, a->rows, a->k, a->in_z_stride, a->type, false));
+            CHECK(check_rows("dx", a->dx, a->rows, a->k, a->dx_stride, a->type, true));
+            CHECK(check_product(a->rows, a->k, a->n, true));
+        }
+    }
+    if (a->dw) {
+        CHECK(check_rows("dw", a->dw, wr, wc, a->dw_stride, a->type, true));
+        CHECK(check_product(wr, wc, a->rows, false));
+    }
+    if (!aligned(a->db, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "db is not aligned to its elements");
+    return DD_OK;
+}
+
+// The two products of a gradient, and the copies of operands that they share.
+struct Gradients {
+    const dd_linear_grad_args &a;
+    dd::GradCopies copies{};
+    int32_t small;
+    dd::Product dw{}, dx{};
+    dd::PadRows pads[3];
+    size_t copied;                  // bytes of the copies
+
+    explicit Gradients(const dd_linear_grad_args &args) : a(args) {
+        if (a.dw && a.dx && a.rows > 0) {
+            const bool of_dy = !dd::loads_directly(a.dy, a.dy_stride, true, a.rows, a.n) || !dd::loads_directly(a.dy, a.dy_stride, false, a.n, a.rows);
+            copies = dd::grad_copies(a.rows, a.k, a.n, a.turned, dd::GradCopies{of_dy, !dd::loads_directly(a.x, a.x_stride, false, a.k, a.rows),
+                                                                             !dd::loads_directly(a.w, a.w_stride, !a.turned, a.k, a.n)});
+        }
+        small = a.rows > 0 && dd::small_gradients(a.rows, a.k, a.n, a.turned);
+        copied = lay_out(reinterpret_cast<char *>(uintptr_t(16)));      // (an address as aligned as the memory's)
+    }
+    // with the copies in `work` (of which the size is returned)
+    size_t lay_out(char *work) {
+        const char *begin = work;
+        const int64_t wr = a.turned ? a.n : a.k, wc = a.turned ? a.k : a.n;
+        const void *dy = a.dy, *x = a.x, *w = a.w;
+        int64_t dy_stride = a.dy_stride, x_stride = a.x_stride, w_stride = a.w_stride;
+        for (dd::PadRows &r : pads) r = dd::PadRows{};
+        dd::PadRows *r = pads;
+        if (copies.dy) work += dd::pad_rows(dy, dy_stride, a.rows, a.n, work, r++);
+        if (copies.x) work += dd::pad_rows(x, x_stride, a.rows, a.k, work, r++);
+        if (copies.w) work += dd::pad_rows(w, w_stride, wr, wc, work, r++);
+        dw = dd::Product{x, dy, wr, wc, a.rows, x_stride, dy_stride, 0, 0, a.type, copies.x | copies.dy << 1, small, {}};
+        if (a.turned) dw = dd::Product{dy, x, wr, wc, a.rows, dy_stride, x_stride, 0, 0, a.type, copies.dy | copies.x << 1, small, {}};
+        dw.e.out = a.dw;
+        dw.e.out_stride = a.dw_stride;
+        dx = dd::Product{dy, w, a.rows, a.k, a.n, dy_stride, w_stride, 1, !a.turned, a.type, copies.dy | copies.w << 1, small, {}};
+        dx.e.in_z = a.in_z;
+        dx.e.side_stride = a.in_z_stride;
+        dx.e.in_act = a.in_act;
+        dx.e.out = a.dx;
+        dx.e.out_stride = a.dx_stride;
+        return (size_t)(work - begin);
+    }
+    size_t need() const {
+        size_t most = 0;
+        auto needs = [&](size_t x) { most = x > most ? x : most; };
+        if (a.dw) needs(dd::product_need(dw));
+        if (a.db) needs(dd::column_sum_work(a.rows, a.n));
+        if (a.dx && a.rows > 0) needs(dd::product_need(dx));
+        return copied + most;
+    }
+};
+
 dd_status check_table(int64_t tokens, int64_t vocab, int64_t cols, int32_t type, const void *ids, int32_t id_bytes, float scale, int32_t reserved) {
     if (tokens < 0 || vocab < 1 || cols < 1) return fail(DD_EINVAL, "tokens must be at least 0, vocab and cols at least 1");
     if (tokens >= (int64_t(1) << 28) || vocab >= kMost || cols >= kMost)
@@ -101,29 +204,21 @@ extern "C" {
 
 size_t dd_linear_work(int64_t rows, int64_t k, int64_t n) { return sizes_known(rows, k, n) && rows > 0 ? dd::product_work(rows, n, k, true) : 0; }
 
+size_t dd_linear_need(const dd_linear_args *a) {
+    size_t need = 0;
+    guarded([&] {
+        CHECK(check_linear(a));
+        if (a->rows) need = dd::product_need(product_of(*a));
+        return DD_OK;
+    });
+    return need;
+}
+
 dd_status dd_linear(const dd_linear_args *a, void *stream) {
     return guarded([&] {
-        if (!a) return fail(DD_EINVAL, "args is NULL");
-        CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
-        if (!act_type(a->act)) return fail(DD_EINVAL, "unknown act %d", a->act);
-        if (!aligned(a->bias, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "bias is not aligned to its elements");
+        CHECK(check_linear(a));
         if (a->rows == 0) return DD_OK;
-        CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
-        CHECK(check_rows("w", a->w, a->turned ? a->n : a->k, a->turned ? a->k : a->n, a->w_stride, a->type, false));
-        if (a->residual) CHECK(check_rows("residual", a->residual, a->rows, a->n, a->residual_stride, a->type, false));
-        CHECK(check_rows("y", a->y, a->rows, a->n, a->y_stride, a->type, true));
-        if (a->z) CHECK(check_rows("z", a->z, a->rows, a->n, a->z_stride, a->type, true));
-        CHECK(check_product(a->rows, a->n, a->k, true));
-        dd::Product p{a->x, a->w, a->rows, a->n, a->k, a->x_stride, a->w_stride, 1, a->turned, a->type, 0, 0, {}};
-        p.e.bias = a->bias;
-        p.e.bias_type = a->bias_type;
-        p.e.act = a->act;
-        p.e.residual = a->residual;
-        p.e.side_stride = a->residual_stride;
-        p.e.z = a->z;
-        p.e.z_stride = a->z_stride;
-        p.e.out = a->y;
-        p.e.out_stride = a->y_stride;
+        const dd::Product p = product_of(*a);
         hipStream_t s = (hipStream_t)stream;
         return with_work(a->work, dd::product_need(p), s, "linear", [&](void *work) { return dd::launch_product(p, work, s); });
     });
@@ -138,79 +233,36 @@ size_t dd_linear_grad_work(int64_t rows, int64_t k, int64_t n) {
     return shared > most ? shared : most;
 }
 
+size_t dd_linear_grad_need(const dd_linear_grad_args *a) {
+    size_t need = 0;
+    guarded([&] {
+        CHECK(check_linear_grad(a));
+        Gradients g(*a);
+        need = g.need();
+        return DD_OK;
+    });
+    return need;
+}
+
 dd_status dd_linear_grad(const dd_linear_grad_args *a, void *stream) {
     return guarded([&] {
-        if (!a) return fail(DD_EINVAL, "args is NULL");
-        CHECK(check_layer(a->rows, a->k, a->n, a->type, a->bias_type, a->turned));
-        if (!act_type(a->in_act)) return fail(DD_EINVAL, "unknown in_act %d", a->in_act);
-        if (!a->in_z && a->in_act != DD_ACT_NONE) return fail(DD_EINVAL, "in_act needs in_z");
-        const int64_t wr = a->turned ? a->n : a->k, wc = a->turned ? a->k : a->n;
-        if (a->rows > 0) {
-            if (a->dx || a->dw || a->db) CHECK(check_rows("dy", a->dy, a->rows, a->n, a->dy_stride, a->type, false));
-            if (a->dw) CHECK(check_rows("x", a->x, a->rows, a->k, a->x_stride, a->type, false));
-            if (a->dx) {
-                CHECK(check_rows("w", a->w, wr, wc, a->w_stride, a->type, false));
-                if (a->in_z) CHECK(check_rows("in_z", a->in_z, a->rows, a->k, a->in_z_stride, a->type, false));
-                CHECK(check_rows("dx", a->dx, a->rows, a->k, a->dx_stride, a->type, true));
-                CHECK(check_product(a->rows, a->k, a->n, true));
-            }
-        }
-        if (a->dw) {
-            CHECK(check_rows("dw", a->dw, wr, wc, a->dw_stride, a->type, true));
-            CHECK(check_product(wr, wc, a->rows, false));
-        }
-        if (!aligned(a->db, dd::elem_size(a->bias_type))) return fail(DD_EINVAL, "db is not aligned to its elements");
+        CHECK(check_linear_grad(a));
         hipStream_t s = (hipStream_t)stream;
-        dd::GradCopies copies{};
-        if (a->dw && a->dx && a->rows > 0) {
-            const bool of_dy = !dd::loads_directly(a->dy, a->dy_stride, true, a->rows, a->n) || !dd::loads_directly(a->dy, a->dy_stride, false, a->n, a->rows);
-            copies = dd::grad_copies(a->rows, a->k, a->n, a->turned, dd::GradCopies{of_dy, !dd::loads_directly(a->x, a->x_stride, false, a->k, a->rows),
-                                                                                     !dd::loads_directly(a->w, a->w_stride, !a->turned, a->k, a->n)});
-        }
-        const int32_t small = a->rows > 0 && dd::small_gradients(a->rows, a->k, a->n, a->turned);
-        // the two products, with copies in `work` (of which the size is returned)
-        dd::Product dw{}, dx{};
-        dd::PadRows pads[3];
-        auto lay_out = [&](char *work) {
-            const char *begin = work;
-            const void *dy = a->dy, *x = a->x, *w = a->w;
-            int64_t dy_stride = a->dy_stride, x_stride = a->x_stride, w_stride = a->w_stride;
-            for (dd::PadRows &r : pads) r = dd::PadRows{};
-            dd::PadRows *r = pads;
-            if (copies.dy) work += dd::pad_rows(dy, dy_stride, a->rows, a->n, work, r++);
-            if (copies.x) work += dd::pad_rows(x, x_stride, a->rows, a->k, work, r++);
-            if (copies.w) work += dd::pad_rows(w, w_stride, wr, wc, work, r++);
-            dw = dd::Product{x, dy, wr, wc, a->rows, x_stride, dy_stride, 0, 0, a->type, copies.x | copies.dy << 1, small, {}};
-            if (a->turned) dw = dd::Product{dy, x, wr, wc, a->rows, dy_stride, x_stride, 0, 0, a->type, copies.dy | copies.x << 1, small, {}};
-            dw.e.out = a->dw;
-            dw.e.out_stride = a->dw_stride;
-            dx = dd::Product{dy, w, a->rows, a->k, a->n, dy_stride, w_stride, 1, !a->turned, a->type, copies.dy | copies.w << 1, small, {}};
-            dx.e.in_z = a->in_z;
-            dx.e.side_stride = a->in_z_stride;
-            dx.e.in_act = a->in_act;
-            dx.e.out = a->dx;
-            dx.e.out_stride = a->dx_stride;
-            return (size_t)(work - begin);
-        };
-        const size_t copied = lay_out(reinterpret_cast<char *>(uintptr_t(16)));      // (an address as aligned as the memory's)
-        size_t need = 0;
-        auto needs = [&](size_t x) { need = x > need ? x : need; };
-        if (a->dw) needs(dd::product_need(dw));
-        if (a->db) needs(dd::column_sum_work(a->rows, a->n));
-        if (a->dx && a->rows > 0) needs(dd::product_need(dx));
-        return with_work(a->work, copied + need, s, "linear gradient", [&](void *given) {
+        Gradients g(*a);
+        return with_work(a->work, g.need(), s, "linear gradient", [&](void *given) {
             char *work = static_cast<char *>(given);
             hipError_t e = hipSuccess;
             bool summed = false;
-            if (copied) {
-                work += lay_out(work);
+            if (g.copied) {
+                work += g.lay_out(work);
                 dd::FewSums sums{};
                 if (a->db && dd::few_rows(a->rows, a->n)) {
                     sums = dd::FewSums{a->dy, a->db, a->dy_stride, a->n, (int32_t)a->rows, a->type, a->bias_type};
                     summed = true;
                 }
-                e = dd::launch_pad_rows(pads[0], pads[1], pads[2], sums, s);
+                e = dd::launch_pad_rows(g.pads[0], g.pads[1], g.pads[2], sums, s);
             }
+            const dd::Product &dw = g.dw, &dx = g.dx;
             const void *x = a->turned ? dw.q : dw.p;
             const int64_t x_stride = a->turned ? dw.q_stride : dw.p_stride;
             const bool both = a->dw && a->dx && a->rows > 0 && dd::goes_together(dw, dx) && !overlap(a->dx, a->dx_stride, x, x_stride, a->rows, a->k);

@@ -102,8 +102,7 @@ def _linear(x, weight, bias, residual, act, want_z):
     y = torch.empty(shape, dtype=x.dtype, device=x.device)
     z = torch.empty_like(y) if want_z else None
     with _on(x, weight, bias, residual):
-        work = _workspace(B.dd_linear_work(x.numel() // k, k, n), x)
-        B.dd_linear(x, weight, y, bias=bias, residual=residual, act=act, z=z, work=work, stream=_stream())
+        B.dd_linear(x, weight, y, bias=bias, residual=residual, act=act, z=z, work=lambda size: _workspace(size, x), stream=_stream())
     return y, z
 
 
@@ -115,8 +114,8 @@ def _linear_grad(dy, x, weight, bias, wanted, in_act="none", in_z=None):
     db = torch.empty_like(bias) if wanted[2] and bias is not None else None
     if dx is not None or dw is not None or db is not None:
         with _on(dy, x, weight, bias):
-            work = _workspace(B.dd_linear_grad_work(dy.numel() // n, k, n), dy)
-            B.dd_linear_grad(dy, x, weight, dx=dx, dw=dw, db=db, in_act=in_act, in_z=in_z, work=work, stream=_stream())
+            B.dd_linear_grad(dy, x, weight, dx=dx, dw=dw, db=db, in_act=in_act, in_z=in_z, work=lambda size: _workspace(size, dy),
+                             stream=_stream())
     return dx, dw, db
 
 

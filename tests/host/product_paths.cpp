@@ -4,7 +4,7 @@
 //   product_paths          reads calls, "fwd" or "grad", rows, k, n, pad (elements between rows), turned, type
 //                          (0: bf16, 1: f16), wanted (1 dx, 2 dw, 4 db), a line each; writes a line for each
 //   product_paths draw N   N drawn calls: what is loaded to LDS directly lies within the reach of a load's
-//                          offset, all that is written to working memory within the bytes that are asked for, and a
+//                          offset, all that is written to working memory within the bytes that the call needs and its sizes ask for, and a
 //                          gradient alone is cut as it is beside the others where operands load directly
 #include "k_linear.hip"
 
@@ -22,7 +22,7 @@ using dd::Plan;
 using dd::Product;
 
 static char *const kWork = reinterpret_cast<char *>(uintptr_t(1) << 50);       // (never touched)
-static size_t room = 0, used = 0;
+static size_t room = 0, need = 0, used = 0;       // by sizes, of the call, and written
 static std::string said;
 static int bad = 0;
 static const void *y_at, *dx_at, *dw_at, *given[3];
@@ -162,6 +162,7 @@ static dd_status run(const Call &c, unsigned odd = 0) {
         a.type = a.bias_type = c.type ? DD_F16 : DD_BF16;
         a.turned = c.turned;
         room = dd_linear_work(c.rows, c.k, c.n);
+        need = dd_linear_need(&a);
         return dd_linear(&a, nullptr);
     }
     dd_linear_grad_args a;
@@ -184,6 +185,7 @@ static dd_status run(const Call &c, unsigned odd = 0) {
     a.type = a.bias_type = c.type ? DD_F16 : DD_BF16;
     a.turned = c.turned;
     room = dd_linear_grad_work(c.rows, c.k, c.n);
+    need = dd_linear_grad_need(&a);
     return dd_linear_grad(&a, nullptr);
 }
 
@@ -202,7 +204,8 @@ int main(int argc, char **argv) {
             if (gen() % 3 == 0) c.rows = (c.rows + 7) / 8 * 8, c.k = (c.k + 7) / 8 * 8, c.n = (c.n + 7) / 8 * 8;
             const dd_status st = run(c, gen() % 3 ? 0 : gen() % 8);
             EXPECT(st == DD_OK || st == DD_EINVAL);
-            EXPECT(used <= room);
+            EXPECT(used <= need && need <= room);
+            EXPECT(st == DD_OK || need == 0);
             // operands that load directly: what is wanted alone has the tiles and parts that it has beside the other
             if (!c.grad || st != DD_OK || c.k % 8 || c.n % 8 || c.pad % 8) continue;
             c.wanted = 7;
@@ -225,7 +228,7 @@ int main(int argc, char **argv) {
     while (scanf("%7s %lld %lld %lld %lld %d %d %d", op, &c.rows, &c.k, &c.n, &c.pad, &c.turned, &c.type, &c.wanted) == 8) {
         c.grad = !strcmp(op, "grad");
         const dd_status st = run(c);
-        printf("%d %zu %zu %s\n", (int)st, used, room, said.c_str());
+        printf("%d %zu %zu %zu %s\n", (int)st, used, need, room, said.c_str());
     }
     return bad ? 1 : 0;
 }

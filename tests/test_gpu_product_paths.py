@@ -123,3 +123,48 @@ def test_rows_longer_than_a_load_reaches():
         assert torch.equal(dw[:, c], (x.float().t() @ dy[:, c].float()).to(torch.bfloat16)), c
         want += dy[:, c].double() @ w[:, c].double().t()
     assert torch.equal(dx, want.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("case", [c for c in CASES if "cut" in c[6] or "c" in c[6].replace("direct", "").replace("rounds", "")][::5], ids=name)
+def test_working_memory_of_a_call(case):
+    """A function is asked for what the call uses: no less, as nothing behind it is touched, and the same bits."""
+    import torch
+    require_gpu()
+    op, rows, k, n, pad, turned, _ = case
+    gen = torch.Generator("cuda").manual_seed(k)
+    x, w, dy = (Rows(rand(gen, a, b, torch.bfloat16), pad).t for a, b in ((rows, k), (n, k) if turned else (k, n), (rows, n)))
+    asked = []
+
+    def give(size):
+        asked.append(torch.full((1024 + size + 4096,), 171, device="cuda", dtype=torch.uint8))
+        return asked[-1][1024:1024 + size]
+    got = []
+    for work in (None, give):
+        y, dx, dw, db = (torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in ((rows, n), (rows, k), w.shape, (n,)))
+        if op == "fwd":
+            B.dd_linear(x, w.t() if turned else w, y, work=work)
+        else:
+            B.dd_linear_grad(dy, x, w.t() if turned else w, dx=dx, dw=dw.t() if turned else dw, db=db, work=work)
+        torch.cuda.synchronize()
+        got.append((y, dx, dw, db))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert len(asked) == 1 and bool((asked[0][:1024] == 171).all()) and bool((asked[0][-4096:] == 171).all())
+
+
+def test_layers_take_no_memory_that_they_do_not_use():
+    """Aligned rows: the gradient's peak is its outputs, dz and the sums' parts."""
+    import torch
+    from paper_2006_03318_amd.training import linear
+    require_gpu()
+    x, w = (torch.ones(s, device="cuda", dtype=torch.bfloat16, requires_grad=True) for s in ((8192, 1024), (1024, 1024)))
+    for _ in range(2):
+        x.grad = w.grad = None
+        y = linear(x, w, act="relu")
+        dy = torch.ones_like(y)
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        y.backward(dy)
+        torch.cuda.synchronize()
+        over = torch.cuda.max_memory_allocated() - before
+    assert over <= 2 * x.numel() * 2 + w.numel() * 2 + (2 << 20)
